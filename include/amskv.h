@@ -50,7 +50,9 @@ typedef enum {
   AMSKV_ERR_NO_HOST_MEMORY = -8   /* a host allocation failed; destroy the cache             */
 } amskv_status;
 
-enum { AMSKV_DTYPE_F32 = 0, AMSKV_DTYPE_BF16 = 1 };
+enum { AMSKV_DTYPE_F32 = 0, AMSKV_DTYPE_BF16 = 1, AMSKV_DTYPE_BF16_KV8 = 2 /* see "8-bit cache" below */ };
+enum { AMSKV_KV8_BLOCK = 16 }; /* tokens of a scale that share a power of two in an 8-bit cache */
+enum { AMSKV_ROPE_HALF = 0, AMSKV_ROPE_INTERLEAVED = 1 };
 enum { AMSKV_LAYOUT_COMPACT = 0, AMSKV_LAYOUT_PLANNED = 1 };
 enum { AMSKV_MODE_SCALE_WINDOW = 0, AMSKV_MODE_TOKEN_BUDGET = 1, AMSKV_MODE_TOKEN_WINDOW = 2 };
 enum { AMSKV_IO_HEAD_MAJOR = 0, AMSKV_IO_TOKEN_MAJOR = 1 };
@@ -67,7 +69,7 @@ typedef struct {
   const int32_t* side_h;  /* host, [n_scales], each >= 1                  */
   const int32_t* side_w;  /* host, [n_scales], each >= 1                  */
   int32_t batch;          /* B >= 1                                       */
-  int32_t dtype;          /* AMSKV_DTYPE_F32 or AMSKV_DTYPE_BF16          */
+  int32_t dtype;          /* AMSKV_DTYPE_F32, _BF16 or _BF16_KV8          */
 } amskv_schedule;
 
 /* Per-layer policy in scale units (Section 4.3; Algorithm 2 with budgets counted in whole
@@ -177,6 +179,19 @@ typedef struct {
  * K_dev/V_dev of scale s must stay valid and unchanged until the iteration has run: until the
  * work enqueued by the next amskv_append_scale / amskv_cache_settle / query on the layer has
  * finished, or until amskv_cache_reset. */
+
+/* 8-bit cache (dtype = AMSKV_DTYPE_BF16_KV8).  Q, K, V and O are bf16; the arena holds K and V in 8 bits.  Every
+ * AMSKV_KV8_BLOCK consecutive tokens of a scale (counted from its first token; the last block may be shorter) share one power
+ * of two per (b, h) and tensor.  With m the largest magnitude of such a block of tokens x D and e the least integer >= -100 with
+ * m <= 448 * 2^e, an element x is held as the e4m3 number nearest to x / 2^e (4 significant bits, ties to even; x must be
+ * finite; beyond 1.875 * 2^127 as that), which stands for that number times 2^e -- a bf16 number exactly, so that nothing else is lost on the way into the
+ * attention: relative error at most 2^-4, absolute error at most 2^(e-10) below 2^(e-6), elements below 2^-110 become 0.
+ * amskv_attend reads the cached values, the current scale's included, unless that scale is read in place
+ * (borrow_unretained), in which case its bf16 K and V are read as they are.  amskv_cache_export writes the values as bf16.
+ * Scale-window mode in either layout, either io layout; fuse_append must be 0.  Slots start at multiples of AMSKV_KV8_BLOCK
+ * tokens and capacities are multiples of it.  amskv_cache_bytes_held counts one byte per element and one per block.  The
+ * similarity and density calls are for 16- and 32-bit caches: they return AMSKV_ERR_INVALID_ARG (a model is profiled on one
+ * of those). */
 
 /* mode = AMSKV_MODE_TOKEN_WINDOW.  The sliding-window and sink-plus-window kept sets that the
  * comparison with other cache strategies (Section 5, the table of SWA / H2O / STA) sets against
@@ -384,6 +399,93 @@ int32_t amskv_cache_reset(amskv_cache* cache);
 
 /* Free the host metadata.  The arena stays the caller's. */
 void amskv_cache_destroy(amskv_cache* cache);
+
+/* ---------------------------------------------------------------- rotary positions
+ * Queries and keys turned by the positions of their tokens, channel pair by channel pair, so that their products depend on
+ * differences of positions.  Of the D channels the first rot_dim turn; pair i = 0 .. rot_dim/2 - 1 is (x, y) =
+ *   channels (i, i + rot_dim/2)     AMSKV_ROPE_HALF
+ *   channels (2i, 2i + 1)           AMSKV_ROPE_INTERLEAVED
+ * and becomes (x c - y s, y c + x s) with (c, s) = amplitude * (cos, sin)(position * frequency).  With n pairs to an axis, pair
+ * i of an axis has the frequency base^(-i/n): one axis takes all pairs (n = rot_dim/2, the position in a sequence); of two,
+ * the first takes the first half of the pairs and the second the rest (n = rot_dim/4, row and column of a grid).
+ * Long contexts: frequency f becomes f * (g + (1 - g) / factor), where g = 0 for low = high = 0 (all pairs interpolated), else
+ * g = (original * f / 2 pi - low) / (high - low) clamped to [0, 1]: pairs that turn more than `high` times over the `original`
+ * positions of the training keep their frequency, pairs that turn less than `low` times are interpolated. */
+typedef struct {
+  int32_t rot_dim;  /* a multiple of 16, 16 .. head_dim                         */
+  int32_t pairing;  /* AMSKV_ROPE_HALF or AMSKV_ROPE_INTERLEAVED                */
+  int32_t axes;     /* 1 or 2                                                   */
+  double base;      /* > 0                                                      */
+  double factor;    /* >= 1; 1: frequencies as they are                         */
+  double original;  /* > 0 where low < high                                     */
+  double low, high; /* 0 <= low < high, or both 0                               */
+  double amplitude; /* > 0                                                      */
+} amskv_rope;
+
+/* Distances in elements between batch elements, heads and tokens of a tensor; the channels of a row are contiguous.  Rows start
+ * at multiples of 16 bytes.  A dimension of size 1 may have any stride, and a tensor that is only read may repeat (stride 0). */
+typedef struct {
+  int64_t batch, head, token;
+} amskv_strides;
+
+/* The cosines and sines of n tokens: positions_dev[n][axes] fp64 -> table_dev[n][rot_dim/2][2] fp32.  Angles are formed and
+ * reduced in 64 bits and every entry is rounded once, so positions may lie anywhere (whole and broken, negative, far).  A table is
+ * made once for a scale, or for the tokens of a step, and used by every layer.  Asynchronous on `stream`. */
+int32_t amskv_rope_table(const amskv_rope* rope, const double* positions_dev, int64_t n, float* table_dev, void* stream);
+
+/* out = x turned, for a tensor [batch][heads][tokens][head_dim] of fp32 or bf16 in any order of its dimensions (x, out strides).
+ * Row t of batch element b turns by table_dev[b * table_batch + t * rot_dim ...] (table_batch in floats; 0: one table for all).
+ * inverse != 0 turns back: the gradient with respect to x of a loss whose gradient with respect to out is given.  fp32
+ * arithmetic, every product rounded by itself (the same bits whoever forms them), one rounding to bf16.  out_dev == x_dev with
+ * equal strides turns in place; otherwise the two must not overlap.  tokens == 0, heads == 0 or batch == 0: nothing to do.
+ * rope gives rot_dim and pairing; its other members are not read.  head_dim 64 or 128.  Asynchronous on `stream`. */
+int32_t amskv_rotate(const amskv_rope* rope, int32_t dtype, int32_t head_dim, int32_t batch, int32_t heads, int32_t tokens,
+                     const float* table_dev, int64_t table_batch, int32_t inverse, const void* x_dev, const amskv_strides* x,
+                     void* out_dev, const amskv_strides* out, void* stream);
+
+/* amskv_append_scale with the scale's keys, and its queries, turned on the way: table_dev holds the T_s tokens of scale s
+ * (amskv_rope_table; one table for all batch rows).  Q_dev turned goes to Q_out_dev, which is laid out as amskv_attend will read
+ * it and may be Q_dev itself if that is too; in a token-major cache q_token_stride is the token stride of Q_dev (0: the cache's
+ * own for Q), so that Q may lie in a fused projection output and Q_out apart.  Q_dev == Q_out_dev == NULL turns keys only.
+ * Where the scale is copied into the cache its turned keys go straight to their slot (quantised in an 8-bit cache: the fp32
+ * result of the turn is rounded once) and K_dev is only read.  Where the scale is read in place instead
+ * (borrow_unretained for a scale no later step reads, fuse_append, the token modes), K_dev itself is turned in place.
+ * K_dev, V_dev and table_dev must not be NULL.  Otherwise, and in its status codes, amskv_append_scale. */
+int32_t amskv_append_scale_rotary(amskv_cache* cache, int32_t layer, int32_t s, const amskv_rope* rope, const float* table_dev,
+                                  const void* Q_dev, int64_t q_token_stride, void* Q_out_dev, void* K_dev, const void* V_dev,
+                                  void* stream);
+
+/* ---------------------------------------------------------------- cross attention
+ * Queries of a step over the states of an encoder (a prompt), which have a length of their own in every batch element:
+ *   O[b,h,i,:] = sum_j softmax_j(Q[b,h,i,:] . K[b,g,j,:] * softmax_scale) V[b,g,j,:],   j < length of b,  g = h / (heads / kv_heads)
+ * A batch element without states (length 0) gets O = 0.  What lies behind a batch element's last state is never read.  Lengths:
+ *   lengths_dev == offsets_dev == NULL   kv_tokens states in every batch element
+ *   lengths_dev[batch]                   lengths, of padded K and V (strides as given); values outside [0, kv_tokens] are clamped
+ *   offsets_dev[batch + 1]               ascending offsets into packed K and V: row j of b is row offsets[b] + j of one axis of
+ *                                        kv_rows rows (k.token, v.token; the batch strides are not used); b has offsets[b+1] -
+ *                                        offsets[b] states, of which what goes beyond kv_tokens or kv_rows is left out
+ * bf16: finite Q, K and V, fp32 accumulation and softmax, P rounded to bf16 before the second product, O rounded to bf16. */
+typedef struct {
+  int32_t batch, heads, kv_heads; /* heads a multiple of kv_heads                            */
+  int32_t head_dim;               /* 64 or 128                                               */
+  int32_t dtype;                  /* AMSKV_DTYPE_BF16                                        */
+  int32_t q_tokens;               /* queries of a batch element and head; 0: nothing to do   */
+  int32_t kv_tokens;              /* most states of a batch element                          */
+  int64_t kv_rows;                /* rows of packed K and V (offsets_dev); else not read     */
+  float softmax_scale;            /* 0 => 1/sqrt(head_dim)                                   */
+  amskv_strides q, k, v, o;       /* (.head of k and v: from one kv head to the next)        */
+} amskv_cross;
+
+/* Few queries over many states are shared between workgroups, whose partial results meet in a workspace: its size for this
+ * shape (0: none is used; depends on nothing but the numbers in *cross).  Host only. */
+int32_t amskv_cross_workspace_bytes(const amskv_cross* cross, uint64_t* bytes_out);
+
+/* workspace_dev: device, 16-byte aligned, at least amskv_cross_workspace_bytes (else AMSKV_ERR_ARENA_TOO_SMALL); nothing in it has
+ * to be kept or cleared.  Calls that may overlap in time need one each.  NULL: done without, by fewer workgroups; the same sums in
+ * another order.  Two launches with it, one without; kernels only, so the call can be captured.  Asynchronous on `stream`. */
+int32_t amskv_cross_attend(const amskv_cross* cross, const void* Q_dev, const void* K_dev, const void* V_dev, void* O_dev,
+                           const int32_t* lengths_dev, const int32_t* offsets_dev, void* workspace_dev,
+                           uint64_t workspace_bytes, void* stream);
 
 /* Static text for a status code. */
 const char* amskv_status_string(int32_t status);

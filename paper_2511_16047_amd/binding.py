@@ -25,7 +25,9 @@ AMSKV_ERR_NO_DEVICE_MEMORY = -6
 AMSKV_ERR_STATIC_LIMIT = -7
 AMSKV_ERR_NO_HOST_MEMORY = -8
 AMSKV_STATIC_MAX_UNITS = 16384
-AMSKV_DTYPE_F32, AMSKV_DTYPE_BF16 = 0, 1
+AMSKV_DTYPE_F32, AMSKV_DTYPE_BF16, AMSKV_DTYPE_BF16_KV8 = 0, 1, 2
+AMSKV_KV8_BLOCK = 16
+AMSKV_ROPE_HALF, AMSKV_ROPE_INTERLEAVED = 0, 1
 AMSKV_LAYOUT_COMPACT, AMSKV_LAYOUT_PLANNED = 0, 1
 AMSKV_MODE_SCALE_WINDOW, AMSKV_MODE_TOKEN_BUDGET, AMSKV_MODE_TOKEN_WINDOW = 0, 1, 2
 AMSKV_IO_HEAD_MAJOR, AMSKV_IO_TOKEN_MAJOR = 0, 1
@@ -41,6 +43,7 @@ EXPORTED = [
     "amskv_attention_density_enqueue", "amskv_attend_density",
     "amskv_cache_set_io_layout", "amskv_interscale_similarity_enqueue", "amskv_interscale_similarity_collect",
     "amskv_interscale_similarity_enqueue_static",
+    "amskv_rope_table", "amskv_rotate", "amskv_append_scale_rotary", "amskv_cross_workspace_bytes", "amskv_cross_attend",
 ]
 
 
@@ -67,6 +70,27 @@ class _Policy(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("layer", C.POINTER(_LayerPolicy)), ("softmax_scale", C.c_float),
                 ("layout", C.c_int32), ("borrow_unretained", C.c_int32), ("fuse_append", C.c_int32),
                 ("mode", C.c_int32), ("budget", C.POINTER(_LayerBudget))]
+
+
+class Rope(C.Structure):
+    """amskv_rope."""
+    _fields_ = [("rot_dim", C.c_int32), ("pairing", C.c_int32), ("axes", C.c_int32), ("base", C.c_double), ("factor", C.c_double),
+                ("original", C.c_double), ("low", C.c_double), ("high", C.c_double), ("amplitude", C.c_double)]
+
+    def __init__(self, rot_dim=0, pairing=AMSKV_ROPE_HALF, axes=1, base=10000.0, factor=1.0, original=0.0, low=0.0, high=0.0, amplitude=1.0):
+        super().__init__(rot_dim, pairing, axes, base, factor, original, low, high, amplitude)
+
+
+class Strides(C.Structure):
+    """amskv_strides: elements from one batch element, head and token to the next."""
+    _fields_ = [("batch", C.c_int64), ("head", C.c_int64), ("token", C.c_int64)]
+
+
+class Cross(C.Structure):
+    """amskv_cross."""
+    _fields_ = [("batch", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("q_tokens", C.c_int32), ("kv_tokens", C.c_int32), ("kv_rows", C.c_int64), ("softmax_scale", C.c_float),
+                ("q", Strides), ("k", Strides), ("v", Strides), ("o", Strides)]
 
 
 _lib = None
@@ -135,6 +159,17 @@ def load_library() -> C.CDLL:
     lib.amskv_interscale_similarity_collect.restype = i32
     lib.amskv_interscale_similarity_enqueue_static.argtypes = [vp, i32, i32, i32, vp, vp]
     lib.amskv_interscale_similarity_enqueue_static.restype = i32
+    pr, pst, px = C.POINTER(Rope), C.POINTER(Strides), C.POINTER(Cross)
+    lib.amskv_rope_table.argtypes = [pr, vp, i64, vp, vp]
+    lib.amskv_rope_table.restype = i32
+    lib.amskv_rotate.argtypes = [pr, i32, i32, i32, i32, i32, vp, i64, i32, vp, pst, vp, pst, vp]
+    lib.amskv_rotate.restype = i32
+    lib.amskv_append_scale_rotary.argtypes = [vp, i32, i32, pr, vp, vp, i64, vp, vp, vp, vp]
+    lib.amskv_append_scale_rotary.restype = i32
+    lib.amskv_cross_workspace_bytes.argtypes = [px, C.POINTER(u64)]
+    lib.amskv_cross_workspace_bytes.restype = i32
+    lib.amskv_cross_attend.argtypes = [px, vp, vp, vp, vp, vp, vp, vp, u64, vp]
+    lib.amskv_cross_attend.restype = i32
 
     try:
         from . import _pycalls
@@ -409,3 +444,41 @@ def amskv_cache_reset(cache):
 
 def amskv_cache_destroy(cache):
     load_library().amskv_cache_destroy(cache)
+
+
+# ------------------------------------------------------------------ rotary positions, cross attention
+def amskv_rope_table(rope, positions, table, n=None, stream=None):
+    """positions: device float64 [n][axes]; table: device float32 [n][rot_dim / 2][2]."""
+    if n is None:
+        n = positions.numel() // rope.axes if rope.axes else 0
+    _check(load_library().amskv_rope_table(rope, _ptr(positions), int(n), _ptr(table), _stream(stream)), "amskv_rope_table")
+
+
+def amskv_rotate(rope, dtype, head_dim, batch, heads, tokens, table, table_batch, x, x_strides, out, out_strides, inverse=False,
+                 stream=None):
+    """x_strides, out_strides: Strides; table_batch: floats from one batch element's table to the next one's (0: shared)."""
+    _check(load_library().amskv_rotate(rope, dtype, head_dim, batch, heads, tokens, _ptr(table), table_batch, int(bool(inverse)), _ptr(x),
+                                       x_strides, _ptr(out), out_strides, _stream(stream)), "amskv_rotate")
+
+
+def amskv_append_scale_rotary(cache, layer, s, rope, table, Q, q_token_stride, Q_out, K, V, stream=None):
+    """Q and Q_out may be None (keys only); K is turned in place where the scale is read in place."""
+    _check(load_library().amskv_append_scale_rotary(cache, layer, s, rope, _ptr(table), _ptr(Q), q_token_stride, _ptr(Q_out), _ptr(K),
+                                                    _ptr(V), _stream(stream)), "amskv_append_scale_rotary")
+
+
+def amskv_cross_workspace_bytes(cross) -> int:
+    out = C.c_uint64(0)
+    _check(load_library().amskv_cross_workspace_bytes(cross, C.byref(out)), "amskv_cross_workspace_bytes")
+    return int(out.value)
+
+
+def amskv_cross_attend(cross, Q, K, V, O, lengths=None, offsets=None, workspace=None, workspace_bytes=None, stream=None):
+    """lengths: device int32 [batch]; offsets: device int32 [batch + 1]; workspace: device tensor (its size is taken from it) or,
+    with workspace_bytes, an address."""
+    if workspace is None:
+        workspace_bytes = 0
+    elif workspace_bytes is None:
+        workspace_bytes = workspace.numel() * workspace.element_size()
+    _check(load_library().amskv_cross_attend(cross, _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(lengths), _ptr(offsets), _ptr(workspace),
+                                             workspace_bytes, _stream(stream)), "amskv_cross_attend")

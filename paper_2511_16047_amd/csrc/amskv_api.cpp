@@ -34,6 +34,7 @@ struct LayerState {
   int64_t cap = 0;         // tokens
   uint64_t k_off = 0;      // byte offset of the K region inside the arena
   uint64_t v_off = 0;
+  uint64_t k_exp = 0, v_exp = 0;  // 8-bit cache: of the exponents of their blocks
   int32_t last_scale = -1;
   std::vector<Segment> segs;        // ascending scale id
   std::vector<int32_t> last_evicted;
@@ -78,6 +79,12 @@ namespace {
 constexpr uint64_t kAlign = 256;
 inline uint64_t align_up(uint64_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
+inline bool eight_bits(int32_t dtype) { return dtype == AMSKV_DTYPE_BF16_KV8; }
+// tokens a slot for t tokens takes: whole blocks in an 8-bit cache
+inline int32_t slot_tokens(int32_t dtype, int32_t t) {
+  return eight_bits(dtype) ? (t + AMSKV_KV8_BLOCK - 1) / AMSKV_KV8_BLOCK * AMSKV_KV8_BLOCK : t;
+}
+
 // Section 4.1 taxonomy / Section 4.3 rolling rule in scale units: after scale s arrives the
 // layer holds the first n_condensed scales, the `window` scales before s, and s.
 inline bool resident(const amskv_layer_policy& p, int s, int k) {
@@ -105,7 +112,8 @@ int validate(int32_t layers, int32_t heads, int32_t head_dim, const amskv_schedu
   if (sc->n_scales < 1 || sc->n_scales > AMSKV_MAX_SCALES || !sc->side_h || !sc->side_w)
     return AMSKV_ERR_INVALID_ARG;
   if (sc->batch < 1) return AMSKV_ERR_INVALID_ARG;
-  if (sc->dtype != AMSKV_DTYPE_F32 && sc->dtype != AMSKV_DTYPE_BF16) return AMSKV_ERR_INVALID_ARG;
+  if (sc->dtype != AMSKV_DTYPE_F32 && sc->dtype != AMSKV_DTYPE_BF16 && !eight_bits(sc->dtype)) return AMSKV_ERR_INVALID_ARG;
+  if (eight_bits(sc->dtype) && (po->mode != AMSKV_MODE_SCALE_WINDOW || po->fuse_append != 0)) return AMSKV_ERR_INVALID_ARG;
   int64_t total = 0;
   for (int i = 0; i < sc->n_scales; ++i) {
     if (sc->side_h[i] < 1 || sc->side_w[i] < 1) return AMSKV_ERR_INVALID_ARG;
@@ -242,7 +250,7 @@ int64_t plan_slots(const amskv_layer_policy& p, const int32_t* tokens, int n_sca
 
 struct Plan {
   std::vector<int64_t> cap;
-  std::vector<uint64_t> k_off, v_off;
+  std::vector<uint64_t> k_off, v_off, k_exp, v_exp;
   std::vector<std::vector<int32_t>> slot;
   uint64_t ws_off = 0, dens_off = 0, total = 0;
 };
@@ -250,8 +258,8 @@ struct Plan {
 void build_plan(int32_t layers, int32_t heads, int32_t head_dim, const amskv_schedule* sc,
                 const amskv_policy* po, Plan* pl) {
   int32_t tokens[AMSKV_MAX_SCALES];
-  for (int i = 0; i < sc->n_scales; ++i) tokens[i] = sc->side_h[i] * sc->side_w[i];
-  const uint64_t eb = sc->dtype == AMSKV_DTYPE_BF16 ? 2 : 4;
+  for (int i = 0; i < sc->n_scales; ++i) tokens[i] = slot_tokens(sc->dtype, sc->side_h[i] * sc->side_w[i]);
+  const uint64_t eb = eight_bits(sc->dtype) ? 1 : sc->dtype == AMSKV_DTYPE_BF16 ? 2 : 4;
   const uint64_t row = (uint64_t)head_dim * eb;
   const uint64_t bh = (uint64_t)sc->batch * heads;
   const bool borrow = po->borrow_unretained != 0;
@@ -259,6 +267,8 @@ void build_plan(int32_t layers, int32_t heads, int32_t head_dim, const amskv_sch
   pl->cap.resize(layers);
   pl->k_off.resize(layers);
   pl->v_off.resize(layers);
+  pl->k_exp.resize(layers);
+  pl->v_exp.resize(layers);
   pl->slot.assign(layers, std::vector<int32_t>(AMSKV_MAX_SCALES, 0));
   for (int l = 0; l < layers; ++l) {
     int64_t cap;
@@ -273,6 +283,16 @@ void build_plan(int32_t layers, int32_t heads, int32_t head_dim, const amskv_sch
     at = align_up(at + bh * (uint64_t)cap * row);
     pl->v_off[l] = at;
     at = align_up(at + bh * (uint64_t)cap * row);
+    if (eight_bits(sc->dtype)) {
+      pl->k_exp[l] = at;
+      at = align_up(at + bh * (uint64_t)cap / AMSKV_KV8_BLOCK);
+      pl->v_exp[l] = at;
+      at = align_up(at + bh * (uint64_t)cap / AMSKV_KV8_BLOCK);
+    }
+  }
+  if (eight_bits(sc->dtype)) {  // neither similarity nor density: no workspaces
+    pl->ws_off = pl->dens_off = pl->total = at;
+    return;
   }
   pl->ws_off = at;
   // similarity workspace: per (tensor, b, h) four partial sums, then per (layer, tensor, h) four totals
@@ -299,6 +319,11 @@ inline RowMap caller_map(const amskv_cache* c, int64_t t, int64_t tok_stride) {
 inline RowMap arena_map(const amskv_cache* c, const LayerState& L) {
   const int64_t row = (int64_t)c->head_dim * c->elem_bytes;
   return RowMap{c->heads * L.cap * row, L.cap * row, row};
+}
+
+inline amskv::Codes codes(const amskv_cache* c, const LayerState& L) {
+  auto at = [&](uint64_t off) { return (unsigned char*)c->arena + off; };
+  return {at(L.k_off), at(L.v_off), at(L.k_exp), at(L.v_exp)};
 }
 
 inline bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
@@ -692,7 +717,7 @@ int32_t amskv_cache_create(int32_t layers, int32_t heads, int32_t head_dim,
   // the token window is the token-budget machinery with one fixed budget and oversize scales cut
   c->mode = po->mode == AMSKV_MODE_TOKEN_WINDOW ? AMSKV_MODE_TOKEN_BUDGET : po->mode;
   c->cut_oversize = po->mode == AMSKV_MODE_TOKEN_WINDOW;
-  c->elem_bytes = sc->dtype == AMSKV_DTYPE_BF16 ? 2 : 4;
+  c->elem_bytes = sc->dtype == AMSKV_DTYPE_F32 ? 4 : 2;  // of Q, K, V and O
   c->softmax_scale = po->softmax_scale > 0.f ? po->softmax_scale : 1.0f / std::sqrt((float)head_dim);
   for (int i = 0; i < sc->n_scales; ++i) {
     c->side_h[i] = sc->side_h[i];
@@ -716,6 +741,8 @@ int32_t amskv_cache_create(int32_t layers, int32_t heads, int32_t head_dim,
     L.cap = pl.cap[l];
     L.k_off = pl.k_off[l];
     L.v_off = pl.v_off[l];
+    L.k_exp = pl.k_exp[l];
+    L.v_exp = pl.v_exp[l];
     for (int i = 0; i < AMSKV_MAX_SCALES; ++i) L.planned_off[i] = pl.slot[l][i];
   }
   if (c->mode == AMSKV_MODE_TOKEN_BUDGET && c->arena) {
@@ -732,8 +759,52 @@ int32_t amskv_cache_create(int32_t layers, int32_t heads, int32_t head_dim,
   return AMSKV_ERR_NO_HOST_MEMORY;  // nothing of the call may have taken effect on the host state that matters: callers destroy the cache
 }
 
-int32_t amskv_append_scale(amskv_cache* c, int32_t layer, int32_t s, const void* K_dev,
-                           const void* V_dev, void* stream) try {
+}  // extern "C"
+
+namespace {
+
+// Positions for the queries and keys of the scale being appended (amskv_append_scale_rotary).
+struct Turn {
+  const amskv_rope* rope;
+  const float* table;
+  const void* q;
+  int64_t q_token_stride;
+  void* q_out;
+};
+
+amskv::Take take_of(const amskv_cache* c, int32_t tokens) {
+  amskv::Take t{};
+  t.batch = c->batch;
+  t.heads = c->heads;
+  t.tokens = tokens;
+  t.head_dim = c->head_dim;
+  t.dtype = c->dtype == AMSKV_DTYPE_F32 ? AMSKV_DTYPE_F32 : AMSKV_DTYPE_BF16;
+  t.eight_bits = eight_bits(c->dtype);
+  return t;
+}
+
+void add_turn(const amskv_cache* c, const Turn& turn, int32_t tokens, amskv::Take* t) {
+  t->table = turn.table;
+  t->rot_dim = turn.rope->rot_dim;
+  t->pairing = turn.rope->pairing;
+  t->q = turn.q;
+  t->q_map = caller_map(c, tokens, turn.q_token_stride ? turn.q_token_stride : c->q_tok);
+  t->q_out = turn.q_out;
+  t->q_out_map = caller_map(c, tokens, c->q_tok);
+}
+
+// Q and K turned where no copy into the cache is made on the way: K stays where it is.
+int turn_in_place(const amskv_cache* c, const Turn& turn, int32_t tokens, const void* K_dev, hipStream_t st) {
+  amskv::Take t = take_of(c, tokens);
+  add_turn(c, turn, tokens, &t);
+  t.eight_bits = false;
+  t.k = K_dev;
+  t.k_out = const_cast<void*>(K_dev);  // amskv_append_scale_rotary's K_dev
+  t.kv_map = t.out_map = caller_map(c, tokens, c->kv_tok);
+  return amskv::launch_take(t, st) == hipSuccess ? AMSKV_OK : AMSKV_ERR_HIP;
+}
+
+int append_step(amskv_cache* c, int32_t layer, int32_t s, const void* K_dev, const void* V_dev, const Turn* turn, void* stream) {
   if (bad_layer(c, layer) || s < 0 || s >= c->n_scales) return AMSKV_ERR_INVALID_ARG;
   if ((K_dev == nullptr) != (V_dev == nullptr) || misaligned(K_dev) || misaligned(V_dev)) return AMSKV_ERR_INVALID_ARG;
   LayerState& L = c->layer[layer];
@@ -751,6 +822,7 @@ int32_t amskv_append_scale(amskv_cache* c, int32_t layer, int32_t s, const void*
     cur.scale = s;
     cur.len = c->tokens[s];
     cur.off = -1;
+    if (turn && (rc = turn_in_place(c, *turn, cur.len, K_dev, (hipStream_t)stream))) return rc;
     cur.ext_k = K_dev;
     cur.ext_v = V_dev;
     L.segs.push_back(cur);
@@ -779,11 +851,11 @@ int32_t amskv_append_scale(amskv_cache* c, int32_t layer, int32_t s, const void*
       if (n.off != g.off) {
         mv.src[mv.n] = g.off;
         mv.dst[mv.n] = n.off;
-        mv.len[mv.n] = g.len;
+        mv.len[mv.n] = slot_tokens(c->dtype, g.len);
         ++mv.n;
       }
     }
-    at += n.len;
+    at += slot_tokens(c->dtype, n.len);
     next.push_back(n);
   }
   Segment cur;
@@ -792,7 +864,7 @@ int32_t amskv_append_scale(amskv_cache* c, int32_t layer, int32_t s, const void*
   const bool keep_copy = stored(L.pol, s, c->n_scales, c->borrow != 0);
   if (keep_copy) {
     cur.off = c->layout == AMSKV_LAYOUT_COMPACT ? at : L.planned_off[s];
-    if ((int64_t)cur.off + cur.len > L.cap) return AMSKV_ERR_ARENA_TOO_SMALL;  // cannot happen: cap is the max over steps
+    if ((int64_t)cur.off + slot_tokens(c->dtype, cur.len) > L.cap) return AMSKV_ERR_ARENA_TOO_SMALL;  // cannot happen: cap is the max over steps
   } else {
     cur.off = -1;
     cur.ext_k = K_dev;
@@ -807,7 +879,35 @@ int32_t amskv_append_scale(amskv_cache* c, int32_t layer, int32_t s, const void*
   next.push_back(cur);
 
   const bool copy_now = keep_copy && !defer;
-  if (K_dev && (copy_now || mv.n > 0)) {
+  if (turn && !copy_now)
+    if (int rc = turn_in_place(c, *turn, cur.len, K_dev, (hipStream_t)stream)) return rc;
+  if (K_dev && (eight_bits(c->dtype) || (turn && copy_now))) {
+    // the survivors first, then the new scale: turned, quantised or both on the way to its slot
+    const hipStream_t st = (hipStream_t)stream;
+    hipError_t e = hipSuccess;
+    if (mv.n > 0)
+      e = eight_bits(c->dtype) ? amskv::launch_move_codes(codes(c, L), bh, c->head_dim, L.cap, mv, st)
+                               : amskv::launch_append(c->arena + L.k_off, c->arena + L.v_off, nullptr, nullptr, bh, row_bytes, L.cap, mv,
+                                                      cur.len, 0, 0, caller_map(c, cur.len, c->kv_tok), c->heads, st);
+    if (e == hipSuccess && copy_now) {
+      amskv::Take t = take_of(c, cur.len);
+      if (turn) add_turn(c, *turn, cur.len, &t);
+      t.k = K_dev;
+      t.v = V_dev;
+      t.kv_map = caller_map(c, cur.len, c->kv_tok);
+      t.cap_tokens = L.cap;
+      t.dst_new = cur.off;
+      if (t.eight_bits) {
+        t.codes = codes(c, L);
+      } else {
+        t.out_map = arena_map(c, L);
+        t.k_out = c->arena + L.k_off + (int64_t)cur.off * row_bytes;
+        t.v_out = c->arena + L.v_off + (int64_t)cur.off * row_bytes;
+      }
+      e = amskv::launch_take(t, st);
+    }
+    if (e != hipSuccess) return AMSKV_ERR_HIP;
+  } else if (K_dev && (copy_now || mv.n > 0)) {
     hipError_t e = amskv::launch_append(c->arena + L.k_off, c->arena + L.v_off, copy_now ? K_dev : nullptr,
                                         copy_now ? V_dev : nullptr, bh, row_bytes, L.cap, mv, cur.len,
                                         copy_now ? cur.off : 0, 0, caller_map(c, cur.len, c->kv_tok), c->heads,
@@ -818,6 +918,34 @@ int32_t amskv_append_scale(amskv_cache* c, int32_t layer, int32_t s, const void*
   L.last_evicted.swap(evicted);
   L.last_scale = s;
   return AMSKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t amskv_append_scale(amskv_cache* c, int32_t layer, int32_t s, const void* K_dev,
+                           const void* V_dev, void* stream) try {
+  return append_step(c, layer, s, K_dev, V_dev, nullptr, stream);
+} catch (const std::bad_alloc&) {
+  return AMSKV_ERR_NO_HOST_MEMORY;  // nothing of the call may have taken effect on the host state that matters: callers destroy the cache
+}
+
+int32_t amskv_append_scale_rotary(amskv_cache* c, int32_t layer, int32_t s, const amskv_rope* rope, const float* table_dev,
+                                  const void* Q_dev, int64_t q_token_stride, void* Q_out_dev, void* K_dev, const void* V_dev,
+                                  void* stream) try {
+  if (!c || !table_dev || !K_dev || !V_dev || (Q_dev == nullptr) != (Q_out_dev == nullptr)) return AMSKV_ERR_INVALID_ARG;
+  if (int rc = amskv::check_turn(rope, c->head_dim)) return rc;
+  if (misaligned(table_dev) || misaligned(Q_dev) || misaligned(Q_out_dev)) return AMSKV_ERR_INVALID_ARG;
+  if (c->io_layout == AMSKV_IO_HEAD_MAJOR) {
+    q_token_stride = 0;
+  } else if (q_token_stride != 0) {
+    const int64_t width = (int64_t)c->heads * c->head_dim, per16 = 16 / c->elem_bytes;
+    if (q_token_stride < width || q_token_stride % per16 != 0 || q_token_stride > ((int64_t)1 << 40)) return AMSKV_ERR_INVALID_ARG;
+    if (Q_dev == Q_out_dev && q_token_stride != c->q_tok) return AMSKV_ERR_INVALID_ARG;  // neither in place nor apart
+  }
+  const Turn turn{rope, table_dev, Q_dev, q_token_stride, Q_out_dev};
+  return append_step(c, layer, s, K_dev, V_dev, &turn, stream);
 } catch (const std::bad_alloc&) {
   return AMSKV_ERR_NO_HOST_MEMORY;  // nothing of the call may have taken effect on the host state that matters: callers destroy the cache
 }
@@ -836,6 +964,7 @@ static int attend_step(amskv_cache* c, int32_t layer, int32_t s, const void* Q_d
   if (s != L.last_scale) return AMSKV_ERR_ORDER;
   // token-budget mode: once the scale's iteration of Algorithm 1 has run it is no longer whole
   if (c->mode == AMSKV_MODE_TOKEN_BUDGET && !L.roll_pending) return AMSKV_ERR_ORDER;
+  if (mass_out_dev && eight_bits(c->dtype)) return AMSKV_ERR_INVALID_ARG;
   if (!c->arena) return AMSKV_ERR_NO_DEVICE_MEMORY;
   ExtKV ext;
   const SegTable t = seg_table(L, &ext);
@@ -941,6 +1070,9 @@ static int attend_step(amskv_cache* c, int32_t layer, int32_t s, const void* Q_d
     e = amskv::launch_attend_bf16(Q_dev, O_dev, c->arena + L.k_off, c->arena + L.v_off, bh,
                                   c->tokens[s], c->head_dim, L.cap, t, ext, io, c->softmax_scale,
                                   (hipStream_t)stream);
+  else if (eight_bits(c->dtype))
+    e = amskv::launch_attend_codes(Q_dev, O_dev, codes(c, L), bh, c->tokens[s], c->head_dim, L.cap, t, ext, io, c->softmax_scale,
+                                   (hipStream_t)stream);
   else
     e = amskv::launch_attend_f32(Q_dev, O_dev, c->arena + L.k_off, c->arena + L.v_off, bh,
                                  c->tokens[s], c->head_dim, L.cap, t, ext, io, c->softmax_scale,
@@ -971,7 +1103,7 @@ int32_t amskv_attend_density(amskv_cache* c, int32_t layer, int32_t s, const voi
 
 // Checks shared by the two ways of asking for Eq. 3; on success cur/prev point at the two whole scales.
 static int similarity_operands(amskv_cache* c, int32_t layer, int32_t s, const Segment** cur, const Segment** prev) {
-  if (bad_layer(c, layer) || s < 1 || s >= c->n_scales) return AMSKV_ERR_INVALID_ARG;
+  if (bad_layer(c, layer) || s < 1 || s >= c->n_scales || eight_bits(c->dtype)) return AMSKV_ERR_INVALID_ARG;
   if (int rc = finish_iteration(c, layer)) return rc;
   LayerState& L = c->layer[layer];
   if (s > L.last_scale) return AMSKV_ERR_ORDER;
@@ -1043,7 +1175,7 @@ int32_t amskv_interscale_similarity_enqueue_static(amskv_cache* c, int32_t layer
 
 int32_t amskv_interscale_similarity_collect(amskv_cache* c, float* cosK_host, float* cosV_host, float* sums_host,
                                             void* stream) try {
-  if (!c || !cosK_host) return AMSKV_ERR_INVALID_ARG;
+  if (!c || !cosK_host || eight_bits(c->dtype)) return AMSKV_ERR_INVALID_ARG;
   if (!c->arena) return AMSKV_ERR_NO_DEVICE_MEMORY;
   const size_t per_layer = 2 * (size_t)c->heads * 4;
   std::vector<float> host(per_layer * c->layers);
@@ -1076,7 +1208,8 @@ int32_t amskv_interscale_similarity_collect(amskv_cache* c, float* cosK_host, fl
 // is null, inside the arena's workspace; *totals is where, and *table describes the groups.
 static int density_launch(amskv_cache* c, int32_t layer, int32_t s, const void* Q_dev, hipStream_t st, SegTable* table,
                           float** totals, float* out_dev) {
-  if (bad_layer(c, layer) || s < 0 || s >= c->n_scales || !Q_dev || misaligned(Q_dev)) return AMSKV_ERR_INVALID_ARG;
+  if (bad_layer(c, layer) || s < 0 || s >= c->n_scales || !Q_dev || misaligned(Q_dev) || eight_bits(c->dtype))
+    return AMSKV_ERR_INVALID_ARG;
   if (int rc = finish_iteration(c, layer)) return rc;
   LayerState& L = c->layer[layer];
   if (s != L.last_scale) return AMSKV_ERR_ORDER;
@@ -1206,10 +1339,18 @@ int64_t amskv_cache_bytes_held(const amskv_cache* c, int32_t layer, int32_t incl
   if (bad_layer(c, layer)) return AMSKV_ERR_INVALID_ARG;
   if (int rc = finish_iteration(c, layer)) return rc;
   const LayerState& L = c->layer[layer];
-  int64_t tok = 0;
+  int64_t tok = 0, held = 0, blocks = 0;  // held, blocks: of an 8-bit cache
   for (const Segment& g : L.segs)
-    if (include_current || g.scale != L.last_scale) tok += g.len;
-  return 2 * (int64_t)c->elem_bytes * c->batch * c->heads * c->head_dim * tok;
+    if (include_current || g.scale != L.last_scale) {
+      if (eight_bits(c->dtype) && g.off >= 0) {
+        held += g.len;
+        blocks += slot_tokens(c->dtype, g.len) / AMSKV_KV8_BLOCK;
+      } else {
+        tok += g.len;
+      }
+    }
+  return 2 * (int64_t)c->batch * c->heads * (held * c->head_dim + blocks) +
+         2 * (int64_t)c->elem_bytes * c->batch * c->heads * c->head_dim * tok;
 }
 
 int64_t amskv_cache_capacity_tokens(const amskv_cache* c, int32_t layer) {
@@ -1227,6 +1368,11 @@ int32_t amskv_cache_export(const amskv_cache* c, int32_t layer, void* K_out_dev,
   ExtKV ext;
   const SegTable t = seg_table(L, &ext);
   if (t.ext_start < t.total && !ext.k) return AMSKV_ERR_NO_DEVICE_MEMORY;
+  if (eight_bits(c->dtype)) {
+    hipError_t e = amskv::launch_export_codes(codes(c, L), K_out_dev, V_out_dev, c->batch * c->heads, c->head_dim, L.cap, t, ext,
+                                              caller_map(c, L.segs.back().len, c->kv_tok), c->heads, (hipStream_t)stream);
+    return e == hipSuccess ? AMSKV_OK : AMSKV_ERR_HIP;
+  }
   hipError_t e = amskv::launch_export(c->arena + L.k_off, c->arena + L.v_off, K_out_dev, V_out_dev,
                                       c->batch * c->heads, c->head_dim * c->elem_bytes, L.cap, t, ext,
                                       caller_map(c, L.segs.back().len, c->kv_tok), c->heads, (hipStream_t)stream);

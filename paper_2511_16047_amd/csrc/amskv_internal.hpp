@@ -281,4 +281,64 @@ hipError_t launch_theta_flag(const float* totals_dev, int heads, double n_tok, f
 hipError_t launch_density_total(const float* partial_ws, int batch, int heads, int n_qblk, int n_groups, float* out_dev,
                                 hipStream_t st);
 
+// ---- rotary positions and the 8-bit cache.  Weak: a build of the host layer by itself need not have them (a cache without
+// either never calls them).
+#define AMSKV_WEAK __attribute__((weak))
+
+// A layer's K and V in 8 bits: codes [BH][cap][D], and per 16 tokens a biased exponent (value = code * 2^(byte - 127)),
+// [BH][cap / 16]; cap and every slot are multiples of 16 tokens.
+struct Codes {
+  unsigned char *k, *v, *k_exp, *v_exp;
+};
+
+// What becomes of a scale's tensors in one launch (take_kernels.hip): Q is turned, K is turned and put in its place, V is put
+// in its place.  A tensor whose source is null is left out.
+struct Take {
+  const void *q, *k, *v;
+  RowMap q_map, kv_map;             // rows of the sources
+  void *q_out, *k_out, *v_out;      // k_out, v_out: not read with eight_bits
+  RowMap q_out_map, out_map;        // rows of the destinations
+  Codes codes;                      // eight_bits: K and V become codes from token dst_new on, a multiple of 16
+  int64_t cap_tokens;
+  int32_t dst_new;
+  const float* table;               // null: nothing turns
+  int64_t table_batch;              // floats from a batch element's table to the next one's
+  int32_t rot_dim, pairing, inverse;
+  int32_t batch, heads, tokens, head_dim, dtype;  // dtype: of the sources, AMSKV_DTYPE_F32 or _BF16
+  bool eight_bits;
+};
+hipError_t launch_take(const Take& t, hipStream_t st) AMSKV_WEAK;
+// The survivors of a compaction slide to their new places (mv in tokens, whole blocks of 16).
+hipError_t launch_move_codes(const Codes& c, int bh, int head_dim, int64_t cap_tokens, const MoveList& mv, hipStream_t st) AMSKV_WEAK;
+// As launch_export, the values of the codes as bf16.
+hipError_t launch_export_codes(const Codes& c, void* k_out, void* v_out, int bh, int head_dim, int64_t cap_tokens, const SegTable& seg,
+                               const ExtKV& ext, const RowMap& ext_map, int heads, hipStream_t st) AMSKV_WEAK;
+hipError_t launch_attend_codes(const void* q, void* o, const Codes& c, int bh, int t_q, int head_dim, int64_t cap_tokens,
+                               const SegTable& seg, const ExtKV& ext, const CallerIo& io, float softmax_scale, hipStream_t st) AMSKV_WEAK;
+
+hipError_t launch_rope_table(const double* frequency, int pairs, int axes, double amplitude, const double* positions, int64_t n,
+                             float* table, hipStream_t st) AMSKV_WEAK;
+
+// Cross attention: K and V rows of the caller's, where each batch element's begin and how many there are left to the device.
+struct CrossCall {
+  const void *q, *k, *v;
+  void* o;
+  RowMap q_map, k_map, v_map, o_map;  // bytes
+  const int32_t *lengths, *offsets;   // at most one of them; none: kv_tokens rows in every batch element
+  int32_t batch, heads, kv_heads, head_dim, q_tokens, kv_tokens;
+  int64_t kv_rows;
+  float softmax_scale;
+  float* workspace;                   // null: not split
+};
+// Bytes of the workspace that a call of this shape uses (0: none).
+uint64_t cross_workspace_bytes(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) AMSKV_WEAK;
+hipError_t launch_cross(const CrossCall& c, hipStream_t st) AMSKV_WEAK;
+
+// What is wrong with a rotary description for rows of head_dim channels: AMSKV_OK or AMSKV_ERR_INVALID_ARG.
+inline int check_turn(const amskv_rope* r, int head_dim) {
+  const bool ok = r && r->rot_dim >= 16 && r->rot_dim <= head_dim && r->rot_dim % 16 == 0 &&
+                  (r->pairing == AMSKV_ROPE_HALF || r->pairing == AMSKV_ROPE_INTERLEAVED);
+  return ok ? AMSKV_OK : AMSKV_ERR_INVALID_ARG;
+}
+
 }  // namespace amskv
