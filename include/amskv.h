@@ -188,8 +188,9 @@ typedef struct {
  * attention: relative error at most 2^-4, absolute error at most 2^(e-10) below 2^(e-6), elements below 2^-110 become 0.
  * amskv_attend reads the cached values, the current scale's included, unless that scale is read in place
  * (borrow_unretained), in which case its bf16 K and V are read as they are.  amskv_cache_export writes the values as bf16.
- * Scale-window mode in either layout, either io layout; fuse_append must be 0.  Slots start at multiples of AMSKV_KV8_BLOCK
- * tokens and capacities are multiples of it.  amskv_cache_bytes_held counts one byte per element and one per block.  The
+ * Scale-window mode in either layout, either io layout (kv_token_stride below 2^23 elements); fuse_append must be 0.  Slots start at multiples of AMSKV_KV8_BLOCK
+ * tokens and capacities are multiples of it.  amskv_cache_bytes_held counts one byte per element and four per
+ * block and tensor.  The
  * similarity and density calls are for 16- and 32-bit caches: they return AMSKV_ERR_INVALID_ARG (a model is profiled on one
  * of those). */
 
@@ -464,6 +465,7 @@ int32_t amskv_append_scale_rotary(amskv_cache* cache, int32_t layer, int32_t s, 
  *   offsets_dev[batch + 1]               ascending offsets into packed K and V: row j of b is row offsets[b] + j of one axis of
  *                                        kv_rows rows (k.token, v.token; the batch strides are not used); b has offsets[b+1] -
  *                                        offsets[b] states, of which what goes beyond kv_tokens or kv_rows is left out
+ * The token strides of K and V are below 2^23 elements.
  * bf16: finite Q, K and V, fp32 accumulation and softmax, P rounded to bf16 before the second product, O rounded to bf16. */
 typedef struct {
   int32_t batch, heads, kv_heads; /* heads a multiple of kv_heads                            */

@@ -34,7 +34,7 @@ struct LayerState {
   int64_t cap = 0;         // tokens
   uint64_t k_off = 0;      // byte offset of the K region inside the arena
   uint64_t v_off = 0;
-  uint64_t k_exp = 0, v_exp = 0;  // 8-bit cache: of the exponents of their blocks
+  uint64_t k_scale = 0, v_scale = 0;  // 8-bit cache: of the powers of two of their blocks
   int32_t last_scale = -1;
   std::vector<Segment> segs;        // ascending scale id
   std::vector<int32_t> last_evicted;
@@ -250,7 +250,7 @@ int64_t plan_slots(const amskv_layer_policy& p, const int32_t* tokens, int n_sca
 
 struct Plan {
   std::vector<int64_t> cap;
-  std::vector<uint64_t> k_off, v_off, k_exp, v_exp;
+  std::vector<uint64_t> k_off, v_off, k_scale, v_scale;
   std::vector<std::vector<int32_t>> slot;
   uint64_t ws_off = 0, dens_off = 0, total = 0;
 };
@@ -267,8 +267,8 @@ void build_plan(int32_t layers, int32_t heads, int32_t head_dim, const amskv_sch
   pl->cap.resize(layers);
   pl->k_off.resize(layers);
   pl->v_off.resize(layers);
-  pl->k_exp.resize(layers);
-  pl->v_exp.resize(layers);
+  pl->k_scale.resize(layers);
+  pl->v_scale.resize(layers);
   pl->slot.assign(layers, std::vector<int32_t>(AMSKV_MAX_SCALES, 0));
   for (int l = 0; l < layers; ++l) {
     int64_t cap;
@@ -284,10 +284,10 @@ void build_plan(int32_t layers, int32_t heads, int32_t head_dim, const amskv_sch
     pl->v_off[l] = at;
     at = align_up(at + bh * (uint64_t)cap * row);
     if (eight_bits(sc->dtype)) {
-      pl->k_exp[l] = at;
-      at = align_up(at + bh * (uint64_t)cap / AMSKV_KV8_BLOCK);
-      pl->v_exp[l] = at;
-      at = align_up(at + bh * (uint64_t)cap / AMSKV_KV8_BLOCK);
+      pl->k_scale[l] = at;
+      at = align_up(at + bh * (uint64_t)cap / AMSKV_KV8_BLOCK * sizeof(float));
+      pl->v_scale[l] = at;
+      at = align_up(at + bh * (uint64_t)cap / AMSKV_KV8_BLOCK * sizeof(float));
     }
   }
   if (eight_bits(sc->dtype)) {  // neither similarity nor density: no workspaces
@@ -322,8 +322,8 @@ inline RowMap arena_map(const amskv_cache* c, const LayerState& L) {
 }
 
 inline amskv::Codes codes(const amskv_cache* c, const LayerState& L) {
-  auto at = [&](uint64_t off) { return (unsigned char*)c->arena + off; };
-  return {at(L.k_off), at(L.v_off), at(L.k_exp), at(L.v_exp)};
+  char* a = c->arena;
+  return {(unsigned char*)a + L.k_off, (unsigned char*)a + L.v_off, (float*)(a + L.k_scale), (float*)(a + L.v_scale)};
 }
 
 inline bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
@@ -741,8 +741,8 @@ int32_t amskv_cache_create(int32_t layers, int32_t heads, int32_t head_dim,
     L.cap = pl.cap[l];
     L.k_off = pl.k_off[l];
     L.v_off = pl.v_off[l];
-    L.k_exp = pl.k_exp[l];
-    L.v_exp = pl.v_exp[l];
+    L.k_scale = pl.k_scale[l];
+    L.v_scale = pl.v_scale[l];
     for (int i = 0; i < AMSKV_MAX_SCALES; ++i) L.planned_off[i] = pl.slot[l][i];
   }
   if (c->mode == AMSKV_MODE_TOKEN_BUDGET && c->arena) {
@@ -1349,7 +1349,7 @@ int64_t amskv_cache_bytes_held(const amskv_cache* c, int32_t layer, int32_t incl
         tok += g.len;
       }
     }
-  return 2 * (int64_t)c->batch * c->heads * (held * c->head_dim + blocks) +
+  return 2 * (int64_t)c->batch * c->heads * (held * c->head_dim + blocks * (int64_t)sizeof(float)) +
          2 * (int64_t)c->elem_bytes * c->batch * c->heads * c->head_dim * tok;
 }
 
@@ -1390,6 +1390,7 @@ int32_t amskv_cache_set_io_layout(amskv_cache* c, int32_t io_layout, int64_t q_t
     const int64_t width = (int64_t)c->heads * c->head_dim, per16 = 16 / c->elem_bytes;
     for (int64_t st : {q_token_stride, kv_token_stride, o_token_stride})
       if (st < width || st % per16 != 0 || st > ((int64_t)1 << 40)) return AMSKV_ERR_INVALID_ARG;
+    if (eight_bits(c->dtype) && kv_token_stride >= (1 << 23)) return AMSKV_ERR_INVALID_ARG;  // 64 rows of a tile by 32-bit offsets
     c->q_tok = q_token_stride;
     c->kv_tok = kv_token_stride;
     c->o_tok = o_token_stride;

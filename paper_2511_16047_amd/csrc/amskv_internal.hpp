@@ -285,10 +285,11 @@ hipError_t launch_density_total(const float* partial_ws, int batch, int heads, i
 // either never calls them).
 #define AMSKV_WEAK __attribute__((weak))
 
-// A layer's K and V in 8 bits: codes [BH][cap][D], and per 16 tokens a biased exponent (value = code * 2^(byte - 127)),
-// [BH][cap / 16]; cap and every slot are multiples of 16 tokens.
+// A layer's K and V in 8 bits: codes [BH][cap][D], and the power of two that every 16 tokens share, [BH][cap / 16] (as fp32: ready
+// for the instruction that turns codes into numbers); cap and every slot are multiples of 16 tokens.
 struct Codes {
-  unsigned char *k, *v, *k_exp, *v_exp;
+  unsigned char *k, *v;
+  float *k_scale, *v_scale;
 };
 
 // What becomes of a scale's tensors in one launch (take_kernels.hip): Q is turned, K is turned and put in its place, V is put

@@ -22,22 +22,22 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void att
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
   const int base = at.tile * U::kRows + 32 * (wave % kTeamWaves);
   const bool active = base < t_q;
-  const int row = min(base + r, t_q - 1);
 
   rows::bf16x8 qf[U::KS];
-  const char* q_row = q + unit_offset(io.q, bh, io.heads) + row * io.q.tok;
+  const char* q_row = q + unit_offset(io.q, bh, io.heads) + min(base + r, t_q - 1) * io.q.tok;
 #pragma unroll
   for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + 32 * t + 16 * h);
 
   const long long x_unit = unit_offset(io.kv, bh, io.heads), blocks = cap_tokens / AMSKV_KV8_BLOCK;
-  const rows::Keys keys{codes.k + bh * cap_tokens * D, codes.v + bh * cap_tokens * D, codes.k_exp + bh * blocks, codes.v_exp + bh * blocks,
+  const rows::Keys keys{codes.k + bh * cap_tokens * D, codes.v + bh * cap_tokens * D, codes.k_scale + bh * blocks, codes.v_scale + bh * blocks,
                         (const char*)ext.k + x_unit, (const char*)ext.v + x_unit, io.kv.tok, io.kv.tok, seg.ext_start,
                         seg.total - seg.ext_start};
   typename U::Result x;
   U::clear(x);
   U::walk(x, qf, lds, keys, seg, 0, U::tiles(keys), scale_log2e, active);
   U::meet(x, lds);
-  U::put(x, reinterpret_cast<__bf16*>(o + unit_offset(io.o, bh, io.heads) + row * io.o.tok), active && base + r < t_q);
+  const int row = base + (U::fresh(threadIdx.x) & 31);  // (not kept over the walk)
+  U::put(x, reinterpret_cast<__bf16*>(o + unit_offset(io.o, bh, io.heads) + min(row, t_q - 1) * io.o.tok), active && row < t_q);
 }
 
 template <int D, int kTeamWaves, int kTeams, int kMinWavesPerSimd>
@@ -60,7 +60,7 @@ hipError_t launch_attend_codes(const void* q, void* o, const Codes& c, int bh, i
   const int blocks = (seg.total + 31) / 32;
   if (t_q <= 32) {
     if (blocks == 1) return head_dim == 64 ? run(go<64, 1, 1, 3>) : run(go<128, 1, 1, 1>);
-    return head_dim == 64 ? run(go<64, 1, 4, 2>) : run(go<128, 1, 4, 1>);
+    return head_dim == 64 ? run(go<64, 1, 4, 3>) : run(go<128, 1, 4, 1>);
   }
   if (t_q <= 128) return head_dim == 64 ? run(go<64, 4, 1, 4>) : run(go<128, 4, 1, 2>);
   return head_dim == 64 ? run(go<64, 8, 1, 4>) : run(go<128, 8, 1, 2>);

@@ -6,10 +6,10 @@
 // probabilities already lie as the second product's B operand wants them; V is transposed by ds_read_b64_tr_b16.  One pass,
 // with the reference of the exponentials lagging behind the running maximum by up to kMaxLag powers of two.
 //
-// A team of kTeamWaves waves shares tiles of keys (64, or 32 where a wave works alone).  A tile goes from memory to
+// A team of kTeamWaves waves shares tiles of keys (64, or 32 for teams of fewer than eight).  A tile goes from memory to
 // registers one tile ahead, is made bf16 there -- once for all waves that read it, which is why codes do not go to LDS as they
-// are -- and is written to LDS when the tile before it is done: two tiles in LDS and one barrier a tile for a team, one
-// tile and no barrier for a wave by itself.  kTeams teams of a workgroup hold the same rows and take every kTeams-th tile;
+// are -- and is written to LDS: a ring of four tiles and one barrier a tile for a team, one tile and no barrier for a wave by
+// itself.  kTeams teams of a workgroup hold the same rows and take every kTeams-th tile;
 // their results meet in LDS at the end.
 #pragma once
 #include "codes.hpp"
@@ -24,14 +24,16 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 #define AMSKV_ROWS_LDS __attribute__((address_space(3)))
 
-// the reference of the exponentials may lag behind the maximum by this many powers of two: weights stay below 2^kMaxLag
-constexpr float kMaxLag = 6.0f;
+// the reference of the exponentials may lag behind the maximum by this many powers of two; a lane's 16 new weights then sum to
+// at most kTripSum = 16 * 2^kMaxLag, and a larger sum says that the reference has to move
+constexpr float kMaxLag = 6.0f, kTripSum = 1024.0f;
 
 // Keys of a unit: n8 rows of codes, located by the segment table, then nx rows of bf16 at a fixed stride.
 struct Keys {
-  const unsigned char *k8, *v8, *k_exp, *v_exp;
+  const unsigned char *k8, *v8;
+  const float *k_scale, *v_scale;  // of every 16 rows of codes
   const char *kx, *vx;
-  long long k_tok, v_tok;  // bytes
+  long long k_tok, v_tok;  // bytes, below 2^24
   int n8, nx;
 };
 
@@ -53,21 +55,44 @@ __device__ __forceinline__ void settle_mfma(f32x16& acc) { asm volatile("s_nop 1
 
 template <int D, int kTeamWaves, int kTeams, bool kEight>
 struct Unit {
-  static constexpr int RB = 2 * D, KS = D / 16, DB = D / 32, CPR = D / 8, CP8 = D / 16;
-  static constexpr int kTile = kTeamWaves == 1 ? 32 : 64;
-  static constexpr int kStages = kTeamWaves == 1 ? 1 : 2;
+  static constexpr int RB = 2 * D, KS = D / 16, DB = D / 32, CPR = D / 8;
+  static constexpr int kTile = kTeamWaves == 8 ? 64 : 32;
+  static constexpr int kStages = kTeamWaves == 1 ? 1 : 4;
   static constexpr int kThreads = 64 * kTeamWaves;
-  static constexpr int kItems = 2 * kTile * CPR / kThreads;  // 16-byte pieces of K and V a thread brings per tile, as bf16
-  static constexpr int kItems8 = kItems / 2;                 // ... as codes
+  static constexpr int kItems = 2 * kTile * CPR / kThreads;  // pieces of 8 channels of K and V that a thread brings per tile
+  static constexpr int kStep = kThreads / CPR;               // rows from a piece to the next one of the same tensor
   static constexpr int kTensor = kTile * RB, kStage = 2 * kTensor, kTeamLds = kStages * kStage;
   static constexpr int kLds = kTeams * kTeamLds;
   static constexpr int kRows = 32 * kTeamWaves;
+  // K fragments of the next block are asked for while the softmax of this one runs, where there are registers for them
+  static constexpr bool kAhead = D == 128 || !kEight;
   static_assert(kTeams == 1 || kTeamLds >= kTeamWaves * 32 * D * 4, "a wave parks its O^T in its share of the tiles");
 
+  // A thread's pieces of a tile: 8 channels of a row each, as bf16, or as codes -- then x holds 16 bytes of which the piece is
+  // one half, so that either kind is one load from one place in the code (two would meet in copies that wait for the data).
   struct Staged {
     u32x4 x[kItems];
-    float scale[kEight ? kItems8 : 1];
+    float scale[kEight ? kItems : 1];
   };
+  // Where the pieces of the next tile lie: uniform bases, and a row per piece.  Found at the top of a tile, so that the table walk at
+  // a segment's end does not stand between matrix instructions.
+  struct Aim {
+    const char *kb, *vb;
+    const float *ks, *vs;
+    unsigned k_step, v_step;     // bytes from row to row
+    unsigned row[kItems / 2];
+    int end = 0, delta = 0;      // codes: segment of the tile's first row, its end, from virtual row to row
+  };
+  // Kinds of tile a loop meets: kAny is found out (uniformly), kCodes and kRows are known.
+  enum Kind { kAny, kCodes, kRowsOnly };
+  template <Kind kKind>
+  struct Of {
+    static constexpr Kind value = kKind;
+  };
+  template <Kind kKind>
+  __device__ static __forceinline__ bool is_codes(const Keys& k, int it) {
+    return kEight && (kKind == kCodes || (kKind == kAny && it < tiles8(k)));
+  }
 
   // tiles [0, tiles8) are codes, [tiles8, tiles) bf16 rows
   __device__ static __forceinline__ int tiles8(const Keys& k) { return kEight ? (k.n8 + kTile - 1) / kTile : 0; }
@@ -77,68 +102,87 @@ struct Unit {
     return kEight && it < t8 ? min(kTile, k.n8 - it * kTile) : min(kTile, k.nx - (it - t8) * kTile);
   }
 
-  // `member`: thread inside the team
-  __device__ static __forceinline__ void load(Staged& s, const Keys& k, const SegTable& seg, int it, int member) {
-    const int t8 = tiles8(k);
-    if (kEight && it < t8) {
-      const int first = it * kTile;
-      int end = k.n8, delta = 0;  // of the segment that holds `first`
-      for (int g = 0; g < seg.n; ++g)
-        if (first >= seg.virt_start[g]) {
-          end = seg.virt_start[g] + seg.len[g];
-          delta = seg.phys_off[g] - seg.virt_start[g];
-        }
-      const bool whole = min(first + kTile, k.n8) <= end;  // uniform
+  // `member`: thread inside the team.  (Through an empty asm, so that what is derived from it is not kept in registers from
+  // before the loop: this is where the widest forms would spill.)
+  __device__ static __forceinline__ int fresh(int x) {
+    if (D == 64 || kTeamWaves == 1) asm volatile("" : "+v"(x));
+    return x;
+  }
+  template <Kind kKind>
+  __device__ static __forceinline__ void aim(Aim& a, const Keys& k, const SegTable& seg, int it, int member) {
+    const bool codes = is_codes<kKind>(k, it);  // uniform
+    const int first = (codes ? it : it - tiles8(k)) * kTile, last = (codes ? k.n8 : k.nx) - 1;
+    const int row0 = fresh(member) / CPR;
+    if (codes) {
+      if (first >= a.end)  // a handful of times: the segment that holds `first`
+        for (int g = 0; g < seg.n; ++g)
+          if (first >= seg.virt_start[g]) {
+            a.end = seg.virt_start[g] + seg.len[g];
+            a.delta = seg.phys_off[g] - seg.virt_start[g];
+          }
+      a.kb = (const char*)k.k8;
+      a.vb = (const char*)k.v8;
+      a.ks = k.k_scale;
+      a.vs = k.v_scale;
+      a.k_step = a.v_step = D;
 #pragma unroll
-      for (int i = 0; i < kItems8; ++i) {
-        constexpr int kPer = kTile * CP8;
-        const int at = i * kThreads + member;
-        const bool is_v = kItems8 > 1 ? i >= kItems8 / 2 : __builtin_amdgcn_readfirstlane(at) >= kPer;
-        const int idx = at & (kPer - 1), c = idx % CP8, j = min(first + idx / CP8, k.n8 - 1);
-        int row = j + delta;
-        if (!whole)
+      for (int i = 0; i < kItems / 2; ++i) a.row[i] = min(first + row0 + i * kStep, last) + a.delta;
+      if (min(first + kTile - 1, last) >= a.end) {  // rows of several segments
+#pragma unroll
+        for (int i = 0; i < kItems / 2; ++i) {
+          const int j = min(first + row0 + i * kStep, last);
           for (int g = 0; g < seg.n; ++g)
-            if (j >= seg.virt_start[g]) row = j + seg.phys_off[g] - seg.virt_start[g];
-        s.x[i] = *reinterpret_cast<const u32x4*>((is_v ? k.v8 : k.k8) + ((long long)row * D + 16 * c));
-        s.scale[i] = __int_as_float((int)(is_v ? k.v_exp : k.k_exp)[row / AMSKV_KV8_BLOCK] << 23);
+            if (j >= seg.virt_start[g]) a.row[i] = j + seg.phys_off[g] - seg.virt_start[g];
+        }
       }
-      return;
-    }
-    const int first = (it - t8) * kTile;
+    } else {
+      a.kb = k.kx + first * k.k_tok;
+      a.vb = k.vx + first * k.v_tok;
+      a.ks = (const float*)k.kx;
+      a.vs = (const float*)k.vx;
+      a.k_step = (unsigned)k.k_tok;
+      a.v_step = (unsigned)k.v_tok;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const bool is_v = i >= kItems / 2;
-      const int idx = (i % (kItems / 2)) * kThreads + member, c = idx % CPR, j = min(first + idx / CPR, k.nx - 1);
-      s.x[i] = *reinterpret_cast<const u32x4*>((is_v ? k.vx : k.kx) + ((long long)j * (is_v ? k.v_tok : k.k_tok) + 16 * c));
+      for (int i = 0; i < kItems / 2; ++i) a.row[i] = min(row0 + i * kStep, last - first);
     }
+  }
+  // (offsets from the bases stay below 2^31: 64 rows at strides below 2^24 bytes, or a unit's codes)
+  template <Kind kKind>
+  __device__ static __forceinline__ void fetch(Staged& s, const Aim& a, const Keys& k, int it, int member) {
+    const bool codes = is_codes<kKind>(k, it);
+    const int c = fresh(member) % CPR;
+    const unsigned in_row = codes ? 16 * (c >> 1) : 16 * c;
+#pragma unroll
+    for (int i = 0; i < kItems / 2; ++i) {
+      s.x[i] = *reinterpret_cast<const u32x4*>(a.kb + (a.row[i] * a.k_step + in_row));
+      s.x[kItems / 2 + i] = *reinterpret_cast<const u32x4*>(a.vb + (a.row[i] * a.v_step + in_row));
+      if constexpr (kEight && kKind != kRowsOnly) {
+        const unsigned at = codes ? a.row[i] / AMSKV_KV8_BLOCK : 0u;  // (bf16 rows: a word that exists)
+        s.scale[i] = a.ks[at];
+        s.scale[kItems / 2 + i] = a.vs[at];
+      }
+    }
+  }
+  template <Kind kKind>
+  __device__ static __forceinline__ void load(Staged& s, Aim& a, const Keys& k, const SegTable& seg, int it, int member) {
+    aim<kKind>(a, k, seg, it, member);
+    fetch<kKind>(s, a, k, it, member);
   }
 
   // `lds`: byte offset of the tile.  (Offsets of a lane's pieces differ from the first one's by a constant and by the flip of
   // address bits that the swizzle of a constant number of rows makes -- swizzle() moves bits, so the swizzles of bits apart add up.)
+  template <Kind kKind>
   __device__ static __forceinline__ void store(const Staged& s, char* lds_all, int lds, const Keys& k, int it, int member) {
-    if (kEight && it < tiles8(k)) {
-      constexpr int kPer = kTile * CP8, kStep = kThreads / CP8 < kTile ? kThreads / CP8 : kTile;  // rows from a piece to the next
-      const int first = member & (kPer - 1), row = first / CP8;
-      const int at = lds + row * RB + 16 * ((2 * (first % CP8)) ^ swizzle<D>(row));
-#pragma unroll
-      for (int i = 0; i < kItems8; ++i) {
-        const int n = kItems8 > 1 ? i % (kItems8 / 2) : 0;
-        const bool is_v = kItems8 > 1 ? i >= kItems8 / 2 : __builtin_amdgcn_readfirstlane(member) >= kPer;
-        u32x4 w[2];
-        values16(s.x[i], s.scale[i], w);
-        char* to = lds_all + ((at ^ (16 * swizzle<D>(n * kStep))) + (is_v ? kTensor : 0) + n * kStep * RB);
-        char* to2 = lds_all + ((at ^ (16 * swizzle<D>(n * kStep)) ^ 16) + (is_v ? kTensor : 0) + n * kStep * RB);
-        *reinterpret_cast<u32x4*>(to) = w[0];
-        *reinterpret_cast<u32x4*>(to2) = w[1];
-      }
-      return;
-    }
-    constexpr int kStep = kThreads / CPR;
-    const int row = member / CPR, at = lds + row * RB + 16 * ((member % CPR) ^ swizzle<D>(row));
+    member = fresh(member);
+    const int row = member / CPR, c = member % CPR, at = lds + row * RB + 16 * (c ^ swizzle<D>(row));
+    const bool codes = is_codes<kKind>(k, it);
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const int n = i % (kItems / 2);
-      *reinterpret_cast<u32x4*>(lds_all + ((at ^ (16 * swizzle<D>(n * kStep))) + (i >= kItems / 2 ? kTensor : 0) + n * kStep * RB)) = s.x[i];
+      u32x4 w = s.x[i];
+      if (codes)
+        w = values8(u32x2{c & 1 ? w[2] : w[0], c & 1 ? w[3] : w[1]}, s.scale[i]);
+      *reinterpret_cast<u32x4*>(lds_all + ((at ^ (16 * swizzle<D>(n * kStep))) + (i >= kItems / 2 ? kTensor : 0) + n * kStep * RB)) = w;
     }
   }
 
@@ -157,73 +201,158 @@ struct Unit {
     x.sum = 0.f;
   }
 
-  // the keys of a tile in LDS
-  __device__ static __forceinline__ void attend(Result& x, const bf16x8 (&qf)[KS], const char* lds_all, int lds, int n_valid, float c, int lane) {
+  // byte offsets, inside a tile, of a lane's K fragment (step 0) and V fragment (d, u, x = 0) of the tile's first 32 keys
+  __device__ static __forceinline__ int k_lane(int lane) {
     const int r = lane & 31, h = lane >> 5;
-    const int tr_key = 4 * h + ((lane & 15) >> 2), tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-    const int ka = lds + r * RB + 16 * (h ^ swizzle<D>(r));
-    const int va = lds + kTensor + tr_key * RB + 16 * ((tr_col >> 3) ^ swizzle<D>(tr_key)) + 2 * (tr_col & 7);
-#pragma unroll 1
-    for (int b = 0; b < kTile / 32; ++b) {
-      if (b > 0 && 32 * b >= n_valid) break;  // uniform
-      f32x16 s;
+    return r * RB + 16 * (h ^ swizzle<D>(r));
+  }
+  __device__ static __forceinline__ int v_lane(int lane) {
+    const int key = 4 * (lane >> 5) + ((lane & 15) >> 2), col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    return kTensor + key * RB + 16 * ((col >> 3) ^ swizzle<D>(key)) + 2 * (col & 7);
+  }
+
+  // K fragments of 32 keys; `at`: k_lane + the block's offset
+  __device__ static __forceinline__ void load_k(bf16x8 (&kf)[KS], const char* lds_all, int at) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = 0.f;
+    for (int t = 0; t < KS; ++t) kf[t] = *reinterpret_cast<const bf16x8*>(lds_all + (at ^ (32 * t)));
+  }
+  // S^T of these keys
+  __device__ static __forceinline__ f32x16 scores(const bf16x8 (&kf)[KS], const bf16x8 (&qf)[KS]) {
+    f32x16 s;
 #pragma unroll
-      for (int t = 0; t < KS; ++t) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds_all + (ka ^ (32 * t)) + 32 * b * RB);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[t], s, 0, 0, 0);
-      }
-      if (n_valid < 32 * b + 32) {
+    for (int v = 0; v < 16; ++v) s[v] = 0.f;
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (32 * b + 8 * (v >> 2) + 4 * h + (v & 3) >= n_valid) s[v] = -INFINITY;
-      }
-      // the reference moves when a score of the block lies more than kMaxLag powers of two above it (from -inf on the first)
-      settle_mfma(s);
-      float m = max3(s[0], s[1], s[2]);
+    for (int t = 0; t < KS; ++t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t], qf[t], s, 0, 0, 0);
+    return s;
+  }
+  // only the first n_valid keys weigh anything
+  __device__ static __forceinline__ void mask(f32x16& s, int n_valid, int lane) {
+    if (n_valid < 32) {
 #pragma unroll
-      for (int v = 3; v < 15; v += 2) m = max3(m, s[v], s[v + 1]);
-      m = max3(m, s[15], s[15]);
-      asm volatile("s_nop 1" : "+v"(m));  // (a lane swap reads what inline assembly wrote)
-      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(m), __float_as_int(m), false, false);
-      const float full = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1])) * c;  // finite: a tile's first key is valid
-      if (__builtin_amdgcn_ballot_w64(full - x.ref > kMaxLag) != 0) {
-        const float ref = full - x.ref > kMaxLag ? full : x.ref;
-        const float alpha = __builtin_amdgcn_exp2f(x.ref - ref);
-        x.ref = ref;
-        x.sum *= alpha;
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) x.o[d][v] *= alpha;
-      }
-      bf16x8 pf[2];
-      float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-      for (int v = 0; v < 16; v += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[v], c, -x.ref)), p1 = __builtin_amdgcn_exp2f(fmaf(s[v + 1], c, -x.ref));
-        s0 += p0;
-        s1 += p1;
-        // bf16: the matrix cores' type; a weight is off by 2^-8 of itself at most, the sum stays in fp32
-        pf[v >> 3][v & 7] = (__bf16)p0;
-        pf[v >> 3][(v & 7) + 1] = (__bf16)p1;
-      }
-      x.sum += s0 + s1;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const bf16x4 lo = tr16(lds_all + (va ^ (64 * d)) + (32 * b + 16 * u) * RB);
-          const bf16x4 hi = tr16(lds_all + (va ^ (64 * d) ^ (16 * swizzle<D>(8))) + (32 * b + 16 * u + 8) * RB);
-          const bf16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-          x.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[u], x.o[d], 0, 0, 0);
-        }
+      for (int v = 0; v < 16; ++v)
+        if (8 * (v >> 2) + 4 * (lane >> 5) + (v & 3) >= n_valid) s[v] = -INFINITY;
     }
+  }
+  // O^T += V^T P^T, keys 16u .. 16u + 15 of a block; `at`: v_lane + the block's offset
+  __device__ static __forceinline__ void add_values(Result& x, const bf16x8& pf, const char* lds_all, int at, int u) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      const bf16x4 lo = tr16(lds_all + (at ^ (64 * d)) + 16 * u * RB);
+      const bf16x4 hi = tr16(lds_all + (at ^ (64 * d) ^ (16 * swizzle<D>(8))) + (16 * u + 8) * RB);
+      const bf16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      x.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf, x.o[d], 0, 0, 0);
+    }
+  }
+  // weights of keys 16u .. 16u + 15; returns the lane's sum.  bf16 is the matrix cores' type: a weight is off by 2^-8 of itself at
+  // most; the sum is taken in fp32 over the unrounded ones.
+  __device__ static __forceinline__ float weights(const f32x16& s, bf16x8& pf, float c, float ref, int u) {
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int v = 0; v < 8; v += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[8 * u + v], c, -ref)), p1 = __builtin_amdgcn_exp2f(fmaf(s[8 * u + v + 1], c, -ref));
+      s0 += p0;
+      s1 += p1;
+      pf[v] = (__bf16)p0;
+      pf[v + 1] = (__bf16)p1;
+    }
+    return s0 + s1;
+  }
+  // the largest score of each query, over both lane halves, times c (finite: a block's first key is valid)
+  __device__ static __forceinline__ float largest(f32x16& s, float c) {
+    settle_mfma(s);
+    float m = max3(s[0], s[1], s[2]);
+#pragma unroll
+    for (int v = 3; v < 15; v += 2) m = max3(m, s[v], s[v + 1]);
+    m = max3(m, s[15], s[15]);
+    asm volatile("s_nop 1" : "+v"(m));  // (a lane swap reads what inline assembly wrote)
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(m), __float_as_int(m), false, false);
+    return fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1])) * c;
+  }
+  __device__ static __forceinline__ void scale_by(Result& x, float alpha) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x.o[d][v] *= alpha;
+  }
+
+  // A block start to end (a wave by itself: other waves of the SIMD fill its gaps).
+  __device__ static __forceinline__ void whole_step(Result& x, const bf16x8 (&qf)[KS], const char* lds_all, int k_at, int v_at, int n_valid,
+                                                    float c, int lane) {
+    bf16x8 kf[KS];
+    load_k(kf, lds_all, k_at);
+    f32x16 s = scores(kf, qf);
+    mask(s, n_valid, lane);
+    const float full = largest(s, c);
+    if (__builtin_amdgcn_ballot_w64(full - x.ref > kMaxLag) != 0) {
+      const float ref = full - x.ref > kMaxLag ? full : x.ref, alpha = __builtin_amdgcn_exp2f(x.ref - ref);
+      x.ref = ref;
+      x.sum *= alpha;
+      scale_by(x, alpha);
+    }
+    bf16x8 pf[2];
+    x.sum += weights(s, pf[0], c, x.ref, 0) + weights(s, pf[1], c, x.ref, 1);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) add_values(x, pf[u], lds_all, v_at, u);
+  }
+
+  // A block, one behind: its softmax on the vector ALUs runs beside the second product of the block before it, whose weights
+  // wait in pf; the two share no data and stand in one basic block.  Weights are formed against the reference as it is; only
+  // when a lane's sum shows that some score lay far above it is the maximum taken and the block's weights formed again, and O^T
+  // follows the new reference at the top of the next step.
+  struct Behind {
+    bf16x8 pf[2];
+    float alpha;
+    int block;  // byte offset of the block before (uniform)
+    bool rescale, first;
+  };
+  // `between`, behind the score products, replaces kf by the next block's fragments: they arrive beside the softmax.
+  template <bool kFull, class Between>
+  __device__ static __forceinline__ void step(Result& x, Behind& w, bf16x8 (&kf)[KS], const bf16x8 (&qf)[KS], const char* lds_all, int ka, int va,
+                                              int block, int n_valid, float c, int lane, Between between) {
+    if (__builtin_expect(w.rescale, 0)) scale_by(x, w.alpha);
+    if constexpr (!kAhead) load_k(kf, lds_all, block + ka);
+    f32x16 s = scores(kf, qf);
+    between();
+    if constexpr (!kFull) mask(s, n_valid, lane);
+    float sum = 0.f;
+    bool trip = true;
+    const bool first = w.first;
+    if (!first) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        add_values(x, w.pf[u], lds_all, w.block + va, u);
+        sum += weights(s, w.pf[u], c, x.ref, u);
+      }
+      trip = __builtin_amdgcn_ballot_w64(!(sum <= kTripSum)) != 0;
+    }
+    w.rescale = trip && !first;  // (nothing has been added up before the first block)
+    if (__builtin_expect(trip, 0)) {
+      const float full = largest(s, c), ref = full - x.ref > kMaxLag ? full : x.ref;
+      w.alpha = __builtin_amdgcn_exp2f(x.ref - ref);
+      x.ref = ref;
+      x.sum *= w.alpha;
+      sum = weights(s, w.pf[0], c, ref, 0);
+      sum += weights(s, w.pf[1], c, ref, 1);
+    }
+    x.sum += sum;
+    w.first = false;
+    w.block = block;
+  }
+  __device__ static __forceinline__ void finish(Result& x, const Behind& w, const char* lds_all, int va) {
+    if (w.first) return;
+    if (w.rescale) scale_by(x, w.alpha);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) add_values(x, w.pf[u], lds_all, w.block + va, u);
   }
   // within 16 lanes, lane i gives the address of 4 channels of key i/4 and receives 4 keys of channel i
   __device__ static __forceinline__ bf16x4 tr16(const char* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((AMSKV_ROWS_LDS bf16x4*)(p));
+  }
+
+  // The wait for Q's loads, here: left to the compiler it stands in the loop, where it waits for the tile just asked for as well.
+  __device__ static __forceinline__ void settle(const bf16x8 (&qf)[KS]) {
+#pragma unroll
+    for (int t = 0; t < KS; ++t) asm volatile("" ::"v"(qf[t]));
   }
 
   // Tiles [from, to) of the keys.  Every wave of the workgroup calls this; one without rows only brings its part of the tiles.
@@ -232,39 +361,119 @@ struct Unit {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int team = wave / kTeamWaves, member = threadIdx.x - team * kThreads;
     const int lds = team * kTeamLds;
+    const int ka = k_lane(lane), va = v_lane(lane);
     Staged s;
+    Aim to_come;
     int it = from + team;
     if constexpr (kTeamWaves == 1) {
-      if (it < to) load(s, k, seg, it, member);
+      if (it < to) load<kAny>(s, to_come, k, seg, it, member);
+      settle(qf);
       for (; it < to; it += kTeams) {
-        store(s, lds_all, lds, k, it, member);
-        if (it + kTeams < to) load(s, k, seg, it + kTeams, member);
+        store<kAny>(s, lds_all, lds, k, it, member);
+        if (it + kTeams < to) load<kAny>(s, to_come, k, seg, it + kTeams, member);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();  // the rows written above by all lanes are read below
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        attend(x, qf, lds_all, lds, valid(k, it), c, lane);
+        whole_step(x, qf, lds_all, lds + ka, lds + va, valid(k, it), c, lane);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();  // ... and overwritten by the next trip
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
       }
     } else {
+      // A ring of four tiles: the one before, whose last V rows may still be to be multiplied (a tile of one block), the one in
+      // use, the next one, whose first keys are asked for in the last step of this one, and the one that is being written.  One
+      // barrier a tile, behind the score products of its last block.
       const int trips = (to - from + kTeams - 1) / kTeams;  // of every team: the barriers are the workgroup's
-      int stage = 0;
-      if (it < to) {
-        load(s, k, seg, it, member);
-        store(s, lds_all, lds, k, it, member);
-        if (it + kTeams < to) load(s, k, seg, it + kTeams, member);
+      if (it < to) load<kAny>(s, to_come, k, seg, it, member);
+      {
+        Staged s2;
+        if (it + kTeams < to) load<kAny>(s2, to_come, k, seg, it + kTeams, member);
+        if (it < to) store<kAny>(s, lds_all, lds, k, it, member);
+        if (it + kTeams < to) store<kAny>(s2, lds_all, lds + kStage, k, it + kTeams, member);
       }
+      if (it + 2 * kTeams < to) load<kAny>(s, to_come, k, seg, it + 2 * kTeams, member);
+      settle(qf);
       __syncthreads();
-      for (int n = 0; n < trips; ++n, it += kTeams) {
-        if (active && it < to) attend(x, qf, lds_all, lds + stage, valid(k, it), c, lane);
-        stage ^= kStage;
-        if (it + kTeams < to) {
-          store(s, lds_all, lds + stage, k, it + kTeams, member);
-          if (it + 2 * kTeams < to) load(s, k, seg, it + 2 * kTeams, member);
-        }
+      int slot = lds, next = lds + kStage, after = lds + 2 * kStage, spare = lds + 3 * kStage;
+      bf16x8 kf[KS];
+      auto turn_over = [&]() {
         __syncthreads();
+        if (it + 2 * kTeams < to) {
+          store<kAny>(s, lds_all, after, k, it + 2 * kTeams, member);
+          if (it + 3 * kTeams < to) fetch<kAny>(s, to_come, k, it + 3 * kTeams, member);
+        }
+      };
+      auto next_tile = [&]() {
+        const int freed = slot;
+        slot = next;
+        next = after;
+        after = spare;
+        spare = freed;
+        it += kTeams;
+      };
+      int n = 0;
+      if (!active) {  // a wave without rows only brings its part of the tiles
+        for (; it < to; ++n) {
+          if (it + 3 * kTeams < to) aim<kAny>(to_come, k, seg, it + 3 * kTeams, member);
+          turn_over();
+          next_tile();
+        }
+      } else if (it < to) {
+        Behind w;
+        w.rescale = false;
+        w.first = true;
+        w.alpha = 1.f;
+        w.block = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w.pf[u][e] = (__bf16)0.f;
+        if constexpr (kAhead) load_k(kf, lds_all, slot + ka);
+        // Tiles of which everything is known -- they are full, so are the next two, the one to bring exists and all are of one
+        // kind -- have no branch between their instructions; the others are walked with every question asked.  Tiles of two blocks
+        // are written in front of the barrier, beside the score products: the V rows that lay in the slot were multiplied in the
+        // first step of the tile before this one, if that had two blocks.
+        auto known = [&](auto kind, int end) {
+          constexpr Kind kKind = decltype(kind)::value;
+          for (; it + 3 * kTeams < end; ++n) {
+            aim<kKind>(to_come, k, seg, it + 3 * kTeams, member);
+            if constexpr (kTile == 64)
+              step<true>(x, w, kf, qf, lds_all, ka, va, slot, 32, c, lane, [&]() {
+                if constexpr (kAhead) load_k(kf, lds_all, slot + ka + 32 * RB);
+              });
+            step<true>(x, w, kf, qf, lds_all, ka, va, slot + (kTile - 32) * RB, 32, c, lane, [&]() {
+              if constexpr (kTile == 32) __syncthreads();
+              store<kKind>(s, lds_all, after, k, it + 2 * kTeams, member);
+              fetch<kKind>(s, to_come, k, it + 3 * kTeams, member);
+              if constexpr (kTile == 64) __syncthreads();
+              if constexpr (kAhead) load_k(kf, lds_all, next + ka);
+            });
+            next_tile();
+          }
+        };
+        const int t8 = min(tiles8(k), to);
+        if constexpr (kEight) known(Of<kCodes>{}, t8);
+        while (it < to) {
+          if (it - kTeams >= t8 || (it >= t8 && n == 0)) known(Of<kRowsOnly>{}, to);
+          if (it + 3 * kTeams < to) aim<kAny>(to_come, k, seg, it + 3 * kTeams, member);
+          int left = valid(k, it), done = 0;
+          if (kTile == 64 && left > 32) {
+            step<false>(x, w, kf, qf, lds_all, ka, va, slot, 32, c, lane, [&]() {
+                if constexpr (kAhead) load_k(kf, lds_all, slot + ka + 32 * RB);
+              });
+            done = 32;
+          }
+          step<false>(x, w, kf, qf, lds_all, ka, va, slot + done * RB, left - done, c, lane, [&]() {
+            turn_over();
+            if (kAhead && it + kTeams < to) load_k(kf, lds_all, next + ka);
+          });
+          next_tile();
+          ++n;
+        }
+        finish(x, w, lds_all, va);
       }
+      if (kTeams > 1 && n < trips) __syncthreads();
+      if constexpr (kTeams > 1) __syncthreads();  // the ring is parked into next
     }
   }
 

@@ -50,14 +50,18 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   const int tile = a.splits == 1 ? at.tile : at.tile / a.splits, split = at.tile - tile * a.splits;
   long long first;
   const int n = states(a, b, first);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
   const int n_rows = a.group * a.q_tokens, base = tile * U::kRows + 32 * (wave % kTeamWaves);
   const bool active = base < n_rows;
-  const int row = min(base + r, n_rows - 1);
-  const int head = a.group == 1 ? 0 : row / a.q_tokens, token = row - head * a.q_tokens;
+  // byte offset of the lane's row in Q or O (found twice, not kept over the walk)
+  auto row_at = [&](const RowMap& m, int of_lane) {
+    const int row = min(base + (of_lane & 31), n_rows - 1);
+    const int head = a.group == 1 ? 0 : row / a.q_tokens, token = row - head * a.q_tokens;
+    return b * m.batch + ((long long)g * a.group + head) * m.head + token * m.tok;
+  };
 
   rows::bf16x8 qf[U::KS];
-  const char* q_row = a.q + b * a.q_map.batch + ((long long)g * a.group + head) * a.q_map.head + token * a.q_map.tok;
+  const char* q_row = a.q + row_at(a.q_map, lane);
 #pragma unroll
   for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + 32 * t + 16 * h);
 
@@ -72,15 +76,15 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   none.n = 0;
   U::walk(x, qf, lds, keys, none, from, to, a.scale_log2e, active);
   U::meet(x, lds);
+  const int late = U::fresh(threadIdx.x) & 63;
   if (a.splits == 1) {
-    U::put(x, reinterpret_cast<__bf16*>(a.o + b * a.o_map.batch + ((long long)g * a.group + head) * a.o_map.head + token * a.o_map.tok),
-           active && base + r < n_rows);
+    U::put(x, reinterpret_cast<__bf16*>(a.o + row_at(a.o_map, late)), active && base + (late & 31) < n_rows);
     return;
   }
   float* mine = a.workspace + (((long long)at.bh * a.row_tiles + tile) * a.splits + split) * partial_floats(U::kRows, D);
-  const int local = 32 * (wave % kTeamWaves) + r;
+  const int local = 32 * (wave % kTeamWaves) + (late & 31);
   if (active) U::put_partial(x, mine + local * D);
-  if (wave < kTeamWaves && lane < 32) *reinterpret_cast<float2*>(mine + U::kRows * D + 2 * local) = make_float2(x.ref, x.sum);
+  if (wave < kTeamWaves && late < 32) *reinterpret_cast<float2*>(mine + U::kRows * D + 2 * local) = make_float2(x.ref, x.sum);
 }
 
 // A lane has 4 channels of a row.
@@ -180,7 +184,7 @@ hipError_t launch_cross(const CrossCall& c, hipStream_t st) {
   if (a.n_units == 0 || a.group * a.q_tokens == 0) return hipSuccess;
   const Division d = divide(a.n_units, a.group * a.q_tokens, a.kv_tokens);
   a.splits = a.workspace ? d.splits : 1;
-  if (d.team_waves == 1) return c.head_dim == 64 ? go<64, 1, 4, 3>(a, st) : go<128, 1, 4, 1>(a, st);
+  if (d.team_waves == 1) return c.head_dim == 64 ? go<64, 1, 4, 3>(a, st) : go<128, 1, 4, 2>(a, st);
   if (d.team_waves == 4) return c.head_dim == 64 ? go<64, 4, 1, 4>(a, st) : go<128, 4, 1, 2>(a, st);
   return c.head_dim == 64 ? go<64, 8, 1, 4>(a, st) : go<128, 8, 1, 2>(a, st);
 }

@@ -123,6 +123,7 @@ int32_t amskv_cross_attend(const amskv_cross* x, const void* Q_dev, const void* 
   if (!map_of(&x->q, nq, x->head_dim, 2, false, &c.q_map) || !map_of(&x->o, nq, x->head_dim, 2, true, &c.o_map) ||
       !map_of(&x->k, nk, x->head_dim, 2, false, &c.k_map) || !map_of(&x->v, nk, x->head_dim, 2, false, &c.v_map))
     return AMSKV_ERR_INVALID_ARG;
+  if (c.k_map.tok >= (1 << 24) || c.v_map.tok >= (1 << 24)) return AMSKV_ERR_INVALID_ARG;  // 64 rows of a tile by 32-bit offsets
   if (misaligned(Q_dev) || misaligned(K_dev) || misaligned(V_dev) || misaligned(O_dev) || misaligned(workspace_dev)) return AMSKV_ERR_INVALID_ARG;
   if (x->batch == 0 || x->heads == 0 || x->q_tokens == 0) return AMSKV_OK;
   // (K and V may be absent where there can be no states)

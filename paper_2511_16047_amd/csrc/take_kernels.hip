@@ -96,7 +96,7 @@ struct TakeArgs {
   const char* src[3];  // K, V, Q
   char* dst[3];
   RowMap from[3], to[3];
-  unsigned char* exps[2];
+  float* scales[2];
   const float* table;
   long long table_batch, cap_tokens;
   int dst_new, pieces_turned, half, inverse;
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
           *reinterpret_cast<u32x2*>(row + at[i][0]) = codes8(x[i][0], by);
           *reinterpret_cast<u32x2*>(row + at[i][1]) = codes8(x[i][1], by);
         }
-        if ((lane & (4 * rows - 1)) == 0) a.exps[tensor][bh * (a.cap_tokens / AMSKV_KV8_BLOCK) + token / AMSKV_KV8_BLOCK] = (unsigned char)(e + 127);
+        if ((lane & (4 * rows - 1)) == 0) a.scales[tensor][bh * (a.cap_tokens / AMSKV_KV8_BLOCK) + token / AMSKV_KV8_BLOCK] = power_of_two(e);
       }
     } else if (live) {
       T* row = reinterpret_cast<T*>(a.dst[tensor] + b * a.to[tensor].batch + h * a.to[tensor].head + t * a.to[tensor].tok);
@@ -217,8 +217,8 @@ hipError_t take(const Take& t, hipStream_t st) {
   a.dst[0] = t.eight_bits ? (char*)t.codes.k : (char*)t.k_out;
   a.dst[1] = t.eight_bits ? (char*)t.codes.v : (char*)t.v_out;
   a.dst[2] = (char*)t.q_out;
-  a.exps[0] = t.codes.k_exp;
-  a.exps[1] = t.codes.v_exp;
+  a.scales[0] = t.codes.k_scale;
+  a.scales[1] = t.codes.v_scale;
   a.table = t.table;
   a.table_batch = t.table_batch;
   a.cap_tokens = t.cap_tokens;
@@ -268,14 +268,14 @@ struct BlockList {
   int32_t n, total;
   int32_t begin[AMSKV_MAX_SCALES], src[AMSKV_MAX_SCALES], dst[AMSKV_MAX_SCALES];
 };
-// One workgroup owns the codes and exponents of one (b,h) of one tensor and moves them a pass at a time: everything a pass
+// One workgroup owns the codes and scales of one (b,h) of one tensor and moves them a pass at a time: everything a pass
 // reads has arrived before any of it is written, and it is written below where it and all that follows is read.
 template <int D>
 __global__ __launch_bounds__(1024) void move_codes_kernel(Codes c, long long cap_tokens, BlockList list) {
   constexpr int kChunks = 4;  // of 16 bytes a thread and pass; a block of 16 tokens is D of them
   const long long bh = blockIdx.x;
   unsigned char* rows = (blockIdx.y ? c.v : c.k) + bh * cap_tokens * D;
-  unsigned char* exps = (blockIdx.y ? c.v_exp : c.k_exp) + bh * (cap_tokens / AMSKV_KV8_BLOCK);
+  float* scales = (blockIdx.y ? c.v_scale : c.k_scale) + bh * (cap_tokens / AMSKV_KV8_BLOCK);
   auto place = [&](int i, int& src, int& dst) {
     src = dst = 0;
     for (int r = 0; r < list.n; ++r)
@@ -308,14 +308,14 @@ __global__ __launch_bounds__(1024) void move_codes_kernel(Codes c, long long cap
   for (int c0 = 0; c0 < list.total; c0 += (int)blockDim.x) {
     const int i = c0 + (int)threadIdx.x;
     int src = 0, dst = 0;
-    unsigned char e = 0;
+    float x = 0.f;
     if (i < list.total) {
       place(i, src, dst);
-      e = exps[src];
+      x = scales[src];
     }
-    asm volatile("s_waitcnt vmcnt(0)" : "+v"(src) : : "memory");
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(x) : : "memory");
     __syncthreads();
-    if (i < list.total) exps[dst] = e;
+    if (i < list.total) scales[dst] = x;
   }
 }
 
@@ -340,8 +340,9 @@ __global__ __launch_bounds__(256) void export_codes_kernel(Codes c, __bf16* __re
   } else {
     const unsigned char* codes = (blockIdx.y ? c.v : c.k) + (bh * cap_tokens + at) * D + piece * 16;
     const u32x4 x = *reinterpret_cast<const u32x4*>(codes);
-    const float scale = __int_as_float((blockIdx.y ? c.v_exp : c.k_exp)[(bh * cap_tokens + at) / AMSKV_KV8_BLOCK] << 23);
-    values16(x, scale, w);
+    const float scale = (blockIdx.y ? c.v_scale : c.k_scale)[(bh * cap_tokens + at) / AMSKV_KV8_BLOCK];
+    w[0] = values8(u32x2{x[0], x[1]}, scale);
+    w[1] = values8(u32x2{x[2], x[3]}, scale);
   }
   u32x4* to = reinterpret_cast<u32x4*>(out + (bh * seg.total + j) * D + piece * 16);
   to[0] = w[0];

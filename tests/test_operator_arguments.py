@@ -105,7 +105,7 @@ def test_cross_buffers(bad):
 
 def test_cross_strides_and_rows():
     for bad in (dict(q=amskv.Strides(1, 448, 64)), dict(k=amskv.Strides(2112, 64, 100)), dict(o=amskv.Strides(2688, 448, 0)),
-                dict(v=amskv.Strides(2112, -64, 192))):
+                dict(v=amskv.Strides(2112, -64, 192)), dict(k=amskv.Strides(1 << 30, 64, 1 << 23))):
         _refused(INVALID, amskv.amskv_cross_attend, _cross(**bad), A, A, A, A)
     for rows in (-1, 1 << 31):
         _refused(INVALID, amskv.amskv_cross_attend, _cross(kv_rows=rows), A, A, A, A, offsets=A)
@@ -166,7 +166,7 @@ def test_eight_bits_layout(layout, borrow):
                         continue
                     assert off % 16 == 0 and off + _slot(n) <= cap
                     at.append((off, off + _slot(n)))
-                    held += 2 * B * H * (D * n + _slot(n) // 16)
+                    held += 2 * B * H * (D * n + _slot(n) // 16 * 4)
                 assert all(a[1] <= b[0] for a, b in zip(sorted(at), sorted(at)[1:]))      # no two scales share a block
                 assert amskv.amskv_cache_bytes_held(h, layer) == held
     finally:
@@ -174,11 +174,20 @@ def test_eight_bits_layout(layout, borrow):
 
 
 def test_eight_bits_arena():
-    """Codes and exponents of K and V, rounded up to 256 bytes each, and no workspace."""
+    """Codes and scales of K and V, rounded up to 256 bytes each, and no workspace."""
     cap, bh = sum(_slot(s * s) for s in VAR), 6
     up = lambda x: (x + 255) // 256 * 256
     need = amskv.amskv_cache_required_bytes(**_args([(0, 0, True)]))
-    assert need == 2 * up(bh * cap * 64) + 2 * up(bh * cap // 16)
+    assert need == 2 * up(bh * cap * 64) + 2 * up(bh * cap // 16 * 4)
+
+
+def test_eight_bits_strides():
+    h = amskv.amskv_cache_create(**_args([(2, 2, False)]))
+    try:
+        _refused(INVALID, amskv.amskv_cache_set_io_layout, h, amskv.AMSKV_IO_TOKEN_MAJOR, 192, 1 << 23, 192)
+        amskv.amskv_cache_set_io_layout(h, amskv.AMSKV_IO_TOKEN_MAJOR, 1 << 23, (1 << 23) - 8, 1 << 23)
+    finally:
+        amskv.amskv_cache_destroy(h)
 
 
 def test_eight_bits_refuse_the_analysis():
