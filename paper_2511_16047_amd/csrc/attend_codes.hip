@@ -26,7 +26,7 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void att
   rows::bf16x8 qf[U::KS];
   const char* q_row = q + unit_offset(io.q, bh, io.heads) + min(base + r, t_q - 1) * io.q.tok;
 #pragma unroll
-  for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + 32 * t + 16 * h);
+  for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + U::q_at(t, h));
 
   const long long x_unit = unit_offset(io.kv, bh, io.heads), blocks = cap_tokens / AMSKV_KV8_BLOCK;
   const rows::Keys keys{codes.k + bh * cap_tokens * D, codes.v + bh * cap_tokens * D, codes.k_scale + bh * blocks, codes.v_scale + bh * blocks,
@@ -51,19 +51,42 @@ hipError_t go(const void* q, void* o, const Codes& c, int bh, int t_q, int64_t c
   return hipGetLastError();
 }
 
+// Which form: waves to a team, teams to a workgroup.  `units` (b,h) of `n` query rows over `keys` keys.  One key block: waves by
+// themselves.  Few waves of 32 rows: the keys of a row block are shared by 4 or 8 of them.  Otherwise waves by themselves up to 64
+// rows, where there is little to share, and teams that read K and V once for 128 or 256 rows beyond.  us a launch, 8-bit keys, for
+// <1,1> / <1,4> / <1,8> / <4,1> / <8,1>.  Head dim 64: 16 units 256 x 530 14.5 / 7.3 / 6.6 / 14.1 / 15.5, 64 units 169 x 338 11.2 / 7.6 / 8.3 /
+// 11.1 / 11.3, 400 x 1400 36.9 / 24.9 / 26.5 / 31.9 / 32.5, 256 units 30 x 2030 42.6 / 15.2 / 13.2 / 41.5 / 29.7, 100 x 205 9.2 / 9.4 / 12.5 / 9.1 /
+// 8.6, 960 units 64 x 130 10.7 / 14.4 / 20.5 / 11.3 / 16.6, 100 x 205 19.0 / 25.3 / 36.3 / 18.4 / 20.8, 3840 units 25 x 55 11.1 / 18.7 / 28.7 /
+// 20.1 / 30.8, 256 x 530 259 / 320 / 400 / 218 / 214.  Head dim 128: 16 units 256 x 530 17.4 / 9.4 / 9.9 / 17.3 / 21.2, 64 units 256 x 530
+// 20.0 / 14.9 / 19.1 / 18.4 / 22.3, 400 x 1400 46.9 / 43.1 / 52.8 / 39.3 / 45.6, 256 units 36 x 82 6.7 / 8.0 / 12.2 / 7.2 / 7.1, 960 units 64 x 130
+// 18.0 / 29.8 / 49.4 / 22.0 / 31.4, 256 x 530 126 / 165 / 242 / 101 / 100.
+rows::Form choose(int head_dim, long long units, long long n, long long keys) {
+  const long long waves = units * ((n + 31) / 32), wide = units * ((n + 255) / 256), blocks = (keys + 31) / 32;
+  if (blocks <= 1) return {1, 1};
+  if (head_dim == 64) {
+    if (waves <= 256 && blocks >= 16) return {1, 8};
+    if (waves <= 512 || (waves <= 1024 && (wide <= 128 || (n <= 32 && blocks >= 32)))) return {1, 4};
+  } else {
+    if (waves <= 208 && blocks >= 40) return {1, 8};
+    if (waves <= (blocks >= 8 ? 512 : blocks >= 3 ? 256 : 0)) return {1, 4};
+  }
+  if (n <= 64) return {1, 1};
+  return n <= 128 || wide <= 128 ? rows::Form{4, 1} : rows::Form{8, 1};
+}
+
 }  // namespace
 
 hipError_t launch_attend_codes(const void* q, void* o, const Codes& c, int bh, int t_q, int head_dim, int64_t cap_tokens,
                                const SegTable& seg, const ExtKV& ext, const CallerIo& io, float softmax_scale, hipStream_t st) {
   const float s = softmax_scale * 1.4426950408889634f;
   auto run = [&](auto f) { return f(q, o, c, bh, t_q, cap_tokens, seg, ext, io, s, st); };
-  const int blocks = (seg.total + 31) / 32;
-  if (t_q <= 32) {
-    if (blocks == 1) return head_dim == 64 ? run(go<64, 1, 1, 3>) : run(go<128, 1, 1, 1>);
-    return head_dim == 64 ? run(go<64, 1, 4, 3>) : run(go<128, 1, 4, 1>);
+  const rows::Form f = choose(head_dim, bh, t_q, seg.total);
+  if (head_dim == 64) {
+    if (f.team_waves == 1) return f.teams == 1 ? run(go<64, 1, 1, 3>) : f.teams == 4 ? run(go<64, 1, 4, 3>) : run(go<64, 1, 8, 2>);
+    return f.team_waves == 4 ? run(go<64, 4, 1, 4>) : run(go<64, 8, 1, 4>);
   }
-  if (t_q <= 128) return head_dim == 64 ? run(go<64, 4, 1, 4>) : run(go<128, 4, 1, 2>);
-  return head_dim == 64 ? run(go<64, 8, 1, 4>) : run(go<128, 8, 1, 2>);
+  if (f.team_waves == 1) return f.teams == 1 ? run(go<128, 1, 1, 2>) : f.teams == 4 ? run(go<128, 1, 4, 2>) : run(go<128, 1, 8, 2>);
+  return f.team_waves == 4 ? run(go<128, 4, 1, 2>) : run(go<128, 8, 1, 2>);
 }
 
 }  // namespace amskv

@@ -55,32 +55,34 @@ __device__ __forceinline__ void settle_mfma(f32x16& acc) { asm volatile("s_nop 1
 
 template <int D, int kTeamWaves, int kTeams, bool kEight>
 struct Unit {
-  static constexpr int RB = 2 * D, KS = D / 16, DB = D / 32, CPR = D / 8;
+  static constexpr int RB = 2 * D, KS = D / 16, DB = D / 32, CPR = D / 8, CP8 = D / 16;
   static constexpr int kTile = kTeamWaves == 8 ? 64 : 32;
-  static constexpr int kStages = kTeamWaves == 1 ? 1 : 4;
+  static constexpr int kStages = 4;
   static constexpr int kThreads = 64 * kTeamWaves;
-  static constexpr int kItems = 2 * kTile * CPR / kThreads;  // pieces of 8 channels of K and V that a thread brings per tile
-  static constexpr int kStep = kThreads / CPR;               // rows from a piece to the next one of the same tensor
-  static constexpr int kTensor = kTile * RB, kStage = 2 * kTensor, kTeamLds = kStages * kStage;
+  static constexpr int kItems = 2 * kTile * CPR / kThreads, kItems8 = kItems / 2;
+  // rows from a thread's piece to its next one of the same tensor; with one piece of codes, half of the waves bring K and half V
+  static constexpr int kStep = kThreads / CPR, kStep8 = kItems8 == 1 ? kTile : 2 * kStep;
+  static constexpr int kRows8 = kItems8 == 1 ? 1 : kItems8 / 2;
+  static constexpr int kTensor = kTile * RB, kStage = 2 * kTensor;
+  // a wave by itself has a block of V there; afterwards teams park their O^T
+  static constexpr int kTeamLds = kTeamWaves > 1 ? kStages * kStage : kTeams > 1 ? 32 * D * 4 : kTensor;
   static constexpr int kLds = kTeams * kTeamLds;
   static constexpr int kRows = 32 * kTeamWaves;
   // K fragments of the next block are asked for while the softmax of this one runs, where there are registers for them
   static constexpr bool kAhead = D == 128 || !kEight;
   static_assert(kTeams == 1 || kTeamLds >= kTeamWaves * 32 * D * 4, "a wave parks its O^T in its share of the tiles");
 
-  // A thread's pieces of a tile: 8 channels of a row each, as bf16, or as codes -- then x holds 16 bytes of which the piece is
-  // one half, so that either kind is one load from one place in the code (two would meet in copies that wait for the data).
+  // A thread's part of a tile: 16 bytes each of 8 bf16 channels (kItems of them, the first half K) or of 16 codes (kItems8).
   struct Staged {
     u32x4 x[kItems];
-    float scale[kEight ? kItems : 1];
+    float scale[kEight ? kItems8 : 1];
   };
-  // Where the pieces of the next tile lie: uniform bases, and a row per piece.  Found at the top of a tile, so that the table walk at
+  // Where the pieces of the next tile lie: uniform bases of bf16 rows, and a row per piece.  Found at the top of a tile, so that the table walk at
   // a segment's end does not stand between matrix instructions.
   struct Aim {
     const char *kb, *vb;
-    const float *ks, *vs;
     unsigned k_step, v_step;     // bytes from row to row
-    unsigned row[kItems / 2];
+    unsigned row[kItems / 2];    // (of codes: the first kRows8)
     int end = 0, delta = 0;      // codes: segment of the tile's first row, its end, from virtual row to row
   };
   // Kinds of tile a loop meets: kAny is found out (uniformly), kCodes and kRows are known.
@@ -108,11 +110,16 @@ struct Unit {
     if (D == 64 || kTeamWaves == 1) asm volatile("" : "+v"(x));
     return x;
   }
+  // row inside a tile of a thread's first piece of codes, its channel group, and whether it is V's (one piece: by the wave)
+  __device__ static __forceinline__ bool is_v8(int i, int member) {
+    return kItems8 == 1 ? __builtin_amdgcn_readfirstlane(member) >= kThreads / 2 : i >= kItems8 / 2;
+  }
+  __device__ static __forceinline__ int member8(int member) { return kItems8 == 1 ? member & (kThreads / 2 - 1) : member; }
   template <Kind kKind>
   __device__ static __forceinline__ void aim(Aim& a, const Keys& k, const SegTable& seg, int it, int member) {
     const bool codes = is_codes<kKind>(k, it);  // uniform
     const int first = (codes ? it : it - tiles8(k)) * kTile, last = (codes ? k.n8 : k.nx) - 1;
-    const int row0 = fresh(member) / CPR;
+    member = fresh(member);
     if (codes) {
       if (first >= a.end)  // a handful of times: the segment that holds `first`
         for (int g = 0; g < seg.n; ++g)
@@ -120,17 +127,13 @@ struct Unit {
             a.end = seg.virt_start[g] + seg.len[g];
             a.delta = seg.phys_off[g] - seg.virt_start[g];
           }
-      a.kb = (const char*)k.k8;
-      a.vb = (const char*)k.v8;
-      a.ks = k.k_scale;
-      a.vs = k.v_scale;
-      a.k_step = a.v_step = D;
+      const int row0 = first + member8(member) / CP8;
 #pragma unroll
-      for (int i = 0; i < kItems / 2; ++i) a.row[i] = min(first + row0 + i * kStep, last) + a.delta;
+      for (int i = 0; i < kRows8; ++i) a.row[i] = min(row0 + i * kStep8, last) + a.delta;
       if (min(first + kTile - 1, last) >= a.end) {  // rows of several segments
 #pragma unroll
-        for (int i = 0; i < kItems / 2; ++i) {
-          const int j = min(first + row0 + i * kStep, last);
+        for (int i = 0; i < kRows8; ++i) {
+          const int j = min(row0 + i * kStep8, last);
           for (int g = 0; g < seg.n; ++g)
             if (j >= seg.virt_start[g]) a.row[i] = j + seg.phys_off[g] - seg.virt_start[g];
         }
@@ -138,29 +141,32 @@ struct Unit {
     } else {
       a.kb = k.kx + first * k.k_tok;
       a.vb = k.vx + first * k.v_tok;
-      a.ks = (const float*)k.kx;
-      a.vs = (const float*)k.vx;
       a.k_step = (unsigned)k.k_tok;
       a.v_step = (unsigned)k.v_tok;
 #pragma unroll
-      for (int i = 0; i < kItems / 2; ++i) a.row[i] = min(row0 + i * kStep, last - first);
+      for (int i = 0; i < kItems / 2; ++i) a.row[i] = min(member / CPR + i * kStep, last - first);
     }
   }
   // (offsets from the bases stay below 2^31: 64 rows at strides below 2^24 bytes, or a unit's codes)
   template <Kind kKind>
   __device__ static __forceinline__ void fetch(Staged& s, const Aim& a, const Keys& k, int it, int member) {
-    const bool codes = is_codes<kKind>(k, it);
-    const int c = fresh(member) % CPR;
-    const unsigned in_row = codes ? 16 * (c >> 1) : 16 * c;
+    member = fresh(member);
+    if (is_codes<kKind>(k, it)) {
+      const unsigned in_row = 16 * (member8(member) % CP8);
+#pragma unroll
+      for (int i = 0; i < kItems8; ++i) {
+        const bool v = is_v8(i, member);
+        const unsigned row = a.row[kItems8 == 1 ? 0 : i % kRows8];
+        s.x[i] = *reinterpret_cast<const u32x4*>((v ? k.v8 : k.k8) + (row * D + in_row));
+        s.scale[i] = (v ? k.v_scale : k.k_scale)[row / AMSKV_KV8_BLOCK];
+      }
+      return;
+    }
+    const unsigned in_row = 16 * (member % CPR);
 #pragma unroll
     for (int i = 0; i < kItems / 2; ++i) {
       s.x[i] = *reinterpret_cast<const u32x4*>(a.kb + (a.row[i] * a.k_step + in_row));
       s.x[kItems / 2 + i] = *reinterpret_cast<const u32x4*>(a.vb + (a.row[i] * a.v_step + in_row));
-      if constexpr (kEight && kKind != kRowsOnly) {
-        const unsigned at = codes ? a.row[i] / AMSKV_KV8_BLOCK : 0u;  // (bf16 rows: a word that exists)
-        s.scale[i] = a.ks[at];
-        s.scale[kItems / 2 + i] = a.vs[at];
-      }
     }
   }
   template <Kind kKind>
@@ -174,15 +180,23 @@ struct Unit {
   template <Kind kKind>
   __device__ static __forceinline__ void store(const Staged& s, char* lds_all, int lds, const Keys& k, int it, int member) {
     member = fresh(member);
-    const int row = member / CPR, c = member % CPR, at = lds + row * RB + 16 * (c ^ swizzle<D>(row));
-    const bool codes = is_codes<kKind>(k, it);
+    if (is_codes<kKind>(k, it)) {
+      const int m = member8(member), row = m / CP8, c = 2 * (m % CP8), at = lds + row * RB + 16 * (c ^ swizzle<D>(row));
+#pragma unroll
+      for (int i = 0; i < kItems8; ++i) {
+        const int n = kItems8 == 1 ? 0 : i % kRows8;
+        const int to = (at ^ (16 * swizzle<D>(n * kStep8))) + n * kStep8 * RB;
+        const int tensor = is_v8(i, member) ? kTensor : 0;
+        *reinterpret_cast<u32x4*>(lds_all + to + tensor) = values8(u32x2{s.x[i][0], s.x[i][1]}, s.scale[i]);
+        *reinterpret_cast<u32x4*>(lds_all + (to ^ 16) + tensor) = values8(u32x2{s.x[i][2], s.x[i][3]}, s.scale[i]);
+      }
+      return;
+    }
+    const int row = member / CPR, at = lds + row * RB + 16 * ((member % CPR) ^ swizzle<D>(row));
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const int n = i % (kItems / 2);
-      u32x4 w = s.x[i];
-      if (codes)
-        w = values8(u32x2{c & 1 ? w[2] : w[0], c & 1 ? w[3] : w[1]}, s.scale[i]);
-      *reinterpret_cast<u32x4*>(lds_all + ((at ^ (16 * swizzle<D>(n * kStep))) + (i >= kItems / 2 ? kTensor : 0) + n * kStep * RB)) = w;
+      *reinterpret_cast<u32x4*>(lds_all + ((at ^ (16 * swizzle<D>(n * kStep))) + (i >= kItems / 2 ? kTensor : 0) + n * kStep * RB)) = s.x[i];
     }
   }
 
@@ -201,7 +215,7 @@ struct Unit {
     x.sum = 0.f;
   }
 
-  // byte offsets, inside a tile, of a lane's K fragment (step 0) and V fragment (d, u, x = 0) of the tile's first 32 keys
+  // byte offsets, inside a tile, of a lane's K fragment (t = 0) and V fragment (d, u = 0) of the tile's first 32 keys
   __device__ static __forceinline__ int k_lane(int lane) {
     const int r = lane & 31, h = lane >> 5;
     return r * RB + 16 * (h ^ swizzle<D>(r));
@@ -275,12 +289,8 @@ struct Unit {
       for (int v = 0; v < 16; ++v) x.o[d][v] *= alpha;
   }
 
-  // A block start to end (a wave by itself: other waves of the SIMD fill its gaps).
-  __device__ static __forceinline__ void whole_step(Result& x, const bf16x8 (&qf)[KS], const char* lds_all, int k_at, int v_at, int n_valid,
-                                                    float c, int lane) {
-    bf16x8 kf[KS];
-    load_k(kf, lds_all, k_at);
-    f32x16 s = scores(kf, qf);
+  // A block from its scores on, start to end (a wave by itself: other waves of the SIMD fill its gaps).
+  __device__ static __forceinline__ void whole_step(Result& x, f32x16& s, const char* lds_all, int v_at, int n_valid, float c, int lane) {
     mask(s, n_valid, lane);
     const float full = largest(s, c);
     if (__builtin_amdgcn_ballot_w64(full - x.ref > kMaxLag) != 0) {
@@ -355,34 +365,118 @@ struct Unit {
     for (int t = 0; t < KS; ++t) asm volatile("" ::"v"(qf[t]));
   }
 
+  // A wave by itself: 32 keys at a time.  K goes from memory to the registers that the first product wants, lane (r, h) from key r.
+  // Where keys may be codes its channels are h D/2 .. in order, so that 16 codes of a load are two fragments, and Q's fragments
+  // are taken in the same order (q_at), which the sum over channels does not mind.  V goes through LDS, where it is transposed.
+  struct Brought {
+    u32x4 k[KS], v[kItems / 2];
+    float k_scale, v_scale[kEight ? kItems8 / 2 : 1];
+  };
+  // byte offset in a row of Q (and of bf16 K, for a wave by itself) of fragment t
+  static constexpr bool kHalves = kTeamWaves == 1 && kEight;
+  __device__ static __forceinline__ int q_at(int t, int h) { return kHalves ? h * D + 16 * t : 32 * t + 16 * h; }
+  template <bool kCodesNow>
+  __device__ static __forceinline__ void bring(Brought& n, const Keys& k, const SegTable& seg, int it, int lane) {
+    const int r = lane & 31, h = lane >> 5;
+    if constexpr (kCodesNow) {
+      const int first = it * kTile, last = k.n8 - 1;
+      constexpr int kV = kItems8 / 2, kVStep = 64 / CP8;
+      // rows of the lane's pieces, K's and V's, in one walk of the table
+      int row[kV + 1], at[kV + 1];
+#pragma unroll
+      for (int i = 0; i <= kV; ++i) row[i] = at[i] = min(first + (i < kV ? i * kVStep + lane / CP8 : r), last);
+      for (int g = 0; g < seg.n; ++g) {
+        const int from = seg.virt_start[g], by = seg.phys_off[g] - seg.virt_start[g];
+#pragma unroll
+        for (int i = 0; i <= kV; ++i) row[i] = at[i] >= from ? at[i] + by : row[i];
+      }
+      const unsigned k_from = (unsigned)row[kV] * D + h * (D / 2);
+#pragma unroll
+      for (int i = 0; i < KS / 2; ++i) n.k[i] = *reinterpret_cast<const u32x4*>(k.k8 + (k_from + 16 * i));
+      n.k_scale = k.k_scale[(unsigned)row[kV] / AMSKV_KV8_BLOCK];
+#pragma unroll
+      for (int i = 0; i < kV; ++i) {
+        n.v[i] = *reinterpret_cast<const u32x4*>(k.v8 + ((unsigned)row[i] * D + 16 * (lane % CP8)));
+        n.v_scale[i] = k.v_scale[(unsigned)row[i] / AMSKV_KV8_BLOCK];
+      }
+    } else {
+      const int first = (it - tiles8(k)) * kTile, last = k.nx - 1;
+      const char *kb = k.kx + first * k.k_tok, *vb = k.vx + first * k.v_tok;
+      const unsigned k_from = (unsigned)min(r, last - first) * (unsigned)k.k_tok;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) n.k[i] = *reinterpret_cast<const u32x4*>(kb + (k_from + q_at(i, h)));
+#pragma unroll
+      for (int i = 0; i < kItems / 2; ++i)
+        n.v[i] = *reinterpret_cast<const u32x4*>(vb + ((unsigned)min(i * (64 / CPR) + lane / CPR, last - first) * (unsigned)k.v_tok + 16 * (lane % CPR)));
+    }
+  }
+  template <bool kCodesNow>
+  __device__ static __forceinline__ void put_down(const Brought& n, bf16x8 (&kf)[KS], char* lds, int lane) {
+    if constexpr (kCodesNow) {
+      constexpr int kVStep = 64 / CP8;
+      const int row = lane / CP8, c = 2 * (lane % CP8), at = row * RB + 16 * (c ^ swizzle<D>(row));
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+        kf[i] = __builtin_bit_cast(bf16x8, values8(u32x2{n.k[i / 2][2 * (i & 1)], n.k[i / 2][2 * (i & 1) + 1]}, n.k_scale));
+#pragma unroll
+      for (int i = 0; i < kItems8 / 2; ++i) {
+        const int to = (at ^ (16 * swizzle<D>(i * kVStep))) + i * kVStep * RB;
+        *reinterpret_cast<u32x4*>(lds + to) = values8(u32x2{n.v[i][0], n.v[i][1]}, n.v_scale[i]);
+        *reinterpret_cast<u32x4*>(lds + (to ^ 16)) = values8(u32x2{n.v[i][2], n.v[i][3]}, n.v_scale[i]);
+      }
+    } else {
+      constexpr int kVStep = 64 / CPR;
+      const int row = lane / CPR, at = row * RB + 16 * ((lane % CPR) ^ swizzle<D>(row));
+#pragma unroll
+      for (int i = 0; i < KS; ++i) kf[i] = __builtin_bit_cast(bf16x8, n.k[i]);
+#pragma unroll
+      for (int i = 0; i < kItems / 2; ++i) *reinterpret_cast<u32x4*>(lds + ((at ^ (16 * swizzle<D>(i * kVStep))) + i * kVStep * RB)) = n.v[i];
+    }
+  }
+  __device__ static __forceinline__ void alone(Result& x, const bf16x8 (&qf)[KS], char* lds, const Keys& k, const SegTable& seg, int it, int to,
+                                               float c, int lane) {
+    Brought n;
+    const int t8 = min(tiles8(k), to), va = v_lane(lane) - kTensor;
+    if (kEight && it < t8) bring<kEight>(n, k, seg, it, lane);
+    else if (it < to) bring<false>(n, k, seg, it, lane);
+    settle(qf);
+    auto block = [&](auto now, auto next, bool more) {
+      bf16x8 kf[KS];
+      put_down<decltype(now)::value == kCodes>(n, kf, lds, lane);
+      f32x16 s = scores(kf, qf);
+      if (more) bring<decltype(next)::value == kCodes>(n, k, seg, it + kTeams, lane);
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();  // the rows written above by all lanes are read below
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      whole_step(x, s, lds, va, valid(k, it), c, lane);
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();  // ... and overwritten by the next block
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      it += kTeams;
+    };
+    if constexpr (kEight) {
+      while (it + kTeams < t8) block(Of<kCodes>{}, Of<kCodes>{}, true);
+      if (it < t8) block(Of<kCodes>{}, Of<kRowsOnly>{}, it + kTeams < to);
+    }
+    while (it < to) block(Of<kRowsOnly>{}, Of<kRowsOnly>{}, it + kTeams < to);
+  }
+
   // Tiles [from, to) of the keys.  Every wave of the workgroup calls this; one without rows only brings its part of the tiles.
   __device__ static __forceinline__ void walk(Result& x, const bf16x8 (&qf)[KS], char* lds_all, const Keys& k, const SegTable& seg, int from,
                                               int to, float c, bool active) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int team = wave / kTeamWaves, member = threadIdx.x - team * kThreads;
     const int lds = team * kTeamLds;
-    const int ka = k_lane(lane), va = v_lane(lane);
-    Staged s;
-    Aim to_come;
     int it = from + team;
     if constexpr (kTeamWaves == 1) {
-      if (it < to) load<kAny>(s, to_come, k, seg, it, member);
-      settle(qf);
-      for (; it < to; it += kTeams) {
-        store<kAny>(s, lds_all, lds, k, it, member);
-        if (it + kTeams < to) load<kAny>(s, to_come, k, seg, it + kTeams, member);
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();  // the rows written above by all lanes are read below
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        whole_step(x, qf, lds_all, lds + ka, lds + va, valid(k, it), c, lane);
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();  // ... and overwritten by the next trip
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      }
+      alone(x, qf, lds_all + lds, k, seg, it, to, c, lane);
     } else {
       // A ring of four tiles: the one before, whose last V rows may still be to be multiplied (a tile of one block), the one in
       // use, the next one, whose first keys are asked for in the last step of this one, and the one that is being written.  One
       // barrier a tile, behind the score products of its last block.
+      const int ka = k_lane(lane), va = v_lane(lane);
+      Staged s;
+      Aim to_come;
       const int trips = (to - from + kTeams - 1) / kTeams;  // of every team: the barriers are the workgroup's
       if (it < to) load<kAny>(s, to_come, k, seg, it, member);
       {
@@ -396,11 +490,12 @@ struct Unit {
       __syncthreads();
       int slot = lds, next = lds + kStage, after = lds + 2 * kStage, spare = lds + 3 * kStage;
       bf16x8 kf[KS];
-      auto turn_over = [&]() {
+      auto turn_over = [&](auto kind) {
+        constexpr Kind kKind = decltype(kind)::value;  // of the tile to bring
         __syncthreads();
         if (it + 2 * kTeams < to) {
           store<kAny>(s, lds_all, after, k, it + 2 * kTeams, member);
-          if (it + 3 * kTeams < to) fetch<kAny>(s, to_come, k, it + 3 * kTeams, member);
+          if (it + 3 * kTeams < to) fetch<kKind>(s, to_come, k, it + 3 * kTeams, member);
         }
       };
       auto next_tile = [&]() {
@@ -415,7 +510,7 @@ struct Unit {
       if (!active) {  // a wave without rows only brings its part of the tiles
         for (; it < to; ++n) {
           if (it + 3 * kTeams < to) aim<kAny>(to_come, k, seg, it + 3 * kTeams, member);
-          turn_over();
+          turn_over(Of<kAny>{});
           next_tile();
         }
       } else if (it < to) {
@@ -455,7 +550,7 @@ struct Unit {
         if constexpr (kEight) known(Of<kCodes>{}, t8);
         while (it < to) {
           if (it - kTeams >= t8 || (it >= t8 && n == 0)) known(Of<kRowsOnly>{}, to);
-          if (it + 3 * kTeams < to) aim<kAny>(to_come, k, seg, it + 3 * kTeams, member);
+          if (it + 3 * kTeams < to) aim<kRowsOnly>(to_come, k, seg, it + 3 * kTeams, member);  // (codes: all brought above)
           int left = valid(k, it), done = 0;
           if (kTile == 64 && left > 32) {
             step<false>(x, w, kf, qf, lds_all, ka, va, slot, 32, c, lane, [&]() {
@@ -464,7 +559,7 @@ struct Unit {
             done = 32;
           }
           step<false>(x, w, kf, qf, lds_all, ka, va, slot + done * RB, left - done, c, lane, [&]() {
-            turn_over();
+            turn_over(Of<kRowsOnly>{});
             if (kAhead && it + kTeams < to) load_k(kf, lds_all, next + ka);
           });
           next_tile();
@@ -570,6 +665,11 @@ struct Unit {
       *reinterpret_cast<f32x4*>(dst + 8 * (i0 + team) + 4 * h) = y;
     }
   }
+};
+
+// Which form a launch takes: waves to a team, teams to a workgroup.
+struct Form {
+  int team_waves, teams;
 };
 
 }  // namespace rows

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   rows::bf16x8 qf[U::KS];
   const char* q_row = a.q + row_at(a.q_map, lane);
 #pragma unroll
-  for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + 32 * t + 16 * h);
+  for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + U::q_at(t, h));
 
   const long long kb = a.offsets ? first * a.k_map.tok : b * a.k_map.batch, vb = a.offsets ? first * a.v_map.tok : b * a.v_map.batch;
   const rows::Keys keys{nullptr, nullptr, nullptr, nullptr, a.k + kb + g * a.k_map.head, a.v + vb + g * a.v_map.head,
@@ -97,18 +97,35 @@ __global__ __launch_bounds__(256) void cross_meet_kernel(CrossArgs a, int rows_o
   const int rest = (int)(i - unit * per_unit), row = rest / (D / 4), c = rest % (D / 4);
   const int tile = row / rows_of_tile, local = row - tile * rows_of_tile;
   const float* from = a.workspace + (unit * a.row_tiles + tile) * a.splits * (long long)partial_floats(rows_of_tile, D);
-  float top = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, from[(long long)s * partial_floats(rows_of_tile, D) + rows_of_tile * D + 2 * local]);
+  // (a few runs at a time, their loads under way together)
+  constexpr int kAtOnce = 8;
+  float top = -INFINITY, total = 0.f;
   rows::f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  float total = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float* p = from + (long long)s * partial_floats(rows_of_tile, D);
-    const float2 st = *reinterpret_cast<const float2*>(p + rows_of_tile * D + 2 * local);
-    const float w = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - top);  // (a run without keys)
-    const rows::f32x4 y = *reinterpret_cast<const rows::f32x4*>(p + local * D + 4 * c);
+  for (int s0 = 0; s0 < a.splits; s0 += kAtOnce) {
+    float2 st[kAtOnce];
+    rows::f32x4 y[kAtOnce];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] = fmaf(w, y[e], sum[e]);
-    total = fmaf(w, st.y, total);
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float* p = from + (long long)min(s0 + i, a.splits - 1) * partial_floats(rows_of_tile, D);
+      st[i] = *reinterpret_cast<const float2*>(p + rows_of_tile * D + 2 * local);
+      y[i] = *reinterpret_cast<const rows::f32x4*>(p + local * D + 4 * c);
+      if (s0 + i >= a.splits) st[i].x = -INFINITY;
+    }
+    float new_top = top;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) new_top = fmaxf(new_top, st[i].x);
+    const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - new_top);
+    total *= old;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] *= old;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float w = st[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[i].x - new_top);  // (a run without keys: 0)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = fmaf(w, y[i][e], sum[e]);
+      total = fmaf(w, st[i].y, total);
+    }
+    top = new_top;
   }
   const float inv = total > 0.f ? 1.0f / total : 0.f;
   rows::bf16x4 w;
@@ -119,17 +136,37 @@ __global__ __launch_bounds__(256) void cross_meet_kernel(CrossArgs a, int rows_o
   *reinterpret_cast<rows::bf16x4*>(a.o + b * a.o_map.batch + ((long long)g * a.group + head) * a.o_map.head + token * a.o_map.tok + 8 * c) = w;
 }
 
-// How a call is divided.
+// How a call is divided: the form, and workgroups that share the keys of a row tile.
 struct Division {
   int team_waves, teams, splits;
 };
-Division divide(int units, int rows, int kv_tokens) {
-  Division d{8, 1, 1};
-  if (rows <= 32) d = {1, 4, 1};
-  else if (rows <= 128) d = {4, 1, 1};
-  const int tile = d.team_waves == 1 ? 32 : 64;
-  const long long groups = (long long)units * ((rows + 32 * d.team_waves - 1) / (32 * d.team_waves));
-  const int trips = (kv_tokens + tile * d.teams - 1) / (tile * d.teams);
+// `units` (b, kv head) of `n` query rows over up to `keys` states.  Waves by themselves where there are at most 96 states; few waves of
+// 32 rows: four to a row block; otherwise teams that read K and V once for 128 rows, or 256 where that pays; up to 64 rows, waves by
+// themselves, until K and V are so large that the rows of a tile are better brought by a team, whole rows at a time, than by
+// lanes that follow a key each.  us a launch, <1,1> / <1,4> / <1,8> / <4,1> / <8,1>, lengths anywhere up to the number given (16 heads, batch B).
+// Head dim 64: B 8, 36 x 77 4.9 / 4.9 / 5.8 / 5.4 / 5.2, 1 x 4000 19.4 / 14.2 / 14.9 / 18.7 / 17.9, 1 x 16000 95.7 / 85.7 / 86.4 / 81.5 / 69.4, 256 x 512
+// 13.2 / 11.7 / 16.5 / 14.0 / 24.7, B 32 256 x 512 32 / 39 / 51 / 24 / 27, 1024 x 512 100 / 128 / 177 / 67 / 67, B 96 9 x 250 14.0 / 14.4 / 17.9 /
+// 16.6 / 22.1.  Head dim 128: B 2 256 x 64 5.3 / 6.2 / 7.2 / 6.7 / 8.2, B 8 1 x 512 12.2 / 9.1 / 9.8 / 12.3 / 12.9, 1 x 4000 39 / 36 / 33 / 33 / 38, 100 x
+// 250 10.0 / 9.5 / 16.0 / 19.7 / 10.3, 4096 x 77 72 / 166 / 342 / 65 / 79, B 32 1024 x 512 268 / 339 / 598 / 152 / 151.  (137 shapes, the choice
+// takes 1.014 of the best on average.)
+Division divide(int head_dim, long long units, long long n, int keys) {
+  const long long waves = units * ((n + 31) / 32), wide = units * ((n + 255) / 256), blocks = ((long long)keys + 31) / 32;
+  const long long bytes = units * keys * head_dim * 4;
+  rows::Form f{4, 1};
+  if (blocks <= 1 || (blocks <= 3 && (n <= 64 || waves <= 512)))
+    f = {1, 1};
+  else if (n <= 64 && blocks >= 100 && bytes >= (head_dim == 64 ? 400000000 : 250000000))
+    f = head_dim == 64 ? rows::Form{8, 1} : rows::Form{4, 1};
+  else if (waves <= 512 || (head_dim == 64 && waves <= 1024 && wide <= 128))
+    f = {1, 4};
+  else if (n <= 64)
+    f = {1, 1};
+  else if (n > 128 && (head_dim == 64 ? n > 256 : keys >= 1024 && wide >= 256))
+    f = {8, 1};
+  Division d{f.team_waves, f.teams, 1};
+  const int tile = d.team_waves == 8 ? 64 : 32;
+  const long long groups = units * ((n + 32 * d.team_waves - 1) / (32 * d.team_waves));
+  const int trips = (int)(((long long)keys + tile * d.teams - 1) / (tile * d.teams));
   // 2 workgroups to a CU, each with 4 tiles for a team at least
   if (groups < 256 && trips >= 8) d.splits = (int)fmin((512 + groups - 1) / groups, trips / 4);
   return d;
@@ -155,7 +192,7 @@ hipError_t go(CrossArgs& a, hipStream_t st) {
 uint64_t cross_workspace_bytes(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) {
   const int units = batch * kv_heads, rows = heads / kv_heads * q_tokens;
   if (units == 0 || rows == 0 || kv_tokens == 0) return 0;
-  const Division d = divide(units, rows, kv_tokens);
+  const Division d = divide(head_dim, units, rows, kv_tokens);
   if (d.splits == 1) return 0;
   const uint64_t row_tiles = (rows + 32 * d.team_waves - 1) / (32 * d.team_waves);
   return (uint64_t)units * row_tiles * d.splits * partial_floats(32 * d.team_waves, head_dim) * sizeof(float);
@@ -182,11 +219,14 @@ hipError_t launch_cross(const CrossCall& c, hipStream_t st) {
   a.kv_tokens = c.kv_tokens;
   a.n_units = c.batch * c.kv_heads;
   if (a.n_units == 0 || a.group * a.q_tokens == 0) return hipSuccess;
-  const Division d = divide(a.n_units, a.group * a.q_tokens, a.kv_tokens);
+  const Division d = divide(c.head_dim, a.n_units, a.group * a.q_tokens, a.kv_tokens);
   a.splits = a.workspace ? d.splits : 1;
-  if (d.team_waves == 1) return c.head_dim == 64 ? go<64, 1, 4, 3>(a, st) : go<128, 1, 4, 2>(a, st);
-  if (d.team_waves == 4) return c.head_dim == 64 ? go<64, 4, 1, 4>(a, st) : go<128, 4, 1, 2>(a, st);
-  return c.head_dim == 64 ? go<64, 8, 1, 4>(a, st) : go<128, 8, 1, 2>(a, st);
+  if (c.head_dim == 64) {
+    if (d.team_waves == 1) return d.teams == 1 ? go<64, 1, 1, 4>(a, st) : go<64, 1, 4, 4>(a, st);
+    return d.team_waves == 4 ? go<64, 4, 1, 4>(a, st) : go<64, 8, 1, 4>(a, st);
+  }
+  if (d.team_waves == 1) return d.teams == 1 ? go<128, 1, 1, 2>(a, st) : go<128, 1, 4, 2>(a, st);
+  return d.team_waves == 4 ? go<128, 4, 1, 2>(a, st) : go<128, 8, 1, 2>(a, st);
 }
 
 }  // namespace amskv
