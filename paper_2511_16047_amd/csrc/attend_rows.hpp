@@ -20,6 +20,7 @@ namespace rows {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 #define AMSKV_ROWS_LDS __attribute__((address_space(3)))
@@ -258,18 +259,20 @@ struct Unit {
     }
   }
   // weights of keys 16u .. 16u + 15; returns the lane's sum.  bf16 is the matrix cores' type: a weight is off by 2^-8 of itself at
-  // most; the sum is taken in fp32 over the unrounded ones.
+  // most.  The sum, in fp32, is over the weights as the second product multiplies them: two to an instruction, and the roundings
+  // of numerator and denominator cancel in part.
   __device__ static __forceinline__ float weights(const f32x16& s, bf16x8& pf, float c, float ref, int u) {
-    float s0 = 0.f, s1 = 0.f;
+    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+    float sum = 0.f;
 #pragma unroll
     for (int v = 0; v < 8; v += 2) {
       const float p0 = __builtin_amdgcn_exp2f(fmaf(s[8 * u + v], c, -ref)), p1 = __builtin_amdgcn_exp2f(fmaf(s[8 * u + v + 1], c, -ref));
-      s0 += p0;
-      s1 += p1;
-      pf[v] = (__bf16)p0;
-      pf[v + 1] = (__bf16)p1;
+      const bf16x2 pk = {(__bf16)p0, (__bf16)p1};
+      sum = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, sum, false);
+      pf[v] = pk[0];
+      pf[v + 1] = pk[1];
     }
-    return s0 + s1;
+    return sum;
   }
   // the largest score of each query, over both lane halves, times c (finite: a block's first key is valid)
   __device__ static __forceinline__ float largest(f32x16& s, float c) {

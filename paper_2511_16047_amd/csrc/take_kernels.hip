@@ -58,16 +58,17 @@ __device__ __forceinline__ void turn(float& x, float& y, float c, float s) {
   y = yc + xs;
 }
 
-// the 8 pairs of an item; t: their (c, s)
-__device__ __forceinline__ void turn_item(Piece& a, Piece& b, const float* t, bool half) {
+// the 8 pairs of an item; t: their (c, s); back: the sign bit to turn by the other angle, or 0
+__device__ __forceinline__ void turn_item(Piece& a, Piece& b, const float* t, bool half, int back) {
+  auto s = [&](int i) { return __int_as_float(__float_as_int(t[2 * i + 1]) ^ back); };
   if (half) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn(a.x[i], b.x[i], t[2 * i], t[2 * i + 1]);
+    for (int i = 0; i < 8; ++i) turn(a.x[i], b.x[i], t[2 * i], s(i));
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      turn(a.x[2 * i], a.x[2 * i + 1], t[2 * i], t[2 * i + 1]);
-      turn(b.x[2 * i], b.x[2 * i + 1], t[8 + 2 * i], t[8 + 2 * i + 1]);
+      turn(a.x[2 * i], a.x[2 * i + 1], t[2 * i], s(i));
+      turn(b.x[2 * i], b.x[2 * i + 1], t[8 + 2 * i], s(4 + i));
     }
   }
 }
@@ -105,7 +106,8 @@ struct TakeArgs {
 
 // One wave: 16 row slots of 4 lanes.  A slot is a token of one head (T > 8) or of one of 16 / 2^row_shift heads at once.
 template <typename T, int D, bool kEight>
-__global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
+__global__ __launch_bounds__(64 * kWaves, 4) void take_kernel(TakeArgs a) {
+  fetch_arguments<sizeof(TakeArgs)>();
   constexpr int kItems = D / 64;  // per lane
   const int tensor = a.which[blockIdx.y];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -132,9 +134,6 @@ __global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) tab[i][4 * v + e] = x[e];
       }
-      if (a.inverse)
-#pragma unroll
-        for (int e = 1; e < 16; e += 2) tab[i][e] = -tab[i][e];
     } else {
 #pragma unroll
       for (int e = 0; e < 16; ++e) tab[i][e] = 0.f;
@@ -158,9 +157,11 @@ __global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
         x[i][1] = load8(row + at[i][1]);
       }
     }
+    int back = a.inverse ? (int)0x80000000 : 0;
+    asm volatile("" : "+v"(back));  // (formed here, so that the rows are asked for before the table is waited for)
 #pragma unroll
     for (int i = 0; i < kItems; ++i)
-      if (turned[i]) turn_item(x[i][0], x[i][1], tab[i], a.half);
+      if (turned[i]) turn_item(x[i][0], x[i][1], tab[i], a.half, back);
     if (kEight && tensor < 2) {
 #pragma unroll
       for (int i = 0; i < kItems; ++i)
@@ -272,6 +273,7 @@ struct BlockList {
 // reads has arrived before any of it is written, and it is written below where it and all that follows is read.
 template <int D>
 __global__ __launch_bounds__(1024) void move_codes_kernel(Codes c, long long cap_tokens, BlockList list) {
+  fetch_arguments<sizeof(Codes) + 8 + sizeof(BlockList)>();
   constexpr int kChunks = 4;  // of 16 bytes a thread and pass; a block of 16 tokens is D of them
   const long long bh = blockIdx.x;
   unsigned char* rows = (blockIdx.y ? c.v : c.k) + bh * cap_tokens * D;
