@@ -106,7 +106,7 @@ struct TakeArgs {
 
 // One wave: 16 row slots of 4 lanes.  A slot is a token of one head (T > 8) or of one of 16 / 2^row_shift heads at once.
 template <typename T, int D, bool kEight>
-__global__ __launch_bounds__(64 * kWaves, 4) void take_kernel(TakeArgs a) {
+__global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
   fetch_arguments<sizeof(TakeArgs)>();
   constexpr int kItems = D / 64;  // per lane
   const int tensor = a.which[blockIdx.y];
@@ -157,8 +157,11 @@ __global__ __launch_bounds__(64 * kWaves, 4) void take_kernel(TakeArgs a) {
         x[i][1] = load8(row + at[i][1]);
       }
     }
-    int back = a.inverse ? (int)0x80000000 : 0;
-    asm volatile("" : "+v"(back));  // (formed here, so that the rows are asked for before the table is waited for)
+    int back = 0;
+    if constexpr (!kEight) {
+      back = a.inverse ? (int)0x80000000 : 0;
+      asm volatile("" : "+v"(back));  // (formed here, so that the rows are asked for before the table is waited for)
+    }
 #pragma unroll
     for (int i = 0; i < kItems; ++i)
       if (turned[i]) turn_item(x[i][0], x[i][1], tab[i], a.half, back);
