@@ -166,6 +166,32 @@ def test_units(B, H):
     _drive([(2, 2), (10, 10)], B, H, 128, [(0, 0, True)])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,H,queries", [(10, 15, 65), (10, 15, 100), (10, 15, 128), (10, 15, 150), (13, 10, 257), (4, 15, 300)])
+@pytest.mark.parametrize("before", [0, 1, 16, 30, 33, 64, 95, 200])
+def test_many_units_of_many_rows(D, B, H, queries, before):
+    """Enough rows for waves that share K and V: any number of tiles of codes, of rows, of both, and rows left over in each."""
+    sides = ([(1, before)] if before else []) + [(1, queries)]
+    for borrow in (False, True):
+        _drive(sides, B, H, D, [(0, 0, True)], seed=queries + before, borrow_unretained=borrow)
+    if before:
+        _drive(sides, B, H, D, [(1, 0, False)], seed=queries, borrow_unretained=True)      # codes, then rows read in place
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("layout", [COMPACT, PLANNED], ids=["compact", "planned"])
+@pytest.mark.parametrize("packed", [False, True])
+def test_many_units_of_short_segments(D, layout, packed):
+    _drive([(1, 1), (1, 2), (1, 3), (4, 4), (1, 5), (1, 1), (6, 6), (9, 20), (15, 20)], 10, 15, D, [(3, 3, False), (0, 6, False)], packed=packed,
+           layout=layout, borrow_unretained=True)
+
+
+@pytest.mark.parametrize("sharp", [0.0, 20.0, 300.0])
+def test_sharp_scores_of_many_units(sharp):
+    _drive([(4, 4), (10, 10), (16, 16)], 10, 15, 64, [(0, 0, True)], sharp=sharp)
+    _drive([(4, 4), (10, 10), (16, 16)], 10, 15, 128, [(2, 0, False)], sharp=sharp, borrow_unretained=True)
+
+
 @pytest.mark.parametrize("sharp", [0.0, 20.0, 300.0])
 def test_flat_and_sharp_scores(sharp):
     """Uniform weights; a few keys that take everything, at the start and the end of long key runs."""

@@ -106,6 +106,31 @@ def test_many_units():
     c.check(c.run())
 
 
+@pytest.mark.parametrize("layout", ["tokens", "heads", "packed"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,Hkv,Tq", [(10, 10, 100), (10, 10, 129), (20, 10, 150), (14, 14, 257), (7, 7, 700)])
+def test_many_units_of_many_rows(layout, D, H, Hkv, Tq):
+    """Enough rows for waves that share K and V: any number of tiles, none, and states left over."""
+    lengths = [200, 0, 1, 31, 32, 33, 63, 64, 65, 96, 97, 127, 128, 129, 199, 160]
+    c = Case(H, Hkv, D, Tq, 200, lengths, layout)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("sharp", [0.0, 1.0, 300.0])
+def test_many_units_over_many_states(D, sharp):
+    c = Case(17, 17, D, 260, 1100, [1100, 1099, 0, 1024, 1025, 513, 64, 1088, 3, 1100, 1056, 700, 1, 1087, 90, 1100], sharp=sharp)
+    c.check(c.run())
+
+
+def test_few_rows_over_states_that_do_not_fit_anywhere_else():
+    """Hundreds of megabytes of states, read once by teams."""
+    c = Case(32, 32, 64, 20, 4100, [4100] * 10 + [4000, 1] + [33] * 3 + [0])
+    c.check(c.run())
+    c = Case(32, 32, 128, 20, 4100, [4100, 4099, 64, 0, 33])
+    c.check(c.run())
+
+
 def test_no_states_at_all():
     c = Case(4, 2, 64, 7, 0, [0, 0, 0], spoil=False)
     c.check(c.run())
