@@ -23,7 +23,8 @@
  *                           arena; the kept scales sit back to back in ascending scale
  *                           order (AMSKV_LAYOUT_COMPACT) or at offsets fixed at create
  *                           time (AMSKV_LAYOUT_PLANNED); amskv_cache_layout reports them
- * Element type: float (dtype 0) or bfloat16 (dtype 1), the same for every tensor.
+ * Element type: float (dtype 0) or bfloat16 (dtype 1), the same for every tensor; with dtype 2 the tensors are bfloat16 and
+ * the cache holds K and V in 8 bits (see "8-bit cache").
  *
  * Every function returns an amskv_status (0 = ok, negative = error) unless stated.
  * On error nothing has been enqueued and the cache state is unchanged; the one exception is
@@ -135,7 +136,7 @@ typedef struct {
  * until the attend call they are the only copy, and similarity/export read them in place.
  * Device work of one layer must be enqueued on one stream (or be ordered by the caller).
  *
- * Stream capture.  In scale-window mode amskv_append_scale, amskv_attend, amskv_attend_density,
+ * Stream capture.  In scale-window mode amskv_append_scale(_rotary), amskv_attend, amskv_attend_density,
  * amskv_attention_density_enqueue, amskv_interscale_similarity_enqueue and
  * amskv_interscale_similarity_enqueue_static enqueue kernels
  * only -- no memory copies, memsets, events or waits -- so a caller whose Q, K, V and O live in
@@ -181,18 +182,18 @@ typedef struct {
  * finished, or until amskv_cache_reset. */
 
 /* 8-bit cache (dtype = AMSKV_DTYPE_BF16_KV8).  Q, K, V and O are bf16; the arena holds K and V in 8 bits.  Every
- * AMSKV_KV8_BLOCK consecutive tokens of a scale (counted from its first token; the last block may be shorter) share one power
- * of two per (b, h) and tensor.  With m the largest magnitude of such a block of tokens x D and e the least integer >= -100 with
- * m <= 448 * 2^e, an element x is held as the e4m3 number nearest to x / 2^e (4 significant bits, ties to even; x must be
- * finite; beyond 1.875 * 2^127 as that), which stands for that number times 2^e -- a bf16 number exactly, so that nothing else is lost on the way into the
- * attention: relative error at most 2^-4, absolute error at most 2^(e-10) below 2^(e-6), elements below 2^-110 become 0.
+ * AMSKV_KV8_BLOCK consecutive tokens of a scale (counted from its first token; the last block may be shorter) share one
+ * power of two per (b, h) and tensor.  With m the largest magnitude of such a block of tokens x D and e the least integer
+ * >= -100 with m <= 448 * 2^e, an element x is held as the e4m3 number nearest to x / 2^e (4 significant bits, ties to
+ * even; x must be finite; beyond 1.875 * 2^127 as that), which stands for that number times 2^e -- a bf16 number exactly,
+ * so that nothing else is lost on the way into the attention: relative error at most 2^-4, absolute error at most 2^(e-10)
+ * below 2^(e-6), elements below 2^-110 become 0.
  * amskv_attend reads the cached values, the current scale's included, unless that scale is read in place
  * (borrow_unretained), in which case its bf16 K and V are read as they are.  amskv_cache_export writes the values as bf16.
- * Scale-window mode in either layout, either io layout (kv_token_stride below 2^23 elements); fuse_append must be 0.  Slots start at multiples of AMSKV_KV8_BLOCK
- * tokens and capacities are multiples of it.  amskv_cache_bytes_held counts one byte per element and four per
- * block and tensor.  The
- * similarity and density calls are for 16- and 32-bit caches: they return AMSKV_ERR_INVALID_ARG (a model is profiled on one
- * of those). */
+ * Scale-window mode in either layout, either io layout (kv_token_stride below 2^23 elements); fuse_append must be 0.
+ * Slots start at multiples of AMSKV_KV8_BLOCK tokens and capacities are multiples of it.  amskv_cache_bytes_held counts one
+ * byte per element and four per block and tensor.  The similarity and density calls are for 16- and 32-bit caches: they
+ * return AMSKV_ERR_INVALID_ARG (a model is profiled on one of those). */
 
 /* mode = AMSKV_MODE_TOKEN_WINDOW.  The sliding-window and sink-plus-window kept sets that the
  * comparison with other cache strategies (Section 5, the table of SWA / H2O / STA) sets against
@@ -424,7 +425,8 @@ typedef struct {
 } amskv_rope;
 
 /* Distances in elements between batch elements, heads and tokens of a tensor; the channels of a row are contiguous.  Rows start
- * at multiples of 16 bytes.  A dimension of size 1 may have any stride, and a tensor that is only read may repeat (stride 0). */
+ * at multiples of 16 bytes.  A dimension of size 1 may have any stride.  A tensor that is only read may repeat (stride 0); of
+ * one that is written each stride, in ascending order, is at least as long as all that the ones before it span. */
 typedef struct {
   int64_t batch, head, token;
 } amskv_strides;

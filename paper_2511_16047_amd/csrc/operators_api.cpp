@@ -1,5 +1,6 @@
 // C ABI of the calls that need no cache: rotary tables, turning a tensor, cross attention.  Checks and the conversion of
 // strides to bytes; everything else is in the kernels' files.
+#include <algorithm>
 #include <cmath>
 #include <limits>
 
@@ -12,7 +13,8 @@ using amskv::RowMap;
 inline bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
 // Strides of a tensor of `n` = {batch, heads, tokens} rows of head_dim elements, in bytes.  False: a row would not start at a
-// multiple of 16 bytes, a stride is negative or out of range, or (written) rows would share an address.
+// multiple of 16 bytes, a stride is negative or out of range, or (written) the dimensions do not nest, so that rows might
+// share an address.
 bool map_of(const amskv_strides* s, const int64_t (&n)[3], int head_dim, int elem, bool written, RowMap* out) {
   if (!s) return false;
   const int64_t st[3] = {s->batch, s->head, s->token};
@@ -21,8 +23,17 @@ bool map_of(const amskv_strides* s, const int64_t (&n)[3], int head_dim, int ele
     bytes[i] = 0;
     if (n[i] <= 1) continue;
     if (st[i] < 0 || st[i] > ((int64_t)1 << 40) || st[i] * elem % 16 != 0) return false;
-    if (written && st[i] < head_dim) return false;
     bytes[i] = st[i] * elem;
+  }
+  if (written) {
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return st[a] < st[b]; });
+    __int128 span = head_dim;  // (strides up to 2^40, sizes up to 2^26)
+    for (int i : order) {
+      if (n[i] <= 1) continue;
+      if (st[i] < span) return false;
+      span += (__int128)st[i] * (n[i] - 1);
+    }
   }
   *out = RowMap{bytes[0], bytes[1], bytes[2]};
   return true;

@@ -54,6 +54,14 @@ def test_rotate(bad):
     _refused(INVALID, amskv.amskv_rotate, **a)
 
 
+@pytest.mark.parametrize("strides", [(960, 64, 64), (64, 320, 64), (320, 320, 64), (959 - 63, 320, 64), (64, 128, 320), (960, 256, 64), (384, 192, 128)],
+                         ids=str)
+def test_rows_written_twice(strides):
+    """[2][3][5] rows: some would share memory, wholly or in part."""
+    _refused(INVALID, amskv.amskv_rotate, **dict(ROTATE, rope=_rope(), out_strides=amskv.Strides(*strides)))
+    _refused(INVALID, amskv.amskv_cross_attend, _cross(batch=2, heads=3, q_tokens=5, o=amskv.Strides(*strides)), A, A, A, A)
+
+
 @pytest.mark.parametrize("empty", ["batch", "heads", "tokens"])
 def test_rotate_nothing(empty):
     amskv.amskv_rotate(**dict(ROTATE, rope=_rope(), table=None, x=None, out=None, **{empty: 0}))
