@@ -433,7 +433,7 @@ typedef struct {
 
 /* The cosines and sines of n tokens: positions_dev[n][axes] fp64 -> table_dev[n][rot_dim/2][2] fp32.  Angles are formed and
  * reduced in 64 bits and every entry is rounded once, so positions may lie anywhere (whole and broken, negative, far).  A table is
- * made once for a scale, or for the tokens of a step, and used by every layer.  Asynchronous on `stream`. */
+ * made once for a scale, or for the tokens of a step, and used by every layer.  n up to 2^25.  Asynchronous on `stream`. */
 int32_t amskv_rope_table(const amskv_rope* rope, const double* positions_dev, int64_t n, float* table_dev, void* stream);
 
 /* out = x turned, for a tensor [batch][heads][tokens][head_dim] of fp32 or bf16 in any order of its dimensions (x, out strides).
@@ -441,7 +441,8 @@ int32_t amskv_rope_table(const amskv_rope* rope, const double* positions_dev, in
  * inverse != 0 turns back: the gradient with respect to x of a loss whose gradient with respect to out is given.  fp32
  * arithmetic, every product rounded by itself (the same bits whoever forms them), one rounding to bf16.  out_dev == x_dev with
  * equal strides turns in place; otherwise the two must not overlap.  tokens == 0, heads == 0 or batch == 0: nothing to do.
- * rope gives rot_dim and pairing; its other members are not read.  head_dim 64 or 128.  Asynchronous on `stream`. */
+ * rope gives rot_dim and pairing; its other members are not read.  head_dim 64 or 128; batch * heads up to 2^24, tokens up to
+ * 2^22, rows up to 2^29.  Asynchronous on `stream`. */
 int32_t amskv_rotate(const amskv_rope* rope, int32_t dtype, int32_t head_dim, int32_t batch, int32_t heads, int32_t tokens,
                      const float* table_dev, int64_t table_batch, int32_t inverse, const void* x_dev, const amskv_strides* x,
                      void* out_dev, const amskv_strides* out, void* stream);
@@ -467,7 +468,8 @@ int32_t amskv_append_scale_rotary(amskv_cache* cache, int32_t layer, int32_t s, 
  *   offsets_dev[batch + 1]               ascending offsets into packed K and V: row j of b is row offsets[b] + j of one axis of
  *                                        kv_rows rows (k.token, v.token; the batch strides are not used); b has offsets[b+1] -
  *                                        offsets[b] states, of which what goes beyond kv_tokens or kv_rows is left out
- * The token strides of K and V are below 2^23 elements.
+ * The token strides of K and V are below 2^23 elements; batch * heads is up to 2^24, q_tokens up to 2^22 (2^26 with the heads
+ * that share a kv head), kv_tokens up to 2^26.  O overlaps none of the others.
  * bf16: finite Q, K and V, fp32 accumulation and softmax, P rounded to bf16 before the second product, O rounded to bf16. */
 typedef struct {
   int32_t batch, heads, kv_heads; /* heads a multiple of kv_heads                            */

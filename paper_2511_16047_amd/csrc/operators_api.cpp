@@ -63,7 +63,7 @@ int32_t amskv_rope_table(const amskv_rope* r, const double* positions_dev, int64
     return AMSKV_ERR_INVALID_ARG;
   const bool ramp = r->low != 0 || r->high != 0;
   if (ramp && (!(r->low >= 0) || !(r->low < r->high) || !std::isfinite(r->high) || !positive(r->original))) return AMSKV_ERR_INVALID_ARG;
-  if (n < 0 || n > (1 << 28) || misaligned(table_dev) || ((uintptr_t)positions_dev & 7) != 0) return AMSKV_ERR_INVALID_ARG;
+  if (n < 0 || n > (1 << 25) || misaligned(table_dev) || ((uintptr_t)positions_dev & 7) != 0) return AMSKV_ERR_INVALID_ARG;
   if (n == 0) return AMSKV_OK;
   if (!positions_dev || !table_dev) return AMSKV_ERR_INVALID_ARG;
   const int pairs = r->rot_dim / 2, per_axis = pairs / r->axes;
@@ -87,7 +87,7 @@ int32_t amskv_rotate(const amskv_rope* rope, int32_t dtype, int32_t head_dim, in
   if ((head_dim != 64 && head_dim != 128) || (dtype != AMSKV_DTYPE_F32 && dtype != AMSKV_DTYPE_BF16)) return AMSKV_ERR_INVALID_ARG;
   if (int rc = amskv::check_turn(rope, head_dim)) return rc;
   if (batch < 0 || heads < 0 || tokens < 0 || tokens > (1 << 22) || (int64_t)batch * heads > (1 << 24)) return AMSKV_ERR_INVALID_ARG;
-  if ((int64_t)batch * heads * tokens > ((int64_t)1 << 34)) return AMSKV_ERR_INVALID_ARG;  // grids count 16 rows in 32 bits
+  if ((int64_t)batch * heads * tokens > (1 << 29)) return AMSKV_ERR_INVALID_ARG;  // 4 lanes to a row, rows in blocks of 16: 2^32 lanes
   if (table_batch < 0 || table_batch % 4 != 0 || table_batch > ((int64_t)1 << 40)) return AMSKV_ERR_INVALID_ARG;
   const int elem = dtype == AMSKV_DTYPE_F32 ? 4 : 2;
   const int64_t n[3] = {batch, heads, tokens};

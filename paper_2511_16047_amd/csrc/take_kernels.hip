@@ -101,7 +101,7 @@ struct TakeArgs {
   const float* table;
   long long table_batch, cap_tokens;
   int dst_new, pieces_turned, half, inverse;
-  int heads, tokens, blocks, row_shift, groups, heads_per_wave;
+  int batch, heads, tokens, blocks, row_shift, groups, heads_per_wave;
 };
 
 // One wave: 16 row slots of 4 lanes.  A slot is a token of one head (T > 8) or of one of 16 / 2^row_shift heads at once.
@@ -110,9 +110,11 @@ __global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
   fetch_arguments<sizeof(TakeArgs)>();
   constexpr int kItems = D / 64;  // per lane
   const int tensor = a.which[blockIdx.y];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const unsigned unit = blockIdx.x / (unsigned)a.groups, group = blockIdx.x - unit * a.groups;
+  const int lane = threadIdx.x & 63;
+  const unsigned wave = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned unit = wave / (unsigned)a.groups, group = wave - unit * a.groups;
   const unsigned b = unit / (unsigned)a.blocks, block = unit - b * a.blocks;
+  if (b >= (unsigned)a.batch) return;
   const int slot = lane >> 2, rows = 1 << a.row_shift, together = 16 >> a.row_shift;
   const int t = block * 16 + (slot & (rows - 1));
   const bool turns = a.table != nullptr && tensor != 1;
@@ -139,7 +141,7 @@ __global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
       for (int e = 0; e < 16; ++e) tab[i][e] = 0.f;
     }
   }
-  const int first = (group * kWaves + wave) * a.heads_per_wave;
+  const int first = group * a.heads_per_wave;
   for (int h0 = first; h0 < min(first + a.heads_per_wave, a.heads); h0 += together) {
     const int h = h0 + (slot >> a.row_shift);
     const bool live = t < a.tokens && h < a.heads;
@@ -230,6 +232,7 @@ hipError_t take(const Take& t, hipStream_t st) {
   a.pieces_turned = t.table ? t.rot_dim / 8 : 0;
   a.half = t.pairing == AMSKV_ROPE_HALF;
   a.inverse = t.inverse;
+  a.batch = t.batch;
   a.heads = t.heads;
   a.tokens = t.tokens;
   a.blocks = (t.tokens + 15) / 16;
@@ -237,9 +240,9 @@ hipError_t take(const Take& t, hipStream_t st) {
   const int together = 16 >> a.row_shift;
   const long long waves = (long long)t.batch * a.blocks * ((t.heads + together - 1) / together);
   a.heads_per_wave = together * (waves > 16384 ? 4 : 1);
-  a.groups = (t.heads + kWaves * a.heads_per_wave - 1) / (kWaves * a.heads_per_wave);
-  const long long grid = (long long)t.batch * a.blocks * a.groups;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  a.groups = (t.heads + a.heads_per_wave - 1) / a.heads_per_wave;
+  const long long grid = ((long long)t.batch * a.blocks * a.groups + kWaves - 1) / kWaves;
+  if (grid > 0xffffff) return hipErrorInvalidValue;  // 2^32 threads
   const dim3 g((unsigned)grid, n), block(64 * kWaves);
   if constexpr (sizeof(T) == 2) {
     if (t.eight_bits) {
@@ -333,7 +336,8 @@ __global__ __launch_bounds__(256) void export_codes_kernel(Codes c, __bf16* __re
   constexpr int kPer = D / 16;
   const unsigned unit = blockIdx.x / (unsigned)parts, part = blockIdx.x - unit * parts;
   const long long bh = unit;
-  const int i = part * 256 + (int)threadIdx.x, j = i / kPer, piece = i % kPer;
+  const long long i = (long long)part * 256 + threadIdx.x;
+  const int j = (int)(i / kPer), piece = (int)(i % kPer);
   if (j >= seg.total) return;
   bool ext;
   const long long at = locate_row(seg, j, ext);

@@ -91,6 +91,17 @@ def test_rotate(B, H, T, D, rot, pairing, dtype):
             check(z)
 
 
+@pytest.mark.parametrize("B,H,T", [(20001, 1, 17), (3001, 7, 1), (5, 5, 9000), (1, 1, 300001)])
+def test_many_rows(B, H, T):
+    """More blocks than waves that take one head each."""
+    rope = amskv.Rope(rot_dim=32, pairing=amskv.AMSKV_ROPE_INTERLEAVED)
+    tab = _table(rope, (_normal(T, 1, seed=3) * 1000).double())
+    x = _normal(B, H, T, 64, seed=T).bfloat16()
+    out, xs = torch.full_like(x, 7.0), amskv.Strides(H * T * 64, T * 64, 64)
+    amskv.amskv_rotate(rope, amskv.AMSKV_DTYPE_BF16, 64, B, H, T, tab, 0, x, xs, out, xs)
+    assert torch.equal(out, plain.turn(x.float(), tab, "interleaved").bfloat16())
+
+
 def test_a_head_for_all():
     """A tensor that repeats is read with stride 0."""
     B, H, T, D = 2, 6, 20, 64

@@ -36,6 +36,12 @@ def test_tables_buffers():
         _refused(INVALID, amskv.amskv_rope_table, _rope(), p, t, n)
     amskv.amskv_rope_table(_rope(), None, None, 0)       # no tokens: nothing to do
     _refused(INVALID, amskv.amskv_rope_table, None, A, A, 4)
+    _refused(INVALID, amskv.amskv_rope_table, _rope(), A, A, (1 << 25) + 1)
+
+
+def test_rows_beyond_a_launch():
+    row = amskv.Strides(1 << 33, 1 << 28, 64)
+    _refused(INVALID, amskv.amskv_rotate, **dict(ROTATE, rope=_rope(), batch=33, heads=8, tokens=1 << 21, x_strides=row, out_strides=row))
 
 
 ROTATE = dict(dtype=amskv.AMSKV_DTYPE_BF16, head_dim=64, batch=2, heads=3, tokens=5, table=A, table_batch=0, x=A,
