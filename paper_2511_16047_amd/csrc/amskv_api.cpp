@@ -882,10 +882,10 @@ int append_step(amskv_cache* c, int32_t layer, int32_t s, const void* K_dev, con
   if (turn && !copy_now)
     if (int rc = turn_in_place(c, *turn, cur.len, K_dev, (hipStream_t)stream)) return rc;
   if (K_dev && (eight_bits(c->dtype) || (turn && copy_now))) {
-    // the survivors first, then the new scale: turned, quantised or both on the way to its slot
+    // the survivors first, then (in an 8-bit cache at once) the new scale: turned, quantised or both on the way to its slot
     const hipStream_t st = (hipStream_t)stream;
     hipError_t e = hipSuccess;
-    if (mv.n > 0)
+    if (mv.n > 0 && !(eight_bits(c->dtype) && copy_now))
       e = eight_bits(c->dtype) ? amskv::launch_move_codes(codes(c, L), bh, c->head_dim, L.cap, mv, st)
                                : amskv::launch_append(c->arena + L.k_off, c->arena + L.v_off, nullptr, nullptr, bh, row_bytes, L.cap, mv,
                                                       cur.len, 0, 0, caller_map(c, cur.len, c->kv_tok), c->heads, st);
@@ -899,6 +899,7 @@ int append_step(amskv_cache* c, int32_t layer, int32_t s, const void* K_dev, con
       t.dst_new = cur.off;
       if (t.eight_bits) {
         t.codes = codes(c, L);
+        t.moves = &mv;
       } else {
         t.out_map = arena_map(c, L);
         t.k_out = c->arena + L.k_off + (int64_t)cur.off * row_bytes;

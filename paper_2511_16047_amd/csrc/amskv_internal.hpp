@@ -307,6 +307,7 @@ struct Take {
   int32_t rot_dim, pairing, inverse;
   int32_t batch, heads, tokens, head_dim, dtype;  // dtype: of the sources, AMSKV_DTYPE_F32 or _BF16
   bool eight_bits;
+  const MoveList* moves;            // eight_bits: survivors that slide to their new places first (launch_move_codes), or null
 };
 hipError_t launch_take(const Take& t, hipStream_t st) AMSKV_WEAK;
 // The survivors of a compaction slide to their new places (mv in tokens, whole blocks of 16).

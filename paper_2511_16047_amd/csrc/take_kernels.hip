@@ -23,7 +23,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4, kOwners = 8;
 
 struct Piece {
   float x[8];
@@ -104,17 +104,12 @@ struct TakeArgs {
   int batch, heads, tokens, blocks, row_shift, groups, heads_per_wave;
 };
 
-// One wave: 16 row slots of 4 lanes.  A slot is a token of one head (T > 8) or of one of 16 / 2^row_shift heads at once.
+// One wave: a block of 16 tokens of heads [first, end) of batch element b, in 16 row slots of 4 lanes.  A slot is a token of one
+// head (T > 8) or of one of 16 / 2^row_shift heads at once.
 template <typename T, int D, bool kEight>
-__global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
-  fetch_arguments<sizeof(TakeArgs)>();
+__device__ __forceinline__ void take_block(const TakeArgs& a, int tensor, unsigned b, int block, int first, int end) {
   constexpr int kItems = D / 64;  // per lane
-  const int tensor = a.which[blockIdx.y];
   const int lane = threadIdx.x & 63;
-  const unsigned wave = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const unsigned unit = wave / (unsigned)a.groups, group = wave - unit * a.groups;
-  const unsigned b = unit / (unsigned)a.blocks, block = unit - b * a.blocks;
-  if (b >= (unsigned)a.batch) return;
   const int slot = lane >> 2, rows = 1 << a.row_shift, together = 16 >> a.row_shift;
   const int t = block * 16 + (slot & (rows - 1));
   const bool turns = a.table != nullptr && tensor != 1;
@@ -141,10 +136,9 @@ __global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
       for (int e = 0; e < 16; ++e) tab[i][e] = 0.f;
     }
   }
-  const int first = group * a.heads_per_wave;
-  for (int h0 = first; h0 < min(first + a.heads_per_wave, a.heads); h0 += together) {
+  for (int h0 = first; h0 < end; h0 += together) {
     const int h = h0 + (slot >> a.row_shift);
-    const bool live = t < a.tokens && h < a.heads;
+    const bool live = t < a.tokens && h < end;
     Piece x[kItems][2];
     float m = 0.f;
 #pragma unroll
@@ -207,66 +201,15 @@ __global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
   }
 }
 
-template <typename T, int D>
-hipError_t take(const Take& t, hipStream_t st) {
-  TakeArgs a{};
-  const void* src[3] = {t.k, t.v, t.q};
-  int n = 0;
-  for (int i = 0; i < 3; ++i)
-    if (src[i]) a.which[n++] = i;
-  if (n == 0 || t.batch == 0 || t.heads == 0 || t.tokens == 0) return hipSuccess;
-  for (int i = 0; i < 3; ++i) {
-    a.src[i] = (const char*)src[i];
-    a.from[i] = i == 2 ? t.q_map : t.kv_map;
-    a.to[i] = i == 2 ? t.q_out_map : t.out_map;
-  }
-  a.dst[0] = t.eight_bits ? (char*)t.codes.k : (char*)t.k_out;
-  a.dst[1] = t.eight_bits ? (char*)t.codes.v : (char*)t.v_out;
-  a.dst[2] = (char*)t.q_out;
-  a.scales[0] = t.codes.k_scale;
-  a.scales[1] = t.codes.v_scale;
-  a.table = t.table;
-  a.table_batch = t.table_batch;
-  a.cap_tokens = t.cap_tokens;
-  a.dst_new = t.dst_new;
-  a.pieces_turned = t.table ? t.rot_dim / 8 : 0;
-  a.half = t.pairing == AMSKV_ROPE_HALF;
-  a.inverse = t.inverse;
-  a.batch = t.batch;
-  a.heads = t.heads;
-  a.tokens = t.tokens;
-  a.blocks = (t.tokens + 15) / 16;
-  a.row_shift = t.tokens > 8 ? 4 : t.tokens > 4 ? 3 : t.tokens > 2 ? 2 : t.tokens > 1 ? 1 : 0;
-  const int together = 16 >> a.row_shift;
-  const long long waves = (long long)t.batch * a.blocks * ((t.heads + together - 1) / together);
-  a.heads_per_wave = together * (waves > 16384 ? 4 : 1);
-  a.groups = (t.heads + a.heads_per_wave - 1) / a.heads_per_wave;
-  const long long grid = ((long long)t.batch * a.blocks * a.groups + kWaves - 1) / kWaves;
-  if (grid > 0xffffff) return hipErrorInvalidValue;  // 2^32 threads
-  const dim3 g((unsigned)grid, n), block(64 * kWaves);
-  if constexpr (sizeof(T) == 2) {
-    if (t.eight_bits) {
-      hipLaunchKernelGGL((take_kernel<T, D, true>), g, block, 0, st, a);
-      return hipGetLastError();
-    }
-  }
-  hipLaunchKernelGGL((take_kernel<T, D, false>), g, block, 0, st, a);
-  return hipGetLastError();
-}
-
-// Angles in 64 bits, one thread to a pair of a token; frequencies come with the arguments.
-struct Frequencies {
-  double f[64];
-};
-__global__ __launch_bounds__(256) void rope_table_kernel(const double* __restrict__ positions, float2* __restrict__ table, int pairs, int axes,
-                                                         double amplitude, long long total, Frequencies f) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= total) return;
-  const long long token = i / pairs;
-  const int pair = (int)(i - token * pairs), per_axis = pairs / axes, axis = pair / per_axis;
-  double s, c;
-  sincos(positions[token * axes + axis] * f.f[pair - axis * per_axis], &s, &c);
-  table[i] = make_float2((float)(amplitude * c), (float)(amplitude * s));
+template <typename T, int D, bool kEight>
+__global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
+  fetch_arguments<sizeof(TakeArgs)>();
+  const unsigned wave = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned unit = wave / (unsigned)a.groups, group = wave - unit * a.groups;
+  const unsigned b = unit / (unsigned)a.blocks, block = unit - b * a.blocks;
+  if (b >= (unsigned)a.batch) return;
+  const int first = group * a.heads_per_wave;
+  take_block<T, D, kEight>(a, a.which[blockIdx.y], b, block, first, min(first + a.heads_per_wave, a.heads));
 }
 
 // Blocks that slide to lower places, in the order of their offsets: begin[i] .. begin[i+1] of the list come from src[i] and go to
@@ -275,15 +218,12 @@ struct BlockList {
   int32_t n, total;
   int32_t begin[AMSKV_MAX_SCALES], src[AMSKV_MAX_SCALES], dst[AMSKV_MAX_SCALES];
 };
-// One workgroup owns the codes and scales of one (b,h) of one tensor and moves them a pass at a time: everything a pass
-// reads has arrived before any of it is written, and it is written below where it and all that follows is read.
+// The codes and scales of one (b,h) of one tensor slide, a pass at a time, by all threads of the workgroup: everything a pass reads
+// has arrived before any of it is written, and it is written below where it and all that follows is read.  Behind the last
+// barrier nothing is left to read.
 template <int D>
-__global__ __launch_bounds__(1024) void move_codes_kernel(Codes c, long long cap_tokens, BlockList list) {
-  fetch_arguments<sizeof(Codes) + 8 + sizeof(BlockList)>();
+__device__ __forceinline__ void slide(unsigned char* rows, float* scales, const BlockList& list) {
   constexpr int kChunks = 4;  // of 16 bytes a thread and pass; a block of 16 tokens is D of them
-  const long long bh = blockIdx.x;
-  unsigned char* rows = (blockIdx.y ? c.v : c.k) + bh * cap_tokens * D;
-  float* scales = (blockIdx.y ? c.v_scale : c.k_scale) + bh * (cap_tokens / AMSKV_KV8_BLOCK);
   auto place = [&](int i, int& src, int& dst) {
     src = dst = 0;
     for (int r = 0; r < list.n; ++r)
@@ -325,6 +265,113 @@ __global__ __launch_bounds__(1024) void move_codes_kernel(Codes c, long long cap
     __syncthreads();
     if (i < list.total) scales[dst] = x;
   }
+}
+
+template <int D>
+__global__ __launch_bounds__(1024) void move_codes_kernel(Codes c, long long cap_tokens, BlockList list) {
+  fetch_arguments<sizeof(Codes) + 8 + sizeof(BlockList)>();
+  const long long bh = blockIdx.x;
+  slide<D>((blockIdx.y ? c.v : c.k) + bh * cap_tokens * D, (blockIdx.y ? c.v_scale : c.k_scale) + bh * (cap_tokens / AMSKV_KV8_BLOCK), list);
+}
+
+// Both in one launch: the workgroup that owns a (b,h) of a tensor slides what stays of it, then its waves take the blocks of the
+// new scale, whose place may be where the survivors lay.
+template <int D>
+__global__ __launch_bounds__(64 * kOwners) void slide_and_take_kernel(TakeArgs a, BlockList list) {
+  fetch_arguments<sizeof(TakeArgs) + sizeof(BlockList)>();
+  const int tensor = a.which[blockIdx.y];
+  const long long bh = blockIdx.x;
+  const unsigned b = (unsigned)bh / (unsigned)a.heads;
+  const int h = (int)(bh - (long long)b * a.heads);
+  if (tensor < 2) slide<D>((unsigned char*)a.dst[tensor] + bh * a.cap_tokens * D, a.scales[tensor] + bh * (a.cap_tokens / AMSKV_KV8_BLOCK), list);
+  for (int block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); block < a.blocks; block += kOwners)
+    take_block<__bf16, D, true>(a, tensor, b, block, h, h + 1);
+}
+
+BlockList block_list(const MoveList& mv) {
+  BlockList list{};
+  for (int i = 0; i < mv.n; ++i) {
+    list.begin[list.n] = list.total;
+    list.src[list.n] = mv.src[i] / AMSKV_KV8_BLOCK;
+    list.dst[list.n] = mv.dst[i] / AMSKV_KV8_BLOCK;
+    list.total += mv.len[i] / AMSKV_KV8_BLOCK;
+    ++list.n;
+  }
+  return list;
+}
+
+template <typename T, int D>
+hipError_t take(const Take& t, hipStream_t st) {
+  TakeArgs a{};
+  const void* src[3] = {t.k, t.v, t.q};
+  int n = 0;
+  for (int i = 0; i < 3; ++i)
+    if (src[i]) a.which[n++] = i;
+  if (n == 0 || t.batch == 0 || t.heads == 0 || t.tokens == 0) return hipSuccess;
+  for (int i = 0; i < 3; ++i) {
+    a.src[i] = (const char*)src[i];
+    a.from[i] = i == 2 ? t.q_map : t.kv_map;
+    a.to[i] = i == 2 ? t.q_out_map : t.out_map;
+  }
+  a.dst[0] = t.eight_bits ? (char*)t.codes.k : (char*)t.k_out;
+  a.dst[1] = t.eight_bits ? (char*)t.codes.v : (char*)t.v_out;
+  a.dst[2] = (char*)t.q_out;
+  a.scales[0] = t.codes.k_scale;
+  a.scales[1] = t.codes.v_scale;
+  a.table = t.table;
+  a.table_batch = t.table_batch;
+  a.cap_tokens = t.cap_tokens;
+  a.dst_new = t.dst_new;
+  a.pieces_turned = t.table ? t.rot_dim / 8 : 0;
+  a.half = t.pairing == AMSKV_ROPE_HALF;
+  a.inverse = t.inverse;
+  a.batch = t.batch;
+  a.heads = t.heads;
+  a.tokens = t.tokens;
+  a.blocks = (t.tokens + 15) / 16;
+  a.row_shift = t.tokens > 8 ? 4 : t.tokens > 4 ? 3 : t.tokens > 2 ? 2 : t.tokens > 1 ? 1 : 0;
+  const int together = 16 >> a.row_shift;
+  const long long waves = (long long)t.batch * a.blocks * ((t.heads + together - 1) / together);
+  a.heads_per_wave = together * (waves > 16384 ? 4 : 1);
+  a.groups = (t.heads + a.heads_per_wave - 1) / a.heads_per_wave;
+  const long long grid = ((long long)t.batch * a.blocks * a.groups + kWaves - 1) / kWaves;
+  if (grid > 0xffffff) return hipErrorInvalidValue;  // 2^32 threads
+  const dim3 g((unsigned)grid, n), block(64 * kWaves);
+  if constexpr (sizeof(T) == 2) {
+    if (t.eight_bits && t.moves != nullptr && t.moves->n > 0) {
+      // us an append, at once / in two launches, units x tokens.  D 64: 16 x 16 3.6 / 4.6, 16 x 256 4.9 / 5.1, 16 x 512 7.1 / 5.8, 256 x 64
+      // 4.8 / 6.4, 256 x 256 9.4 / 13.1, 256 x 512 16.3 / 20.4 (turned: 29.8 / 28.3), 960 x 16 9.1 / 6.8, 960 x 256 30.7 / 32.8.  D 128: 16 x
+      // 128 4.6 / 5.4, 16 x 256 6.2 / 6.1, 256 x 128 10.8 / 11.6, 256 x 256 20.3 / 20.2, 960 x 64 21.2 / 17.3.  So: where a workgroup to a
+      // (b,h) and tensor has few blocks to a wave, and there are no more of them than the chip holds at once.
+      if (t.batch * t.heads <= 256 && t.tokens * D <= 16384) {
+        hipLaunchKernelGGL((slide_and_take_kernel<D>), dim3(t.batch * t.heads, n), dim3(64 * kOwners), 0, st, a, block_list(*t.moves));
+        return hipGetLastError();
+      }
+      const hipError_t e = launch_move_codes(t.codes, t.batch * t.heads, t.head_dim, t.cap_tokens, *t.moves, st);
+      if (e != hipSuccess) return e;
+    }
+    if (t.eight_bits) {
+      hipLaunchKernelGGL((take_kernel<T, D, true>), g, block, 0, st, a);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((take_kernel<T, D, false>), g, block, 0, st, a);
+  return hipGetLastError();
+}
+
+// Angles in 64 bits, one thread to a pair of a token; frequencies come with the arguments.
+struct Frequencies {
+  double f[64];
+};
+__global__ __launch_bounds__(256) void rope_table_kernel(const double* __restrict__ positions, float2* __restrict__ table, int pairs, int axes,
+                                                         double amplitude, long long total, Frequencies f) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= total) return;
+  const long long token = i / pairs;
+  const int pair = (int)(i - token * pairs), per_axis = pairs / axes, axis = pair / per_axis;
+  double s, c;
+  sincos(positions[token * axes + axis] * f.f[pair - axis * per_axis], &s, &c);
+  table[i] = make_float2((float)(amplitude * c), (float)(amplitude * s));
 }
 
 // The values of the resident segments, ascending and back to back, as bf16 [BH][T_kept][D]; a lane takes 16 channels of a row.
@@ -376,14 +423,7 @@ hipError_t launch_rope_table(const double* frequency, int pairs, int axes, doubl
 }
 
 hipError_t launch_move_codes(const Codes& c, int bh, int head_dim, int64_t cap_tokens, const MoveList& mv, hipStream_t st) {
-  BlockList list{};
-  for (int i = 0; i < mv.n; ++i) {
-    list.begin[list.n] = list.total;
-    list.src[list.n] = mv.src[i] / AMSKV_KV8_BLOCK;
-    list.dst[list.n] = mv.dst[i] / AMSKV_KV8_BLOCK;
-    list.total += mv.len[i] / AMSKV_KV8_BLOCK;
-    ++list.n;
-  }
+  const BlockList list = block_list(mv);
   if (list.total == 0) return hipSuccess;
   const int threads = (long long)list.total * head_dim <= 1024 && bh >= 128 ? 256 : 1024;
   auto kernel = head_dim == 64 ? move_codes_kernel<64> : move_codes_kernel<128>;
