@@ -5,6 +5,8 @@
 // head's r / T -- so shared heads read K and V once, and a single token of 8 heads is one block of 8 rows, not 8 of one.
 // A launch over few rows and many states does not fill the chip with one workgroup to 32 or 128 rows; then `splits` workgroups
 // take equal runs of key tiles each, leave their sums unnormalised in the workspace, and a second launch puts them together.
+#include <cmath>
+
 #include "attend_rows.hpp"
 
 namespace amskv {
@@ -167,8 +169,26 @@ Division divide(int head_dim, long long units, long long n, int keys) {
   const int tile = d.team_waves == 8 ? 64 : 32;
   const long long groups = units * ((n + 32 * d.team_waves - 1) / (32 * d.team_waves));
   const int trips = (int)(((long long)keys + tile * d.teams - 1) / (tile * d.teams));
-  // 2 workgroups to a CU, each with 4 tiles for a team at least
-  if (groups < 256 && trips >= 8) d.splits = (int)fmin((512 + groups - 1) / groups, trips / 4);
+  // The keys of a row tile are shared by `splits` workgroups, each with 4 tiles for a team at least and 2 to a CU at most, where
+  // that is estimated to be shorter (us): a tile takes 0.6 (a block of 32 keys at head dim 128 by one wave 1.1, a tile of 64 by
+  // eight waves 0.8), longer where a CU has several workgroups, beside what K and V take to arrive; splitting costs a launch and the
+  // way of its sums through the workspace.  us with / without:  Head dim 64: 8 x 1 query x 2000
+  // states 8.4 / 12.2, 16000 12.7 / 71.5, 64 x 1 x 16000 49 / 110, 150 x 128 x 2000 31 / 40, 16000 174 / 302 (with 4 instead of 3 to a row tile
+  // 167, with 2 195).  Head dim 128: 16 x 256 x 4000 29 / 40, 230 row tiles of 128 x 16000 270 / 303, x 2000 not split 43 (in two 55).
+  if (groups >= 256 || trips < 8) return d;
+  const double tile_us = d.team_waves == 8 ? 0.8 : d.team_waves == 1 && head_dim == 128 ? 1.1 : 0.6, arrive = bytes / 5.5e6;
+  const double share = d.team_waves == 1 ? 1.15 : d.team_waves == 4 ? 0.65 : 0.75;
+  const double sums = 2e-6 / 2.5 * groups * partial_floats(32 * d.team_waves, head_dim) * 4;
+  double least = 0;
+  for (int s = 1; s <= min((512 + groups - 1) / groups, trips / 4ll); s += s < 16 ? 1 : s / 8) {
+    const long long per_cu = (groups * s + 255) / 256;
+    const double walk = (double)trips / s * tile_us * (per_cu == 1 ? 1.0 : fmax(1.0, share * per_cu));
+    const double us = std::hypot(walk, arrive) + (s == 1 ? 0 : 3 + 0.1 * s + sums * s);
+    if (s == 1 || us < least) {
+      least = us;
+      d.splits = s;
+    }
+  }
   return d;
 }
 
