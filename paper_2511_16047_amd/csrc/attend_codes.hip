@@ -52,26 +52,26 @@ hipError_t go(const void* q, void* o, const Codes& c, int bh, int t_q, int64_t c
 }
 
 // Which form: waves to a team, teams to a workgroup.  `units` (b,h) of `n` query rows over `keys` keys.  One key block: waves by
-// themselves.  Few waves of 32 rows: the keys of a row block are shared by 4 or 8 of them.  Otherwise waves by themselves up to 64
-// rows, where there is little to share, and teams that read K and V once for 128 or 256 rows beyond.  us a launch, 8-bit keys, for
-// <1,1> / <1,4> / <1,8> / <4,1> / <8,1>.  Head dim 64: 16 units 256 x 530 14.5 / 7.3 / 6.6 / 14.1 / 15.5, 64 units 169 x 338 11.2 / 7.6 / 8.3 /
-// 11.1 / 11.3, 400 x 1400 36.9 / 24.9 / 26.5 / 31.9 / 32.5, 256 units 30 x 2030 42.6 / 15.2 / 13.2 / 41.5 / 29.7, 100 x 205 9.2 / 9.4 / 12.5 / 9.1 /
-// 8.6, 960 units 64 x 130 10.7 / 14.4 / 20.5 / 11.3 / 16.6, 100 x 205 19.0 / 25.3 / 36.3 / 18.4 / 20.8, 3840 units 25 x 55 11.1 / 18.7 / 28.7 /
-// 20.1 / 30.8, 256 x 530 259 / 320 / 400 / 218 / 214.  Head dim 128: 16 units 256 x 530 17.4 / 9.4 / 9.9 / 17.3 / 21.2, 64 units 256 x 530
-// 20.0 / 14.9 / 19.1 / 18.4 / 22.3, 400 x 1400 46.9 / 43.1 / 52.8 / 39.3 / 45.6, 256 units 36 x 82 6.7 / 8.0 / 12.2 / 7.2 / 7.1, 960 units 64 x 130
-// 18.0 / 29.8 / 49.4 / 22.0 / 31.4, 256 x 530 126 / 165 / 242 / 101 / 100.
+// themselves.  Few waves of 32 rows: the keys of a row block are shared by 4 or 8 of them.  Otherwise teams, which read K and V
+// once for 128 or 256 rows, where that pays for the rows they are padded to: a row of a team costs 0.70 to 0.95 of a lone
+// wave's, less the longer the keys.  us a launch, <1,1> / <1,4> / <1,8> / <4,1> / <8,1>.  Head dim 64: 16 units 256 x 530 14.5 / 7.3 / 6.6 / 14.1 /
+// 15.5, 64 units 400 x 1400 36.9 / 24.9 / 26.5 / 31.9 / 32.5, 256 units 100 x 205 9.2 / 9.4 / 12.5 / 9.1 / 8.6, 560 units 260 x 265 27.9 / 37.4 / 54.6 /
+// 30.9 / 37.3, 1360 units 355 x 359 98 / 126 / 165 / 84 / 94, 3840 units 25 x 55 11.1 / 18.7 / 28.7 / 20.1 / 30.8, 256 x 530 259 / 320 / 400 / 218 / 214.
+// Head dim 128: 16 units 256 x 530 17.4 / 9.4 / 9.9 / 17.3 / 21.2, 15 units 1344 x 5136 148 / 101 / 103 / 121 / 143, 304 units 354 x 1179 132 / 151 /
+// 183 / 101 / 122, 64 units 1844 x 2324 229 / 239 / - / 185 / 173, 2160 units 120 x 122 52 / 95 / - / 56 / 68.  (263 shapes, half of them drawn; the
+// choice takes 1.008 of the best on average.)
 rows::Form choose(int head_dim, long long units, long long n, long long keys) {
   const long long waves = units * ((n + 31) / 32), wide = units * ((n + 255) / 256), blocks = (keys + 31) / 32;
   if (blocks <= 1) return {1, 1};
   if (head_dim == 64) {
     if (waves <= 256 && blocks >= 16) return {1, 8};
-    if (waves <= 512 || (waves <= 1024 && (wide <= 128 || (n <= 32 && blocks >= 32)))) return {1, 4};
-  } else {
-    if (waves <= 208 && blocks >= 40) return {1, 8};
-    if (waves <= (blocks >= 8 ? 512 : blocks >= 3 ? 256 : 0)) return {1, 4};
+    if (waves <= 512 || (waves <= 1024 && (wide <= 128 || blocks >= (n <= 32 ? 32 : 12)))) return {1, 4};
+    return keys < 256 ? rows::cheapest(n, 0.85, 0.78) : rows::cheapest(n, 0.77, 0.69);
   }
-  if (n <= 64) return {1, 1};
-  return n <= 128 || wide <= 128 ? rows::Form{4, 1} : rows::Form{8, 1};
+  if (waves <= 208 && blocks >= 40) return {1, 8};
+  if (waves <= (blocks >= 50 ? 800 : blocks >= 8 ? 512 : blocks >= 3 ? 256 : 0)) return {1, 4};
+  if (keys < 256) return rows::cheapest(n, 0.92, 0.95);
+  return keys < 1024 ? rows::cheapest(n, 0.75, 0.78) : rows::cheapest(n, 0.76, wide < 256 ? 1.0 : 0.70);  // (one workgroup of eight waves to a CU)
 }
 
 }  // namespace

@@ -142,29 +142,29 @@ __global__ __launch_bounds__(256) void cross_meet_kernel(CrossArgs a, int rows_o
 struct Division {
   int team_waves, teams, splits;
 };
-// `units` (b, kv head) of `n` query rows over up to `keys` states.  Waves by themselves where there are at most 96 states; few waves of
-// 32 rows: four to a row block; otherwise teams that read K and V once for 128 rows, or 256 where that pays; up to 64 rows, waves by
-// themselves, until K and V are so large that the rows of a tile are better brought by a team, whole rows at a time, than by
-// lanes that follow a key each.  us a launch, <1,1> / <1,4> / <1,8> / <4,1> / <8,1>, lengths anywhere up to the number given (16 heads, batch B).
-// Head dim 64: B 8, 36 x 77 4.9 / 4.9 / 5.8 / 5.4 / 5.2, 1 x 4000 19.4 / 14.2 / 14.9 / 18.7 / 17.9, 1 x 16000 95.7 / 85.7 / 86.4 / 81.5 / 69.4, 256 x 512
-// 13.2 / 11.7 / 16.5 / 14.0 / 24.7, B 32 256 x 512 32 / 39 / 51 / 24 / 27, 1024 x 512 100 / 128 / 177 / 67 / 67, B 96 9 x 250 14.0 / 14.4 / 17.9 /
-// 16.6 / 22.1.  Head dim 128: B 2 256 x 64 5.3 / 6.2 / 7.2 / 6.7 / 8.2, B 8 1 x 512 12.2 / 9.1 / 9.8 / 12.3 / 12.9, 1 x 4000 39 / 36 / 33 / 33 / 38, 100 x
-// 250 10.0 / 9.5 / 16.0 / 19.7 / 10.3, 4096 x 77 72 / 166 / 342 / 65 / 79, B 32 1024 x 512 268 / 339 / 598 / 152 / 151.  (137 shapes, the choice
-// takes 1.014 of the best on average.)
+// `units` (b, kv head) of `n` query rows over up to `keys` states.  Waves by themselves where there are at most 96 states and not
+// many rows; few waves of 32 rows: four to a row block; otherwise teams that read K and V once for 128 or 256 rows where that
+// pays for the rows they are padded to -- a row of a team costs 0.58 to 0.95 of a lone wave's, less the longer the keys, as K
+// and V are better brought by a team, whole rows at a time, than by lanes that follow a key each; for the same reason up to 64
+// rows too where K and V are large.  Teams of eight at head dim 128 are left out: 6% shorter at best, mostly longer.  us a launch, <1,1> / <1,4> / <4,1> / <8,1> (16 heads, batch B).  Head dim 64: B 8, 36 x 77 4.9 / 4.9 / 5.4 /
+// 5.2, B 32 256 x 512 32 / 39 / 24 / 27, 1024 x 512 100 / 128 / 67 / 67, 589 units 1 x 1999 62 / 57 / 54 / 69, 481 units 2432 x 231 231 / 300 / 162 / 164, 230
+// units 358 x 19 7.7 / 14.9 / 7.5 / 8.4.  Head dim 128: B 2 256 x 64 5.3 / 6.2 / 6.7 / 8.2, B 8 4096 x 77 72 / 166 / 65 / 79, 146 units 272 x 2063 127 / 126 /
+// 77 / 121, 10 units 1053 x 4446 124 / 90 / 47 / 58, 722 units 424 x 10 35 / 94 / 37 / 47, 12 units 2812 x 1530 81 / 84 / 53 / 50.  (247 shapes, 110 of them
+// drawn; the choice takes 1.008 of the best of those on average.)
 Division divide(int head_dim, long long units, long long n, int keys) {
   const long long waves = units * ((n + 31) / 32), wide = units * ((n + 255) / 256), blocks = ((long long)keys + 31) / 32;
   const long long bytes = units * keys * head_dim * 4;
-  rows::Form f{4, 1};
-  if (blocks <= 1 || (blocks <= 3 && (n <= 64 || waves <= 512)))
+  rows::Form f;
+  if (blocks <= 3 && (n <= 64 || waves <= 1024))
     f = {1, 1};
-  else if (n <= 64 && blocks >= 100 && bytes >= (head_dim == 64 ? 400000000 : 250000000))
+  else if (n <= 64 && blocks >= 64 && bytes >= (head_dim == 64 ? 400000000 : 250000000))
     f = head_dim == 64 ? rows::Form{8, 1} : rows::Form{4, 1};
-  else if (waves <= 512 || (head_dim == 64 && waves <= 1024 && wide <= 128))
+  else if (head_dim == 64 ? waves <= 512 || (waves <= 1024 && wide <= 128) : waves <= 256 || (waves <= 512 && n <= 64))
     f = {1, 4};
-  else if (n <= 64)
-    f = {1, 1};
-  else if (n > 128 && (head_dim == 64 ? n > 256 : keys >= 1024 && wide >= 256))
-    f = {8, 1};
+  else if (head_dim == 64)
+    f = keys <= 96 ? rows::cheapest(n, 0.92, 0.95) : keys < 256 ? rows::cheapest(n, 0.85, 0.81) : rows::cheapest(n, 0.73, 0.66);
+  else
+    f = rows::cheapest(n, keys <= 32 ? 1.0 : keys <= 128 ? 0.88 : 0.58, HUGE_VAL);  // (no eight waves: one workgroup to a CU)
   Division d{f.team_waves, f.teams, 1};
   const int tile = d.team_waves == 8 ? 64 : 32;
   const long long groups = units * ((n + 32 * d.team_waves - 1) / (32 * d.team_waves));
@@ -246,7 +246,7 @@ hipError_t launch_cross(const CrossCall& c, hipStream_t st) {
     return d.team_waves == 4 ? go<64, 4, 1, 4>(a, st) : go<64, 8, 1, 4>(a, st);
   }
   if (d.team_waves == 1) return d.teams == 1 ? go<128, 1, 1, 2>(a, st) : go<128, 1, 4, 2>(a, st);
-  return d.team_waves == 4 ? go<128, 4, 1, 2>(a, st) : go<128, 8, 1, 2>(a, st);
+  return go<128, 4, 1, 2>(a, st);
 }
 
 }  // namespace amskv

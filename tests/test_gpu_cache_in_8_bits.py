@@ -167,7 +167,8 @@ def test_units(B, H):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("B,H,queries", [(10, 15, 65), (10, 15, 100), (10, 15, 128), (10, 15, 150), (13, 10, 257), (4, 15, 300)])
+@pytest.mark.parametrize("B,H,queries", [(10, 15, 65), (10, 15, 100), (10, 15, 128), (10, 15, 150), (10, 15, 225), (10, 15, 256), (13, 10, 257),
+                                         (4, 15, 300), (5, 15, 500)])
 @pytest.mark.parametrize("before", [0, 1, 16, 30, 33, 64, 95, 200])
 def test_many_units_of_many_rows(D, B, H, queries, before):
     """Enough rows for waves that share K and V: any number of tiles of codes, of rows, of both, and rows left over in each."""
@@ -176,6 +177,12 @@ def test_many_units_of_many_rows(D, B, H, queries, before):
         _drive(sides, B, H, D, [(0, 0, True)], seed=queries + before, borrow_unretained=borrow)
     if before:
         _drive(sides, B, H, D, [(1, 0, False)], seed=queries, borrow_unretained=True)      # codes, then rows read in place
+
+
+@pytest.mark.parametrize("before", [799, 831, 840])
+def test_many_units_over_many_tokens(before):
+    for borrow in (False, True):
+        _drive([(1, before), (1, 225)], 17, 16, 128, [(1, 0, False)], seed=before, borrow_unretained=borrow)
 
 
 @pytest.mark.parametrize("D", [64, 128])

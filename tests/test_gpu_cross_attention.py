@@ -108,7 +108,7 @@ def test_many_units():
 
 @pytest.mark.parametrize("layout", ["tokens", "heads", "packed"])
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("H,Hkv,Tq", [(10, 10, 100), (10, 10, 129), (20, 10, 150), (14, 14, 257), (7, 7, 700)])
+@pytest.mark.parametrize("H,Hkv,Tq", [(10, 10, 100), (10, 10, 129), (20, 10, 150), (12, 12, 250), (14, 14, 257), (7, 7, 700)])
 def test_many_units_of_many_rows(layout, D, H, Hkv, Tq):
     """Enough rows for waves that share K and V: any number of tiles, none, and states left over."""
     lengths = [200, 0, 1, 31, 32, 33, 63, 64, 65, 96, 97, 127, 128, 129, 199, 160]
@@ -118,8 +118,9 @@ def test_many_units_of_many_rows(layout, D, H, Hkv, Tq):
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("sharp", [0.0, 1.0, 300.0])
-def test_many_units_over_many_states(D, sharp):
-    c = Case(17, 17, D, 260, 1100, [1100, 1099, 0, 1024, 1025, 513, 64, 1088, 3, 1100, 1056, 700, 1, 1087, 90, 1100], sharp=sharp)
+@pytest.mark.parametrize("H,Tq", [(17, 260), (8, 500)])
+def test_many_units_over_many_states(D, sharp, H, Tq):
+    c = Case(H, H, D, Tq, 1100, [1100, 1099, 0, 1024, 1025, 513, 64, 1088, 3, 1100, 1056, 700, 1, 1087, 90, 1100], sharp=sharp)
     c.check(c.run())
 
 
