@@ -66,12 +66,25 @@ rows::Form choose(int head_dim, long long units, long long n, long long keys) {
   if (head_dim == 64) {
     if (waves <= 256 && blocks >= 16) return {1, 8};
     if (waves <= 512 || (waves <= 1024 && (wide <= 128 || blocks >= (n <= 32 ? 32 : 12)))) return {1, 4};
-    return keys < 256 ? rows::cheapest(n, 0.85, 0.78) : rows::cheapest(n, 0.77, 0.69);
+  } else {
+    if (waves <= 208 && blocks >= 40) return {1, 8};
+    if (waves <= (blocks >= 50 ? 800 : blocks >= 8 ? 512 : blocks >= 3 ? 256 : 0)) return {1, 4};
   }
-  if (waves <= 208 && blocks >= 40) return {1, 8};
-  if (waves <= (blocks >= 50 ? 800 : blocks >= 8 ? 512 : blocks >= 3 ? 256 : 0)) return {1, 4};
-  if (keys < 256) return rows::cheapest(n, 0.92, 0.95);
-  return keys < 1024 ? rows::cheapest(n, 0.75, 0.78) : rows::cheapest(n, 0.76, wide < 256 ? 1.0 : 0.70);  // (one workgroup of eight waves to a CU)
+  rows::Form f;
+  if (head_dim == 64)
+    f = keys < 256 ? rows::cheapest(n, 0.85, 0.78) : rows::cheapest(n, 0.77, 0.69);
+  else
+    f = keys < 256 ? rows::cheapest(n, 0.92, 0.95) : keys < 1024 ? rows::cheapest(n, 0.74, 0.78) : rows::cheapest(n, 0.76, 0.70);
+  // Less than a round: one small workgroup to a CU, or one large one where the small ones would be two (head dim 128, 64 units 576 x 997
+  // 38.5 us in large ones, 43.9 in small ones; 16 units 1344 x 5136 121 in small ones, 143 in large ones).
+  if (f.team_waves > 1) {
+    const long long small = units * ((n + 127) / 128);
+    if (small <= 256)
+      f = {4, 1};
+    else if (small <= 512 && wide <= 256)
+      f = {8, 1};
+  }
+  return f;
 }
 
 }  // namespace
