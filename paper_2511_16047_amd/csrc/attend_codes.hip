@@ -75,14 +75,12 @@ rows::Form choose(int head_dim, long long units, long long n, long long keys) {
     f = keys < 256 ? rows::cheapest(n, 0.85, 0.78) : rows::cheapest(n, 0.77, 0.69);
   else
     f = keys < 256 ? rows::cheapest(n, 0.92, 0.95) : keys < 1024 ? rows::cheapest(n, 0.74, 0.78) : rows::cheapest(n, 0.76, 0.70);
-  // Less than a round: one small workgroup to a CU, or one large one where the small ones would be two (head dim 128, 64 units 576 x 997
-  // 38.5 us in large ones, 43.9 in small ones; 16 units 1344 x 5136 121 in small ones, 143 in large ones).
+  // Large teams where the fullest CU then has about as few rows (the keys of a tile are read for twice as many).  us, large / small, head
+  // dim 128: 64 units 4096 x 6421 776 / 831, 576 x 997 34 / 38, 80 units 1024 x 2000 (512 rows on a CU or 384) 124 / 114, 16 units 1344 x 5136 (256
+  // or 128) 143 / 121; head dim 64: 40 units 1444 x 3700 73 / 90, 100 units 700 x 1500 (512 or 384) 55 / 50.
   if (f.team_waves > 1) {
-    const long long small = units * ((n + 127) / 128);
-    if (small <= 256)
-      f = {4, 1};
-    else if (small <= 512 && wide <= 256)
-      f = {8, 1};
+    const long long small = (units * ((n + 127) / 128) + 255) / 256 * 128, large = (wide + 255) / 256 * 256;
+    f = (head_dim == 64 || keys >= 1024 ? 0.86 : 0.97) * large <= small ? rows::Form{8, 1} : rows::Form{4, 1};
   }
   return f;
 }
