@@ -33,6 +33,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // the reference of the exponentials may lag behind the maximum by this many powers of two; a lane's 16 new weights then sum to
 // at most kTripSum = 16 * 2^kMaxLag, and a larger sum says that the reference has to move
 constexpr float kMaxLag = 6.0f, kTripSum = 1024.0f;
+// the reference before any key: finite, so that a block whose scores are all -inf (products beyond fp32) weighs nothing
+constexpr float kNoKeys = -0x1.fffffep127f;
 
 // Keys of a unit: n8 rows of codes, located by the segment table, then nx rows of bf16 at a fixed stride.
 struct Keys {
@@ -217,7 +219,7 @@ struct Unit {
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int v = 0; v < 16; ++v) x.o[d][v] = 0.f;
-    x.ref = -INFINITY;
+    x.ref = kNoKeys;
     x.sum = 0.f;
   }
 
@@ -279,7 +281,7 @@ struct Unit {
     }
     return sum;
   }
-  // the largest score of each query, over both lane halves, times c (finite: a block's first key is valid)
+  // the largest score of each query, over both lane halves, times c
   __device__ static __forceinline__ float largest(f32x16& s, float c) {
     settle_mfma(s);
     float m = max3(s[0], s[1], s[2]);
@@ -605,7 +607,7 @@ struct Unit {
 #pragma unroll
       for (int p = 0; p < kTeams; ++p) {
         const float2 y = stat[p * kTeamWaves + rows_of][r];
-        w[p] = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - top);  // (a team without keys)
+        w[p] = __builtin_amdgcn_exp2f(y.x - top);  // (a team without keys: of sums that are 0)
         total = fmaf(w[p], y.y, total);
       }
 #pragma unroll

@@ -205,6 +205,25 @@ def test_flat_and_sharp_scores(sharp):
     _drive([(4, 4), (10, 10), (16, 16)], 1, 4, 64, [(0, 0, True)], sharp=sharp)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,queries", [(2, 5), (16, 60), (150, 100), (150, 256)])
+@pytest.mark.parametrize("first", [32, 48, 64])
+def test_scores_beyond_fp32_weigh_nothing(D, H, queries, first):
+    """A whole scale whose scores are -inf in fp32 (2^100 times -2^100), then keys as if alone: codes, and rows read in place."""
+    for borrow in (False, True):
+        with Cache([(1, first), (1, queries)], 1, H, D, [(0, 0, True)], borrow_unretained=borrow) as c:
+            k0, v0 = (_normal(1, H, first, D, seed=i).bfloat16() for i in (1, 2))
+            q, k, v = (_normal(1, H, queries, D, seed=i).bfloat16() for i in (3, 4, 5))
+            q[..., 0], k0[..., 0], k[..., 0] = 2.0 ** 100, -2.0 ** 100, 0
+            o = torch.empty_like(q)
+            amskv.amskv_append_scale(c.h, 0, 0, k0, v0)
+            amskv.amskv_append_scale(c.h, 0, 1, k, v)
+            amskv.amskv_attend(c.h, 0, 1, q, o)
+            kk, vv = (x.double() if borrow else plain.held(x) for x in (k, v))
+            want, bound = plain.attention(q, kk, vv, 1 / math.sqrt(D))
+            assert bool(((o.double() - want).abs() <= bound).all())
+
+
 def test_many_tokens():
     """Offsets of codes and of a layer's regions beyond 2^31 bytes."""
     B, H, D, T = 24, 16, 128, 45000

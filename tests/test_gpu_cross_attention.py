@@ -94,6 +94,22 @@ def test_shared_between_workgroups(D, Tq, H, Hkv, lengths):
     assert torch.equal(a, c.run())      # the order of the sums is fixed
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,Tq,Tk", [(2, 5, 90), (4, 40, 500), (2, 1, 5000), (80, 100, 300), (80, 500, 300), (200, 70, 200)])
+@pytest.mark.parametrize("start,end", [(0, 40), (0, 64), (33, 75), (32, 80)])
+def test_scores_beyond_fp32_weigh_nothing(D, H, Tq, Tk, start, end):
+    """A channel of 2^100 times -2^100: -inf in fp32, at the first keys, whole blocks and parts of them; the other keys as if alone."""
+    c = Case(H, H, D, Tq, Tk, [Tk])
+    c.q[..., 0] = 2.0 ** 100
+    for x in {id(y): y for y in (c.k, c.kv[0])}.values():
+        x[..., 0] = 0
+        x[:, start:end, :, 0] = -2.0 ** 100
+    out = c.run()
+    k, v = (torch.cat((x[0, :start], x[0, end:])).transpose(0, 1).clone() for x in c.kv)
+    want, bound = plain.attention(c.q[0], k, v, 1 / math.sqrt(D))
+    assert bool(((out[0].double() - want).abs() <= bound).all())
+
+
 @pytest.mark.parametrize("sharp", [0.0, 30.0, 300.0])
 @pytest.mark.parametrize("Tq,Tk", [(1, 3000), (64, 500)])
 def test_flat_and_sharp_scores(sharp, Tq, Tk):
