@@ -95,11 +95,11 @@ class Cross(C.Structure):
 
 _lib = None
 _lookup = None   # torch's raw stream lookup, once asked for
-_append = _attend = None   # set by load_library
+_append = _attend = _append_rotary = _rotate = _cross = None   # set by load_library
 
 
 def load_library() -> C.CDLL:
-    global _lib, _append, _attend
+    global _lib, _append, _attend, _append_rotary, _rotate, _cross
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -175,15 +175,23 @@ def load_library() -> C.CDLL:
         from . import _pycalls
     except ImportError:   # not built for this interpreter: the same calls, 3 us slower each
         _append, _attend = _by_ctypes(lib.amskv_append_scale), _by_ctypes(lib.amskv_attend)
+        _append_rotary = _rotate = _cross = _not_built
     else:
         _append, _attend = _pycalls.append_scale, _pycalls.attend
         _pycalls.bind(C.cast(lib.amskv_append_scale, vp).value, C.cast(lib.amskv_attend, vp).value, _raw_stream_lookup)
+        _append_rotary, _rotate, _cross = _pycalls.append_scale_rotary, _pycalls.rotate, _pycalls.cross_attend
+        _pycalls.bind_operators(*(C.cast(f, vp).value for f in (lib.amskv_append_scale_rotary, lib.amskv_rotate, lib.amskv_cross_attend)),
+                                Rope, Strides, Cross)
     _lib = lib
     return lib
 
 
 def _by_ctypes(call):
     return lambda cache, layer, s, a, b, stream: call(cache, layer, s, _ptr(a), _ptr(b), _stream(stream))
+
+
+def _not_built(*args):
+    raise TypeError
 
 
 def _raw_stream_lookup():
@@ -282,7 +290,7 @@ def amskv_cache_create(layers, heads, head_dim, sides_h, sides_w, batch, dtype, 
     return h.value
 
 
-# The two calls made for every layer and scale go through the extension module (csrc/pycalls.cpp); what it does not know
+# The calls made for every layer and scale go through the extension module (csrc/pycalls.cpp); what it does not know
 # how to pass (it says so before it calls anything) goes through ctypes, as in all other calls.
 _UNUSUAL = (TypeError, AttributeError, OverflowError)
 
@@ -457,14 +465,29 @@ def amskv_rope_table(rope, positions, table, n=None, stream=None):
 def amskv_rotate(rope, dtype, head_dim, batch, heads, tokens, table, table_batch, x, x_strides, out, out_strides, inverse=False,
                  stream=None):
     """x_strides, out_strides: Strides; table_batch: floats from one batch element's table to the next one's (0: shared)."""
-    _check(load_library().amskv_rotate(rope, dtype, head_dim, batch, heads, tokens, _ptr(table), table_batch, int(bool(inverse)), _ptr(x),
-                                       x_strides, _ptr(out), out_strides, _stream(stream)), "amskv_rotate")
+    if _lib is None:
+        load_library()
+    inverse = int(bool(inverse))
+    try:
+        status = _rotate(rope, dtype, head_dim, batch, heads, tokens, table, table_batch, inverse, x, x_strides, out, out_strides, stream)
+    except _UNUSUAL:
+        status = _lib.amskv_rotate(rope, dtype, head_dim, batch, heads, tokens, _ptr(table), table_batch, inverse, _ptr(x), x_strides, _ptr(out),
+                                   out_strides, _stream(stream))
+    if status:
+        _check(status, "amskv_rotate")
 
 
 def amskv_append_scale_rotary(cache, layer, s, rope, table, Q, q_token_stride, Q_out, K, V, stream=None):
     """Q and Q_out may be None (keys only); K is turned in place where the scale is read in place."""
-    _check(load_library().amskv_append_scale_rotary(cache, layer, s, rope, _ptr(table), _ptr(Q), q_token_stride, _ptr(Q_out), _ptr(K),
-                                                    _ptr(V), _stream(stream)), "amskv_append_scale_rotary")
+    if _lib is None:
+        load_library()
+    try:
+        status = _append_rotary(cache, layer, s, rope, table, Q, q_token_stride, Q_out, K, V, stream)
+    except _UNUSUAL:
+        status = _lib.amskv_append_scale_rotary(cache, layer, s, rope, _ptr(table), _ptr(Q), q_token_stride, _ptr(Q_out), _ptr(K), _ptr(V),
+                                                _stream(stream))
+    if status:
+        _check(status, "amskv_append_scale_rotary")
 
 
 def amskv_cross_workspace_bytes(cross) -> int:
@@ -480,5 +503,12 @@ def amskv_cross_attend(cross, Q, K, V, O, lengths=None, offsets=None, workspace=
         workspace_bytes = 0
     elif workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size()
-    _check(load_library().amskv_cross_attend(cross, _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(lengths), _ptr(offsets), _ptr(workspace),
-                                             workspace_bytes, _stream(stream)), "amskv_cross_attend")
+    if _lib is None:
+        load_library()
+    try:
+        status = _cross(cross, Q, K, V, O, lengths, offsets, workspace, workspace_bytes, stream)
+    except _UNUSUAL:
+        status = _lib.amskv_cross_attend(cross, _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(lengths), _ptr(offsets), _ptr(workspace),
+                                         workspace_bytes, _stream(stream))
+    if status:
+        _check(status, "amskv_cross_attend")

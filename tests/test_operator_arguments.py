@@ -1,5 +1,8 @@
 """What the rotary, 8-bit and cross-attention calls refuse, and the host side of the 8-bit cache: no GPU needed."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -221,3 +224,48 @@ def test_eight_bits_refuse_the_analysis():
         assert [x[0] for x in amskv.amskv_cache_layout(h, 0)] == [0, 1]
     finally:
         amskv.amskv_cache_destroy(h)
+
+
+# ---------------------------------------------------------------- how the calls are made
+CALLS = """
+import sys
+if sys.argv[1] == "ctypes":
+    sys.modules["paper_2511_16047_amd._pycalls"] = None      # as where it is not built: importing it raises ImportError
+import ctypes
+import paper_2511_16047_amd as amskv
+rope, st = amskv.Rope(rot_dim=64), amskv.Strides(64, 64, 64)
+cross = amskv.Cross(batch=1, heads=1, kv_heads=1, head_dim=64, dtype=amskv.AMSKV_DTYPE_BF16, q_tokens=1, kv_tokens=1, q=st, k=st, v=st, o=st)
+h = amskv.amskv_cache_create(1, 1, 64, (1,), (1,), 1, amskv.AMSKV_DTYPE_BF16, [(0, 0, True)])
+A = 4096
+calls = [lambda: amskv.amskv_rotate(rope, 1, 64, 1, 1, 1, A, 0, A + 2, st, A, st, stream=0),
+         lambda: amskv.amskv_rotate(None, 1, 64, 1, 1, 1, A, 0, A, st, A, st),
+         lambda: amskv.amskv_rotate(rope, 1, 64, 1, 0, 1, None, 0, None, st, None, st),
+         lambda: amskv.amskv_rotate(rope, 1, 64, 1, 0, 1, None, 0, None, ctypes.pointer(st), None, st),
+         lambda: amskv.amskv_append_scale_rotary(h, 0, 0, rope, A, A, 0, A, A, A),
+         lambda: amskv.amskv_append_scale_rotary(ctypes.c_void_p(h), 0, 0, rope, A, A, 0, A, A, A, stream=ctypes.c_void_p(0).value),
+         lambda: amskv.amskv_append_scale_rotary(None, 0, 0, rope, A, A, 0, A, A, A),
+         lambda: amskv.amskv_append_scale_rotary(h, 0, 0, None, A, A, 0, A, A, A),
+         lambda: amskv.amskv_cross_attend(cross, A, A, A, A + 8),
+         lambda: amskv.amskv_cross_attend(cross, A, A, A, A, lengths=A, offsets=A),
+         lambda: amskv.amskv_cross_attend(None, A, A, A, A),
+         lambda: amskv.amskv_rotate(st, 1, 64, 1, 1, 1, A, 0, A, st, A, st),
+         lambda: amskv.amskv_cross_attend(rope, A, A, A, A)]
+for call in calls:
+    try:
+        call()
+        print("0")
+    except amskv.AmskvError as e:
+        print(e.status)
+    except (TypeError, ctypes.ArgumentError):
+        print("wrong")
+amskv.amskv_cache_destroy(h)
+"""
+
+
+@pytest.mark.parametrize("way", ["extension", "ctypes"])
+def test_both_ways_to_make_a_call(way):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    p = subprocess.run([sys.executable, "-c", CALLS, way], cwd=root, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert p.returncode == 0, p.stdout
+    want = [INVALID, INVALID, 0, 0, NO_MEMORY, NO_MEMORY, INVALID, INVALID, INVALID, INVALID, INVALID, "wrong", "wrong"]
+    assert p.stdout.split() == [str(x) for x in want]
