@@ -12,8 +12,8 @@
 // itself (kTeamWaves 1) takes K straight to registers and has one tile of V in LDS, no barriers; kTeams such waves of a
 // workgroup hold the same rows, take every kTeams-th tile, and their results meet in LDS at the end.
 //
-// Bound: where keys are many the matrix and vector pipes and what power leaves of them (head dim 128, 64 units 4096 x 6421, codes: 845
-// us, 1.02 PFLOP/s, with the staging of codes 13% behind keys that are bf16 rows already; a large library product reaches 1.22;
+// Bound: where keys are many the matrix and vector pipes and what power leaves of them (head dim 128, 64 units 4096 x 6421, codes: 802
+// us, 1.07 PFLOP/s, with the staging of codes 8% behind keys that are bf16 rows already; a large library product reaches 1.22;
 // head dim 64, 3840 units 256 x 530: 190 us, 0.70 PFLOP/s, the exponentials' share is twice as large); where they are few, the
 // latency of arguments, Q, the first tiles and O in turn: 3.5 to 7 us.
 #pragma once
@@ -66,6 +66,7 @@ struct Unit {
   static constexpr int RB = 2 * D, KS = D / 16, DB = D / 32, CPR = D / 8, CP8 = D / 16;
   static constexpr int kTile = kTeamWaves == 8 ? 64 : 32;
   static constexpr int kStages = 4;
+  static constexpr bool kAlone = kTeamWaves == 8 && D == 128;  // 128 KB of LDS
   static constexpr int kThreads = 64 * kTeamWaves;
   static constexpr int kItems = 2 * kTile * CPR / kThreads, kItems8 = kItems / 2;
   // rows from a thread's piece to its next one of the same tensor; with one piece of codes, half of the waves bring K and half V
@@ -325,6 +326,9 @@ struct Unit {
     int block;  // byte offset of the block before (uniform)
     bool rescale, first;
   };
+  // Where a team of eight has the CU to itself (head dim 128), the softmax goes before the score products of the wave it shares a SIMD
+  // with, so that the two come to differ in what they do: 64 units 4096 x 6421 834 -> 802 us.  Waves of two teams on a SIMD hold each
+  // other up instead: teams of four, 80 units 1024 x 2000, 121 -> 134, of eight at head dim 64, 150 units 1100 x 2000, 112 -> 125.
   // `between`, behind the score products, replaces kf by the next block's fragments: they arrive beside the softmax.
   template <bool kFull, class Between>
   __device__ static __forceinline__ void step(Result& x, Behind& w, bf16x8 (&kf)[KS], const bf16x8 (&qf)[KS], const char* lds_all, int ka, int va,
@@ -334,6 +338,7 @@ struct Unit {
     f32x16 s = scores(kf, qf);
     between();
     if constexpr (!kFull) mask(s, n_valid, lane);
+    if constexpr (kAlone) __builtin_amdgcn_s_setprio(1);
     float sum = 0.f;
     bool trip = true;
     const bool first = w.first;
@@ -354,6 +359,7 @@ struct Unit {
       sum = weights(s, w.pf[0], c, ref, 0);
       sum += weights(s, w.pf[1], c, ref, 1);
     }
+    if constexpr (kAlone) __builtin_amdgcn_s_setprio(0);
     x.sum += sum;
     w.first = false;
     w.block = block;
