@@ -64,6 +64,7 @@ __device__ __forceinline__ void settle_mfma(f32x16& acc) { asm volatile("s_nop 1
 template <int D, int kTeamWaves, int kTeams, bool kEight>
 struct Unit {
   static constexpr int RB = 2 * D, KS = D / 16, DB = D / 32, CPR = D / 8, CP8 = D / 16;
+  static_assert(kTeamWaves == 1 || kTeams == 1, "a team of several waves has the workgroup to itself");
   static constexpr int kTile = kTeamWaves == 8 ? 64 : 32;
   static constexpr int kStages = 4;
   static constexpr bool kAlone = kTeamWaves == 8 && D == 128;  // 128 KB of LDS
@@ -320,6 +321,11 @@ struct Unit {
   // wait in pf; the two share no data and stand in one basic block.  Weights are formed against the reference as it is; only
   // when a lane's sum shows that some score lay far above it is the maximum taken and the block's weights formed again, and O^T
   // follows the new reference at the top of the next step.
+  //
+  // Codes at head dim 128: the first block, which has none before it, is no question but weights of 0 for what lies in its
+  // slot, and O^T follows at once: one basic block from K to the weights (64 units 2304 x 3925 363 -> 349 us, 32 units 209 -> 196, 4096 x
+  // 6421 808 -> 784).  Elsewhere walks are short for four products more, and their registers (head dim 64, 256 x 530 188 -> 193).
+  static constexpr bool kOneBlock = D == 128 && kEight;
   struct Behind {
     bf16x8 pf[2];
     float alpha;
@@ -333,7 +339,7 @@ struct Unit {
   template <bool kFull, class Between>
   __device__ static __forceinline__ void step(Result& x, Behind& w, bf16x8 (&kf)[KS], const bf16x8 (&qf)[KS], const char* lds_all, int ka, int va,
                                               int block, int n_valid, float c, int lane, Between between) {
-    if (__builtin_expect(w.rescale, 0)) scale_by(x, w.alpha);
+    if (!kOneBlock && __builtin_expect(w.rescale, 0)) scale_by(x, w.alpha);
     if constexpr (!kAhead) load_k(kf, lds_all, block + ka);
     f32x16 s = scores(kf, qf);
     between();
@@ -341,7 +347,7 @@ struct Unit {
     if constexpr (kAlone) __builtin_amdgcn_s_setprio(1);
     float sum = 0.f;
     bool trip = true;
-    const bool first = w.first;
+    const bool first = !kOneBlock && w.first;
     if (!first) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -356,6 +362,7 @@ struct Unit {
       w.alpha = __builtin_amdgcn_exp2f(x.ref - ref);
       x.ref = ref;
       x.sum *= w.alpha;
+      if constexpr (kOneBlock) scale_by(x, w.alpha);
       sum = weights(s, w.pf[0], c, ref, 0);
       sum += weights(s, w.pf[1], c, ref, 1);
     }
@@ -365,8 +372,7 @@ struct Unit {
     w.block = block;
   }
   __device__ static __forceinline__ void finish(Result& x, const Behind& w, const char* lds_all, int va) {
-    if (w.first) return;
-    if (w.rescale) scale_by(x, w.alpha);
+    if (!kOneBlock && w.rescale) scale_by(x, w.alpha);
 #pragma unroll
     for (int u = 0; u < 2; ++u) add_values(x, w.pf[u], lds_all, w.block + va, u);
   }
@@ -481,37 +487,35 @@ struct Unit {
   __device__ static __forceinline__ void walk(Result& x, const bf16x8 (&qf)[KS], char* lds_all, const Keys& k, const SegTable& seg, int from,
                                               int to, float c, bool active) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int team = wave / kTeamWaves, member = threadIdx.x - team * kThreads;
-    const int lds = team * kTeamLds;
-    int it = from + team;
     if constexpr (kTeamWaves == 1) {
-      alone(x, qf, lds_all + lds, k, seg, it, to, c, lane);
+      alone(x, qf, lds_all + wave * kTeamLds, k, seg, from + wave, to, c, lane);
     } else {
+      const int member = threadIdx.x;
+      int it = from;
       // A ring of four tiles: the one before, whose last V rows may still be to be multiplied (a tile of one block), the one in
       // use, the next one, whose first keys are asked for in the last step of this one, and the one that is being written.  One
       // barrier a tile, behind the score products of its last block.
       const int ka = k_lane(lane), va = v_lane(lane);
       Staged s;
       Aim to_come;
-      const int trips = (to - from + kTeams - 1) / kTeams;  // of every team: the barriers are the workgroup's
       if (it < to) load<kAny>(s, to_come, k, seg, it, member);
       {
         Staged s2;
-        if (it + kTeams < to) load<kAny>(s2, to_come, k, seg, it + kTeams, member);
-        if (it < to) store<kAny>(s, lds_all, lds, k, it, member);
-        if (it + kTeams < to) store<kAny>(s2, lds_all, lds + kStage, k, it + kTeams, member);
+        if (it + 1 < to) load<kAny>(s2, to_come, k, seg, it + 1, member);
+        if (it < to) store<kAny>(s, lds_all, 0, k, it, member);
+        if (it + 1 < to) store<kAny>(s2, lds_all, kStage, k, it + 1, member);
       }
-      if (it + 2 * kTeams < to) load<kAny>(s, to_come, k, seg, it + 2 * kTeams, member);
+      if (it + 2 < to) load<kAny>(s, to_come, k, seg, it + 2, member);
       settle(qf);
       __syncthreads();
-      int slot = lds, next = lds + kStage, after = lds + 2 * kStage, spare = lds + 3 * kStage;
+      int slot = 0, next = kStage, after = 2 * kStage, spare = 3 * kStage;
       bf16x8 kf[KS];
       auto turn_over = [&](auto kind) {
         constexpr Kind kKind = decltype(kind)::value;  // of the tile to bring
         __syncthreads();
-        if (it + 2 * kTeams < to) {
-          store<kAny>(s, lds_all, after, k, it + 2 * kTeams, member);
-          if (it + 3 * kTeams < to) fetch<kKind>(s, to_come, k, it + 3 * kTeams, member);
+        if (it + 2 < to) {
+          store<kAny>(s, lds_all, after, k, it + 2, member);
+          if (it + 3 < to) fetch<kKind>(s, to_come, k, it + 3, member);
         }
       };
       auto next_tile = [&]() {
@@ -520,12 +524,11 @@ struct Unit {
         next = after;
         after = spare;
         spare = freed;
-        it += kTeams;
+        ++it;
       };
-      int n = 0;
       if (!active) {  // a wave without rows only brings its part of the tiles
-        for (; it < to; ++n) {
-          if (it + 3 * kTeams < to) aim<kAny>(to_come, k, seg, it + 3 * kTeams, member);
+        while (it < to) {
+          if (it + 3 < to) aim<kAny>(to_come, k, seg, it + 3, member);
           turn_over(Of<kAny>{});
           next_tile();
         }
@@ -546,16 +549,16 @@ struct Unit {
         // first step of the tile before this one, if that had two blocks.
         auto known = [&](auto kind, int end) {
           constexpr Kind kKind = decltype(kind)::value;
-          for (; it + 3 * kTeams < end; ++n) {
-            aim<kKind>(to_come, k, seg, it + 3 * kTeams, member);
+          while (it + 3 < end) {
+            aim<kKind>(to_come, k, seg, it + 3, member);
             if constexpr (kTile == 64)
               step<true>(x, w, kf, qf, lds_all, ka, va, slot, 32, c, lane, [&]() {
                 if constexpr (kAhead) load_k(kf, lds_all, slot + ka + 32 * RB);
               });
             step<true>(x, w, kf, qf, lds_all, ka, va, slot + (kTile - 32) * RB, 32, c, lane, [&]() {
               if constexpr (kTile == 32) __syncthreads();
-              store<kKind>(s, lds_all, after, k, it + 2 * kTeams, member);
-              fetch<kKind>(s, to_come, k, it + 3 * kTeams, member);
+              store<kKind>(s, lds_all, after, k, it + 2, member);
+              fetch<kKind>(s, to_come, k, it + 3, member);
               if constexpr (kTile == 64) __syncthreads();
               if constexpr (kAhead) load_k(kf, lds_all, next + ka);
             });
@@ -565,8 +568,8 @@ struct Unit {
         const int t8 = min(tiles8(k), to);
         if constexpr (kEight) known(Of<kCodes>{}, t8);
         while (it < to) {
-          if (it - kTeams >= t8 || (it >= t8 && n == 0)) known(Of<kRowsOnly>{}, to);
-          if (it + 3 * kTeams < to) aim<kRowsOnly>(to_come, k, seg, it + 3 * kTeams, member);  // (codes: all brought above)
+          if (it - 1 >= t8 || (it >= t8 && it == from)) known(Of<kRowsOnly>{}, to);
+          if (it + 3 < to) aim<kRowsOnly>(to_come, k, seg, it + 3, member);  // (codes: all brought above)
           int left = valid(k, it), done = 0;
           if (kTile == 64 && left > 32) {
             step<false>(x, w, kf, qf, lds_all, ka, va, slot, 32, c, lane, [&]() {
@@ -576,28 +579,24 @@ struct Unit {
           }
           step<false>(x, w, kf, qf, lds_all, ka, va, slot + done * RB, left - done, c, lane, [&]() {
             turn_over(Of<kRowsOnly>{});
-            if (kAhead && it + kTeams < to) load_k(kf, lds_all, next + ka);
+            if (kAhead && it + 1 < to) load_k(kf, lds_all, next + ka);
           });
           next_tile();
-          ++n;
         }
         finish(x, w, lds_all, va);
       }
-      if (kTeams > 1 && n < trips) __syncthreads();
-      if constexpr (kTeams > 1) __syncthreads();  // the ring is parked into next
     }
   }
 
-  // The results of all teams.  Afterwards a wave holds, of its 32 rows, chunks i (i % kTeams == team) of 8 channels: o[i/4][4 (i%4)
+  // The results of all teams.  Afterwards a wave holds, of its 32 rows, chunks i (i % kTeams == wave) of 8 channels: o[i/4][4 (i%4)
   // + ..]; ref, sum are the rows' (over all keys).  Every wave of the workgroup calls this.
   __device__ static __forceinline__ void meet(Result& x, char* lds_all) {
     x.sum += __shfl_xor(x.sum, 32, 64);
     if constexpr (kTeams > 1) {
-      __shared__ float2 stat[kTeams * kTeamWaves][32];
+      __shared__ float2 stat[kTeams][32];
       const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 31;
-      const int team = wave / kTeamWaves, rows_of = wave - team * kTeamWaves;
-      constexpr int kPark = 32 * D * 4;
-      if constexpr (kTeamWaves == 1) __builtin_amdgcn_wave_barrier();  // its own tile; a team's last barrier was behind its last tile
+      constexpr int kPark = 32 * D * 4;  // where the wave's own tile was
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int i = 0; i < 4 * DB; ++i) {
         f32x4 y;
@@ -609,20 +608,20 @@ struct Unit {
       __syncthreads();
       float top = -INFINITY, total = 0.f, w[kTeams];
 #pragma unroll
-      for (int p = 0; p < kTeams; ++p) top = fmaxf(top, stat[p * kTeamWaves + rows_of][r].x);
+      for (int p = 0; p < kTeams; ++p) top = fmaxf(top, stat[p][r].x);
 #pragma unroll
       for (int p = 0; p < kTeams; ++p) {
-        const float2 y = stat[p * kTeamWaves + rows_of][r];
+        const float2 y = stat[p][r];
         w[p] = __builtin_amdgcn_exp2f(y.x - top);  // (a team without keys: of sums that are 0)
         total = fmaf(w[p], y.y, total);
       }
 #pragma unroll
       for (int i0 = 0; i0 < 4 * DB; i0 += kTeams) {
-        const char* from = lds_all + rows_of * kPark + (i0 + team) * 1024 + lane * 16;
+        const char* from = lds_all + (i0 + wave) * 1024 + lane * 16;
         f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int p = 0; p < kTeams; ++p) {
-          const f32x4 z = *reinterpret_cast<const f32x4*>(from + p * kTeamWaves * kPark);
+          const f32x4 z = *reinterpret_cast<const f32x4*>(from + p * kPark);
 #pragma unroll
           for (int e = 0; e < 4; ++e) y[e] = fmaf(w[p], z[e], y[e]);
         }
@@ -658,13 +657,12 @@ struct Unit {
           if (stored) *reinterpret_cast<u32x4*>(dst + 32 * d + 16 * k + 8 * h) = w;
         }
     } else {
-      const int team = wave / kTeamWaves;
 #pragma unroll
       for (int i0 = 0; i0 < 4 * DB; i0 += kTeams) {
         bf16x4 w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = (__bf16)(x.o[i0 >> 2][4 * (i0 & 3) + e] * inv);
-        if (stored) *reinterpret_cast<bf16x4*>(dst + 8 * (i0 + team) + 4 * h) = w;
+        if (stored) *reinterpret_cast<bf16x4*>(dst + 8 * (i0 + wave) + 4 * h) = w;
       }
     }
   }
@@ -672,13 +670,13 @@ struct Unit {
   // ... as fp32, not divided, at `dst`
   __device__ static __forceinline__ void put_partial(const Result& x, float* dst) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
-    const int team = kTeams == 1 ? 0 : wave / kTeamWaves;
+    const int part = kTeams == 1 ? 0 : wave;
 #pragma unroll
     for (int i0 = 0; i0 < 4 * DB; i0 += kTeams) {
       f32x4 y;
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = x.o[i0 >> 2][4 * (i0 & 3) + e];
-      *reinterpret_cast<f32x4*>(dst + 8 * (i0 + team) + 4 * h) = y;
+      *reinterpret_cast<f32x4*>(dst + 8 * (i0 + part) + 4 * h) = y;
     }
   }
 };
