@@ -237,6 +237,25 @@ def test_far_rows():
         assert bool(((out[b].double() - want).abs() <= bound).all())
 
 
+def test_far_queries():
+    """The most queries a head may have, of eight heads that share one: Q and O beyond 2^32 bytes."""
+    H, D, Tq, Tk = 8, 64, 1 << 22, 33
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    q = torch.empty(1, H, Tq, D, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    k, v = (_normal(1, Tk, 1, D, seed=i).bfloat16() for i in (1, 2))
+    assert q.numel() * 2 >= 2 ** 32
+    out = torch.full_like(q, 9.0)
+    qs, st = amskv.Strides(0, Tq * D, D), amskv.Strides(0, 0, D)
+    x = amskv.Cross(batch=1, heads=H, kv_heads=1, head_dim=D, dtype=amskv.AMSKV_DTYPE_BF16, q_tokens=Tq, kv_tokens=Tk, q=qs, k=st, v=st, o=qs)
+    amskv.amskv_cross_attend(x, q, k, v, out)
+    assert not bool((out[:, :, ::4097] == 9.0).all(dim=-1).any())
+    for h in (0, 3, H - 1):
+        for at in (0, 2 ** 21 - 50, Tq - 100):
+            want, bound = plain.attention(q[0, h, at:at + 100], k[0, :, 0], v[0, :, 0], 1 / math.sqrt(D))
+            assert bool(((out[0, h, at:at + 100].double() - want).abs() <= bound).all())
+
+
 def test_captured_and_replayed():
     """Lengths are read when the graph runs, not when it is captured; eager calls in between use a workspace of their own."""
     for Tq, Tk in ((70, 200), (1, 4000)):

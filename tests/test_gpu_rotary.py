@@ -102,6 +102,20 @@ def test_many_rows(B, H, T):
     assert torch.equal(out, plain.turn(x.float(), tab, "interleaved").bfloat16())
 
 
+def test_far_rows():
+    """A tensor beyond 2^32 bytes, turned in place, with the most tokens it may have."""
+    H, T, D = 9, 1 << 22, 64
+    rope = amskv.Rope(rot_dim=16)
+    tab = _table(rope, torch.arange(T, dtype=torch.float64, device="cuda")[:, None])
+    x = torch.empty(1, H, T, D, dtype=torch.bfloat16, device="cuda").fill_(0.5)
+    x[..., :16] = _normal(16, seed=1).bfloat16()
+    want = plain.turn(x[0, 0].float(), tab, "half").bfloat16()
+    xs = amskv.Strides(0, T * D, D)
+    amskv.amskv_rotate(rope, amskv.AMSKV_DTYPE_BF16, D, 1, H, T, tab, 0, x, xs, x, xs)
+    for h in range(H):
+        assert torch.equal(x[0, h], want)
+
+
 def test_a_head_for_all():
     """A tensor that repeats is read with stride 0."""
     B, H, T, D = 2, 6, 20, 64
