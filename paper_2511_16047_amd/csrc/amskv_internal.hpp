@@ -281,9 +281,13 @@ hipError_t launch_theta_flag(const float* totals_dev, int heads, double n_tok, f
 hipError_t launch_density_total(const float* partial_ws, int batch, int heads, int n_qblk, int n_groups, float* out_dev,
                                 hipStream_t st);
 
-// ---- rotary positions and the 8-bit cache.  Weak: a build of the host layer by itself need not have them (a cache without
-// either never calls them).
-#define AMSKV_WEAK __attribute__((weak))
+// ---- rotary positions and the 8-bit cache.  A build of the host layer by itself, without the device compiler (a test of it on the
+// CPU), need not have them: a cache without either never calls them.  In the library they are as all others.
+#if defined(__HIPCC__)
+#define AMSKV_OPTIONAL
+#else
+#define AMSKV_OPTIONAL __attribute__((weak))
+#endif
 
 // A layer's K and V in 8 bits: codes [BH][cap][D], and the power of two that every 16 tokens share, [BH][cap / 16] (as fp32: ready
 // for the instruction that turns codes into numbers); cap and every slot are multiples of 16 tokens.
@@ -309,17 +313,17 @@ struct Take {
   bool eight_bits;
   const MoveList* moves;            // eight_bits: survivors that slide to their new places first (launch_move_codes), or null
 };
-hipError_t launch_take(const Take& t, hipStream_t st) AMSKV_WEAK;
+hipError_t launch_take(const Take& t, hipStream_t st) AMSKV_OPTIONAL;
 // The survivors of a compaction slide to their new places (mv in tokens, whole blocks of 16).
-hipError_t launch_move_codes(const Codes& c, int bh, int head_dim, int64_t cap_tokens, const MoveList& mv, hipStream_t st) AMSKV_WEAK;
+hipError_t launch_move_codes(const Codes& c, int bh, int head_dim, int64_t cap_tokens, const MoveList& mv, hipStream_t st) AMSKV_OPTIONAL;
 // As launch_export, the values of the codes as bf16.
 hipError_t launch_export_codes(const Codes& c, void* k_out, void* v_out, int bh, int head_dim, int64_t cap_tokens, const SegTable& seg,
-                               const ExtKV& ext, const RowMap& ext_map, int heads, hipStream_t st) AMSKV_WEAK;
+                               const ExtKV& ext, const RowMap& ext_map, int heads, hipStream_t st) AMSKV_OPTIONAL;
 hipError_t launch_attend_codes(const void* q, void* o, const Codes& c, int bh, int t_q, int head_dim, int64_t cap_tokens,
-                               const SegTable& seg, const ExtKV& ext, const CallerIo& io, float softmax_scale, hipStream_t st) AMSKV_WEAK;
+                               const SegTable& seg, const ExtKV& ext, const CallerIo& io, float softmax_scale, hipStream_t st) AMSKV_OPTIONAL;
 
 hipError_t launch_rope_table(const double* frequency, int pairs, int axes, double amplitude, const double* positions, int64_t n,
-                             float* table, hipStream_t st) AMSKV_WEAK;
+                             float* table, hipStream_t st) AMSKV_OPTIONAL;
 
 // Cross attention: K and V rows of the caller's, where each batch element's begin and how many there are left to the device.
 struct CrossCall {
@@ -333,8 +337,8 @@ struct CrossCall {
   float* workspace;                   // null: not split
 };
 // Bytes of the workspace that a call of this shape uses (0: none).
-uint64_t cross_workspace_bytes(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) AMSKV_WEAK;
-hipError_t launch_cross(const CrossCall& c, hipStream_t st) AMSKV_WEAK;
+uint64_t cross_workspace_bytes(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) AMSKV_OPTIONAL;
+hipError_t launch_cross(const CrossCall& c, hipStream_t st) AMSKV_OPTIONAL;
 
 // What is wrong with a rotary description for rows of head_dim channels: AMSKV_OK or AMSKV_ERR_INVALID_ARG.
 inline int check_turn(const amskv_rope* r, int head_dim) {
