@@ -685,18 +685,6 @@ struct Unit {
   }
 };
 
-// Which form a launch takes: waves to a team, teams to a workgroup.
-struct Form {
-  int team_waves, teams;
-};
-
-// Of waves by themselves and teams of four and eight for n rows: the fewest rows, of whole blocks of 32, whole 128 and whole 256, where a
-// row of a team costs four (eight) of a lone wave's.
-inline Form cheapest(long long n, double four, double eight) {
-  const double alone = (double)((n + 31) / 32 * 32), team4 = four * (double)((n + 127) / 128 * 128), team8 = eight * (double)((n + 255) / 256 * 256);
-  return alone <= team4 && alone <= team8 ? Form{1, 1} : team4 <= team8 ? Form{4, 1} : Form{8, 1};
-}
-
 }  // namespace rows
 }  // namespace amskv
 #endif

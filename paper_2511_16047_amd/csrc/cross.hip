@@ -8,9 +8,8 @@
 // hides (8 x 16 heads, 4096 x up to 512, head dim 128: 120 us, 0.57 PFLOP/s and 2.4 TB/s).
 // A launch over few rows and many states does not fill the chip with one workgroup to 32 or 128 rows; then `splits` workgroups
 // take equal runs of key tiles each, leave their sums unnormalised in the workspace, and a second launch puts them together.
-#include <cmath>
-
 #include "attend_rows.hpp"
+#include "attend_rows_choice.hpp"
 
 namespace amskv {
 namespace {
@@ -27,9 +26,6 @@ struct CrossArgs {
   float scale_log2e;
   int kv_heads, group, q_tokens, kv_tokens, n_units, row_tiles, splits, n_whole;
 };
-
-// what a workgroup leaves for the second launch: O^T of its rows, then (reference, sum) of each
-constexpr int partial_floats(int rows, int head_dim) { return rows * (head_dim + 2); }
 
 // the states of batch element b: first row (of the packed axis) and how many; whatever the device arrays hold, rows exist
 __device__ __forceinline__ int states(const CrossArgs& a, unsigned b, long long& first) {
@@ -86,7 +82,7 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
     U::put(x, reinterpret_cast<__bf16*>(a.o + row_at(a.o_map, late)), active && base + (late & 31) < n_rows);
     return;
   }
-  float* mine = a.workspace + (((long long)at.bh * a.row_tiles + tile) * a.splits + split) * partial_floats(U::kRows, D);
+  float* mine = a.workspace + (((long long)at.bh * a.row_tiles + tile) * a.splits + split) * rows::partial_floats(U::kRows, D);
   const int local = 32 * (wave % kTeamWaves) + (late & 31);
   if (active) U::put_partial(x, mine + local * D);
   if (wave < kTeamWaves && late < 32) *reinterpret_cast<float2*>(mine + U::kRows * D + 2 * local) = make_float2(x.ref, x.sum);
@@ -101,7 +97,7 @@ __global__ __launch_bounds__(256) void cross_meet_kernel(CrossArgs a, int rows_o
   if (unit >= a.n_units) return;
   const int rest = (int)(i - unit * per_unit), row = rest / (D / 4), c = rest % (D / 4);
   const int tile = row / rows_of_tile, local = row - tile * rows_of_tile;
-  const float* from = a.workspace + (unit * a.row_tiles + tile) * a.splits * (long long)partial_floats(rows_of_tile, D);
+  const float* from = a.workspace + (unit * a.row_tiles + tile) * a.splits * (long long)rows::partial_floats(rows_of_tile, D);
   // (a few runs at a time, their loads under way together)
   constexpr int kAtOnce = 8;
   float top = -INFINITY, total = 0.f;
@@ -111,7 +107,7 @@ __global__ __launch_bounds__(256) void cross_meet_kernel(CrossArgs a, int rows_o
     rows::f32x4 y[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      const float* p = from + (long long)min(s0 + i, a.splits - 1) * partial_floats(rows_of_tile, D);
+      const float* p = from + (long long)min(s0 + i, a.splits - 1) * rows::partial_floats(rows_of_tile, D);
       st[i] = *reinterpret_cast<const float2*>(p + rows_of_tile * D + 2 * local);
       y[i] = *reinterpret_cast<const rows::f32x4*>(p + local * D + 4 * c);
       if (s0 + i >= a.splits) st[i].x = -INFINITY;
@@ -141,60 +137,6 @@ __global__ __launch_bounds__(256) void cross_meet_kernel(CrossArgs a, int rows_o
   *reinterpret_cast<rows::bf16x4*>(a.o + b * a.o_map.batch + ((long long)g * a.group + head) * a.o_map.head + token * a.o_map.tok + 8 * c) = w;
 }
 
-// How a call is divided: the form, and workgroups that share the keys of a row tile.
-struct Division {
-  int team_waves, teams, splits;
-};
-// `units` (b, kv head) of `n` query rows over up to `keys` states.  Waves by themselves where there are at most 96 states and not
-// many rows; few waves of 32 rows: four to a row block; otherwise teams that read K and V once for 128 or 256 rows where that
-// pays for the rows they are padded to -- a row of a team costs 0.58 to 0.95 of a lone wave's, less the longer the keys, as K
-// and V are better brought by a team, whole rows at a time, than by lanes that follow a key each; for the same reason up to 64
-// rows too where K and V are large.  Teams of eight at head dim 128 are left out: 6% shorter at best, mostly longer.  us a launch, <1,1> / <1,4> / <4,1> / <8,1> (16 heads, batch B).  Head dim 64: B 8, 36 x 77 4.9 / 4.9 / 5.4 /
-// 5.2, B 32 256 x 512 32 / 39 / 24 / 27, 1024 x 512 100 / 128 / 67 / 67, 589 units 1 x 1999 62 / 57 / 54 / 69, 481 units 2432 x 231 231 / 300 / 162 / 164, 230
-// units 358 x 19 7.7 / 14.9 / 7.5 / 8.4.  Head dim 128: B 2 256 x 64 5.3 / 6.2 / 6.7 / 8.2, B 8 4096 x 77 72 / 166 / 65 / 79, 146 units 272 x 2063 127 / 126 /
-// 77 / 121, 10 units 1053 x 4446 124 / 90 / 47 / 58, 722 units 424 x 10 35 / 94 / 37 / 47, 12 units 2812 x 1530 81 / 84 / 53 / 50.  (247 shapes, 110 of them
-// drawn; the choice takes 1.008 of the best of those on average.)
-Division divide(int head_dim, long long units, long long n, int keys) {
-  const long long waves = units * ((n + 31) / 32), wide = units * ((n + 255) / 256), blocks = ((long long)keys + 31) / 32;
-  const long long bytes = units * keys * head_dim * 4;
-  rows::Form f;
-  if (blocks <= 3 && (n <= 64 || waves <= 1024))
-    f = {1, 1};
-  else if (n <= 64 && blocks >= 64 && bytes >= (head_dim == 64 ? 400000000 : 250000000))
-    f = head_dim == 64 ? rows::Form{8, 1} : rows::Form{4, 1};
-  else if (head_dim == 64 ? waves <= 512 || (waves <= 1024 && wide <= 128) : waves <= 256 || (waves <= 512 && n <= 64))
-    f = {1, 4};
-  else if (head_dim == 64)
-    f = keys <= 96 ? rows::cheapest(n, 0.92, 0.95) : keys < 256 ? rows::cheapest(n, 0.85, 0.81) : rows::cheapest(n, 0.73, 0.66);
-  else
-    f = rows::cheapest(n, keys <= 32 ? 1.0 : keys <= 128 ? 0.88 : 0.58, HUGE_VAL);  // (no eight waves: one workgroup to a CU)
-  Division d{f.team_waves, f.teams, 1};
-  const int tile = d.team_waves == 8 ? 64 : 32;
-  const long long groups = units * ((n + 32 * d.team_waves - 1) / (32 * d.team_waves));
-  const int trips = (int)(((long long)keys + tile * d.teams - 1) / (tile * d.teams));
-  // The keys of a row tile are shared by `splits` workgroups, each with 4 tiles for a team at least and 2 to a CU at most, where
-  // that is estimated to be shorter (us): a tile takes 0.6 (a block of 32 keys at head dim 128 by one wave 1.1, a tile of 64 by
-  // eight waves 0.8), longer where a CU has several workgroups, beside what K and V take to arrive; splitting costs a launch and the
-  // way of its sums through the workspace.  us with / without:  Head dim 64: 8 x 1 query x 2000
-  // states 8.4 / 12.2, 16000 12.7 / 71.5, 64 x 1 x 16000 49 / 110, 150 x 128 x 2000 31 / 40, 16000 174 / 302 (with 4 instead of 3 to a row tile
-  // 167, with 2 195).  Head dim 128: 16 x 256 x 4000 29 / 40, 230 row tiles of 128 x 16000 270 / 303, x 2000 not split 43 (in two 55).
-  if (groups >= 256 || trips < 8) return d;
-  const double tile_us = d.team_waves == 8 ? 0.8 : d.team_waves == 1 && head_dim == 128 ? 1.1 : 0.6, arrive = bytes / 5.5e6;
-  const double share = d.team_waves == 1 ? 1.15 : d.team_waves == 4 ? 0.65 : 0.75;
-  const double sums = 2e-6 / 2.5 * groups * partial_floats(32 * d.team_waves, head_dim) * 4;
-  double least = 0;
-  for (int s = 1; s <= min((512 + groups - 1) / groups, trips / 4ll); s += s < 16 ? 1 : s / 8) {
-    const long long per_cu = (groups * s + 255) / 256;
-    const double walk = (double)trips / s * tile_us * (per_cu == 1 ? 1.0 : fmax(1.0, share * per_cu));
-    const double us = std::hypot(walk, arrive) + (s == 1 ? 0 : 3 + 0.1 * s + sums * s);
-    if (s == 1 || us < least) {
-      least = us;
-      d.splits = s;
-    }
-  }
-  return d;
-}
-
 template <int D, int kTeamWaves, int kTeams, int kMinWavesPerSimd>
 hipError_t go(CrossArgs& a, hipStream_t st) {
   const int n_rows = a.group * a.q_tokens;
@@ -215,10 +157,10 @@ hipError_t go(CrossArgs& a, hipStream_t st) {
 uint64_t cross_workspace_bytes(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) {
   const int units = batch * kv_heads, rows = heads / kv_heads * q_tokens;
   if (units == 0 || rows == 0 || kv_tokens == 0) return 0;
-  const Division d = divide(head_dim, units, rows, kv_tokens);
+  const rows::Division d = rows::divide(head_dim, units, rows, kv_tokens);
   if (d.splits == 1) return 0;
   const uint64_t row_tiles = (rows + 32 * d.team_waves - 1) / (32 * d.team_waves);
-  return (uint64_t)units * row_tiles * d.splits * partial_floats(32 * d.team_waves, head_dim) * sizeof(float);
+  return (uint64_t)units * row_tiles * d.splits * rows::partial_floats(32 * d.team_waves, head_dim) * sizeof(float);
 }
 
 hipError_t launch_cross(const CrossCall& c, hipStream_t st) {
@@ -242,7 +184,7 @@ hipError_t launch_cross(const CrossCall& c, hipStream_t st) {
   a.kv_tokens = c.kv_tokens;
   a.n_units = c.batch * c.kv_heads;
   if (a.n_units == 0 || a.group * a.q_tokens == 0) return hipSuccess;
-  const Division d = divide(c.head_dim, a.n_units, a.group * a.q_tokens, a.kv_tokens);
+  const rows::Division d = rows::divide(c.head_dim, a.n_units, a.group * a.q_tokens, a.kv_tokens);
   a.splits = a.workspace ? d.splits : 1;
   if (c.head_dim == 64) {
     if (d.team_waves == 1) return d.teams == 1 ? go<64, 1, 1, 4>(a, st) : go<64, 1, 4, 4>(a, st);
