@@ -469,7 +469,8 @@ int32_t amskv_append_scale_rotary(amskv_cache* cache, int32_t layer, int32_t s, 
  *                                        kv_rows rows (k.token, v.token; the batch strides are not used); b has offsets[b+1] -
  *                                        offsets[b] states, of which what goes beyond kv_tokens or kv_rows is left out
  * The token strides of K and V are below 2^23 elements; batch * heads is up to 2^24, q_tokens up to 2^22 (2^26 with the heads
- * that share a kv head), kv_tokens up to 2^26.  O overlaps none of the others.
+ * that share a kv head), kv_tokens up to 2^26, and blocks of 32 queries -- of all heads that share a kv head together -- over all
+ * (b, kv head) up to 2^26 - 8.  O overlaps none of the others.
  * bf16: finite Q, K and V, fp32 accumulation and softmax, P rounded to bf16 before the second product, O rounded to bf16. */
 typedef struct {
   int32_t batch, heads, kv_heads; /* heads a multiple of kv_heads                            */

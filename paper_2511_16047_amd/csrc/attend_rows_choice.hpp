@@ -84,6 +84,8 @@ inline Division divide(int head_dim, long long units, long long n, int keys) {
     f = keys <= 96 ? cheapest(n, 0.92, 0.95) : keys < 256 ? cheapest(n, 0.85, 0.81) : cheapest(n, 0.73, 0.66);
   else
     f = cheapest(n, keys <= 32 ? 1.0 : keys <= 128 ? 0.88 : 0.58, HUGE_VAL);  // (no eight waves: one workgroup to a CU)
+  // (a launch has fewer than 2^32 threads; waves by themselves have the fewest, 64 to 32 rows, and the caller sees to it that they fit)
+  if ((units * ((n + 32 * f.team_waves - 1) / (32 * f.team_waves)) + 7) * 64 * f.team_waves * f.teams > 0xffffffffll) f = {1, 1};
   Division d{f.team_waves, f.teams, 1};
   const int tile = d.team_waves == 8 ? 64 : 32;
   const long long groups = units * ((n + 32 * d.team_waves - 1) / (32 * d.team_waves));

@@ -49,7 +49,12 @@ int check_cross(const amskv_cross* x) {
   // grids count (b, head, block of rows) in 32 bits, rows of a unit too
   if ((int64_t)x->batch * x->heads > (1 << 24) || x->q_tokens > (1 << 22) || x->kv_tokens > (1 << 26)) return AMSKV_ERR_INVALID_ARG;
   if ((int64_t)x->batch * x->heads * x->q_tokens > ((int64_t)1 << 32)) return AMSKV_ERR_INVALID_ARG;
-  if (x->heads > 0 && (int64_t)(x->heads / x->kv_heads) * x->q_tokens > (1 << 26)) return AMSKV_ERR_INVALID_ARG;
+  if (x->heads > 0) {
+    const int64_t rows = (int64_t)(x->heads / x->kv_heads) * x->q_tokens;
+    if (rows > (1 << 26)) return AMSKV_ERR_INVALID_ARG;
+    // a launch has fewer than 2^32 threads, 64 of them to 32 rows; a grid is rounded up by 7 at most
+    if ((int64_t)x->batch * x->kv_heads * ((rows + 31) / 32) > (1 << 26) - 8) return AMSKV_ERR_INVALID_ARG;
+  }
   return AMSKV_OK;
 }
 

@@ -110,3 +110,16 @@ def test_workspaces_hold_what_a_division_writes(choose):
         assert splits == 1 or (units * tiles < 256 and splits * 4 * (64 if waves == 8 else 32) * teams <= keys + 63)
         split += splits > 1
     assert split > 100
+
+
+# the most (b, kv head) there may be, with the rows of a unit that memory has room for: calls that the checks let through
+MOST = [(d, units, n, keys) for d in (64, 128) for units in (1 << 22, (1 << 23) - 1, 1 << 23, (1 << 24) - 1, 1 << 24) for n in (1, 32, 64, 96, 120)
+        for keys in (1, 33, 96, 300, 2017, 2048, 1 << 26) if units * ((n + 31) // 32) <= (1 << 26) - 8] + [(64, 1, 1 << 26, 70), (128, 2, 1 << 26, 3000)]
+
+
+def test_launches_stay_below_the_threads_a_grid_may_have(choose):
+    """2^32 along an axis."""
+    for x, (waves, teams, splits) in zip(MOST, choose(1, MOST)):
+        d, units, n, keys = x
+        groups = (units * -(-n // (32 * waves)) + 7) * splits
+        assert groups * 64 * waves * teams < 1 << 32, x
