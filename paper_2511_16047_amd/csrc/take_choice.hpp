@@ -1,0 +1,17 @@
+// How the launches of take_kernels.hip that move an 8-bit cache's codes are divided: plain host code.  A launch has fewer than 2^32
+// threads along an axis.
+#pragma once
+
+namespace amskv {
+
+constexpr long long kMostThreads = 0xffffffffll;
+
+// Threads of a workgroup, one to a (b,h) and tensor, that slides `blocks` blocks of 16 tokens: the smallest that takes them in one pass
+// where there are many (b,h), else a large one; smaller ones again where the (b,h) are so many that large ones are no launch.
+inline int move_threads(long long blocks, int head_dim, int bh) {
+  int threads = blocks * head_dim <= 1024 && bh >= 128 ? 256 : 1024;
+  while ((long long)bh * threads > kMostThreads) threads /= 2;   // (bh up to 2^24: 128 and more)
+  return threads;
+}
+
+}  // namespace amskv

@@ -18,6 +18,7 @@
 // dim 128 59 us (270 MB); K and V of 3840 (b,h), 169 tokens, head dim 64, to codes 48.6 us (249 MB); Q and K turned, K and V to codes,
 // 960 (b,h), 256 tokens 31.8 us (157 MB).  Launch and the latency of arguments, rows and stores at the coarse ones: 2.4 to 5 us.
 #include "codes.hpp"
+#include "take_choice.hpp"
 
 namespace amskv {
 namespace {
@@ -430,7 +431,7 @@ hipError_t launch_rope_table(const double* frequency, int pairs, int axes, doubl
 hipError_t launch_move_codes(const Codes& c, int bh, int head_dim, int64_t cap_tokens, const MoveList& mv, hipStream_t st) {
   const BlockList list = block_list(mv);
   if (list.total == 0) return hipSuccess;
-  const int threads = (long long)list.total * head_dim <= 1024 && bh >= 128 ? 256 : 1024;
+  const int threads = move_threads(list.total, head_dim, bh);
   auto kernel = head_dim == 64 ? move_codes_kernel<64> : move_codes_kernel<128>;
   hipLaunchKernelGGL(kernel, dim3(bh, 2), dim3(threads), 0, st, c, (long long)cap_tokens, list);
   return hipGetLastError();

@@ -30,3 +30,42 @@ def test_cross_attention_of_very_many_units(B, Tk):
     for b in (0, 1, B // 2 - 1, B // 2, B - 1):
         want, bound = plain.attention(q[b], k.transpose(0, 1), v.transpose(0, 1), 1 / math.sqrt(D))
         assert bool(((out[b].double() - want).abs() <= bound).all())
+
+
+class Cache8:
+    """One layer of 8 bits over scales of single rows."""
+
+    def __init__(self, B, H, D, tokens, pol, **kw):
+        args = (1, H, D, (1,) * len(tokens), tokens, B, amskv.AMSKV_DTYPE_BF16_KV8, [pol])
+        self.arena = torch.empty(amskv.amskv_cache_required_bytes(*args, **kw), dtype=torch.uint8, device="cuda").fill_(0xFF)
+        self.h = amskv.amskv_cache_create(*args, arena=self.arena, **kw)
+
+    def __enter__(self):
+        return self.h
+
+    def __exit__(self, *a):
+        torch.cuda.synchronize()
+        amskv.amskv_cache_destroy(self.h)
+
+
+def test_compaction_of_very_many_units():
+    """2^22 (b,h): the scale that stays slides to the front, step after step."""
+    B, H, D, tokens = 1 << 18, 16, 64, (1, 1, 2, 1)
+    some = [slice(0, 3), slice(B // 2 - 2, B // 2 + 2), slice(B - 3, B)]
+    with Cache8(B, H, D, tokens, (0, 1, False)) as h:
+        kept = []
+        for s, t in enumerate(tokens):
+            q, k, v = (_normal(B, H, t, D, seed=10 * s + i) for i in range(3))
+            o = torch.full_like(q, 9.0)
+            amskv.amskv_append_scale(h, 0, s, k, v)
+            amskv.amskv_attend(h, 0, s, q, o)
+            kept = kept[-1:] + [[(plain.held(k[x]), plain.held(v[x])) for x in some]]
+            n = sum(tokens[s - 1: s + 1]) if s else tokens[0]
+            ko, vo = (torch.full((B, H, n, D), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            amskv.amskv_cache_export(h, 0, ko, vo)
+            for i, x in enumerate(some):
+                kk, vv = (torch.cat([step[i][j] for step in kept], dim=2) for j in range(2))
+                assert torch.equal(ko[x].double(), kk) and torch.equal(vo[x].double(), vv)
+                want, bound = plain.attention(q[x], kk, vv, 1 / math.sqrt(D))
+                assert bool(((o[x].double() - want).abs() <= bound).all())
+            assert not bool((ko == 9.0).all(dim=-1).any()) and not bool((vo == 9.0).all(dim=-1).any())

@@ -1,0 +1,50 @@
+"""The rules that divide the launches over an 8-bit cache's codes (csrc/take_choice.hpp, the code the dispatch runs) built for the CPU."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+PROGRAM = r"""
+#include <cstdio>
+#include "take_choice.hpp"
+using namespace amskv;
+int main() {
+  char what;
+  long long a, b, c;
+  while (std::scanf(" %c %lld %lld %lld", &what, &a, &b, &c) == 4)
+    if (what == 'm') std::printf("%d\n", move_threads(a, (int)b, (int)c));
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def ask(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("no host compiler")
+    d = tmp_path_factory.mktemp("choice")
+    src, exe = str(d / "choice.cpp"), str(d / "choice")
+    with open(src, "w") as f:
+        f.write(PROGRAM)
+    b = subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-fsanitize=undefined", "-fno-sanitize-recover=all",
+                        "-I" + os.path.join(ROOT, "paper_2511_16047_amd", "csrc"), src, "-o", exe],
+                       stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert b.returncode == 0, b.stdout[-4000:]
+
+    def run(what, launches):
+        r = subprocess.run([exe], input="".join("%s %d %d %d\n" % (what, *x) for x in launches), stdout=subprocess.PIPE, text=True, timeout=120, check=True)
+        return [tuple(int(y) for y in line.split()) for line in r.stdout.splitlines()]
+
+    return run
+
+
+MANY = (1, 100, 128, 4000, (1 << 22) - 1, 1 << 22, 1 << 23, (1 << 24) - 1, 1 << 24)    # (b,h)
+
+
+def test_a_slide_is_a_launch(ask):
+    """Whole waves, as many as a workgroup may have, fewer than 2^32 threads in all."""
+    launches = [(blocks, d, bh) for blocks in (1, 8, 16, 17, 300) for d in (64, 128) for bh in MANY]
+    for (blocks, d, bh), (threads,) in zip(launches, ask("m", launches)):
+        assert threads in (128, 256, 512, 1024) and threads * bh < 1 << 32
+        assert bh >= 1 << 22 or threads == (256 if blocks * d <= 1024 and bh >= 128 else 1024)
