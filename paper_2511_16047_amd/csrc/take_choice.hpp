@@ -14,4 +14,14 @@ inline int move_threads(long long blocks, int head_dim, int bh) {
   return threads;
 }
 
+// Workgroups of 256 threads, `parts` to a (b,h), for a read-back of `rows` rows: units of them along one axis of the grid, as many as it
+// may have threads for, and `layers` of these along another.
+struct ExportGrid {
+  long long parts, units, layers;
+};
+inline ExportGrid export_grid(int bh, long long rows, int head_dim) {
+  const long long parts = (rows * (head_dim / 16) + 255) / 256, most = kMostThreads / 256 / parts, units = bh < most ? bh : most;
+  return {parts, units, (bh + units - 1) / units};
+}
+
 }  // namespace amskv

@@ -383,12 +383,14 @@ __global__ __launch_bounds__(256) void rope_table_kernel(const double* __restric
 // Bound: HBM (960 (b,h), up to 640 tokens, head dim 64: 44 us, about 5 TB/s).
 template <int D>
 __global__ __launch_bounds__(256) void export_codes_kernel(Codes c, __bf16* __restrict__ k_out, __bf16* __restrict__ v_out, long long cap_tokens,
-                                                           SegTable seg, ExtKV ext_kv, RowMap ext_map, int heads, int parts) {
+                                                           SegTable seg, ExtKV ext_kv, RowMap ext_map, int heads, int parts, int units,
+                                                           int n_bh) {
   __bf16* out = blockIdx.y ? v_out : k_out;
   if (!out) return;
   constexpr int kPer = D / 16;
   const unsigned unit = blockIdx.x / (unsigned)parts, part = blockIdx.x - unit * parts;
-  const long long bh = unit;
+  const long long bh = (long long)blockIdx.z * units + unit;
+  if (bh >= n_bh) return;
   const long long i = (long long)part * 256 + threadIdx.x;
   const int j = (int)(i / kPer), piece = (int)(i % kPer);
   if (j >= seg.total) return;
@@ -439,11 +441,12 @@ hipError_t launch_move_codes(const Codes& c, int bh, int head_dim, int64_t cap_t
 
 hipError_t launch_export_codes(const Codes& c, void* k_out, void* v_out, int bh, int head_dim, int64_t cap_tokens, const SegTable& seg,
                                const ExtKV& ext, const RowMap& ext_map, int heads, hipStream_t st) {
-  const long long parts = ((long long)seg.total * (head_dim / 16) + 255) / 256;
-  if (parts * bh > 0x7fffffff) return hipErrorInvalidValue;
+  if (seg.total == 0) return hipSuccess;
+  const ExportGrid g = export_grid(bh, seg.total, head_dim);
+  if (g.layers > 65535) return hipErrorInvalidValue;
   auto kernel = head_dim == 64 ? export_codes_kernel<64> : export_codes_kernel<128>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(parts * bh), 2), dim3(256), 0, st, c, (__bf16*)k_out, (__bf16*)v_out, (long long)cap_tokens, seg,
-                     ext, ext_map, heads, (int)parts);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(g.parts * g.units), 2, (unsigned)g.layers), dim3(256), 0, st, c, (__bf16*)k_out, (__bf16*)v_out,
+                     (long long)cap_tokens, seg, ext, ext_map, heads, (int)g.parts, (int)g.units, bh);
   return hipGetLastError();
 }
 

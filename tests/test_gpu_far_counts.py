@@ -69,3 +69,18 @@ def test_compaction_of_very_many_units():
                 want, bound = plain.attention(q[x], kk, vv, 1 / math.sqrt(D))
                 assert bool(((o[x].double() - want).abs() <= bound).all())
             assert not bool((ko == 9.0).all(dim=-1).any()) and not bool((vo == 9.0).all(dim=-1).any())
+
+
+def test_a_read_back_of_very_many_units():
+    """2^24 (b,h), the most a cache may have, of one token each: appended, attended, read back."""
+    B, H, D = 1 << 20, 16, 64
+    with Cache8(B, H, D, (1,), (0, 0, True)) as h:
+        q, k, v = (_normal(B, H, 1, D, seed=i) for i in range(3))
+        o, ko, vo = (torch.full((B, H, 1, D), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+        amskv.amskv_append_scale(h, 0, 0, k, v)
+        amskv.amskv_attend(h, 0, 0, q, o)
+        amskv.amskv_cache_export(h, 0, ko, vo)
+        for x in (slice(0, 5), slice(B // 2 - 3, B // 2 + 3), slice(B - 5, B)):
+            assert torch.equal(ko[x].double(), plain.held(k[x])) and torch.equal(vo[x].double(), plain.held(v[x]))
+            assert torch.equal(o[x], vo[x])                       # one key: its value
+        assert torch.equal(o, vo) and not bool((ko == 9.0).all(dim=-1).any())

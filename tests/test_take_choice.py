@@ -13,8 +13,13 @@ using namespace amskv;
 int main() {
   char what;
   long long a, b, c;
-  while (std::scanf(" %c %lld %lld %lld", &what, &a, &b, &c) == 4)
+  while (std::scanf(" %c %lld %lld %lld", &what, &a, &b, &c) == 4) {
     if (what == 'm') std::printf("%d\n", move_threads(a, (int)b, (int)c));
+    if (what == 'e') {
+      const ExportGrid g = export_grid((int)c, a, (int)b);
+      std::printf("%lld %lld %lld\n", g.parts, g.units, g.layers);
+    }
+  }
 }
 """
 
@@ -48,3 +53,13 @@ def test_a_slide_is_a_launch(ask):
     for (blocks, d, bh), (threads,) in zip(launches, ask("m", launches)):
         assert threads in (128, 256, 512, 1024) and threads * bh < 1 << 32
         assert bh >= 1 << 22 or threads == (256 if blocks * d <= 1024 and bh >= 128 else 1024)
+
+
+def test_a_read_back_is_a_launch(ask):
+    """Every (b,h) has its workgroups, fewer than 2^32 threads along an axis, and none beyond 2^31 workgroups or 65535 layers."""
+    launches = [(rows, d, bh) for rows in (1, 16, 33, 64, 65, 300, 5000, 1 << 22) for d in (64, 128) for bh in MANY if rows * bh < 1 << 33]
+    for (rows, d, bh), (parts, units, layers) in zip(launches, ask("e", launches)):
+        assert (parts - 1) * 256 < rows * d // 16 <= parts * 256
+        assert parts * units * 256 < 1 << 32 and 1 <= layers <= 65535
+        assert (layers - 1) * units < bh <= layers * units
+        assert layers == 1 or parts * bh * 256 >= 1 << 32
