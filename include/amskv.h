@@ -454,6 +454,8 @@ int32_t amskv_rotate(const amskv_rope* rope, int32_t dtype, int32_t head_dim, in
  * Where the scale is copied into the cache its turned keys go straight to their slot (quantised in an 8-bit cache: the fp32
  * result of the turn is rounded once) and K_dev is only read.  Where the scale is read in place instead
  * (borrow_unretained for a scale no later step reads, fuse_append, the token modes), K_dev itself is turned in place.
+ * What is written -- Q_out_dev, and K_dev where it is turned in place -- overlaps nothing else that is passed (Q_out_dev == Q_dev as
+ * said above apart); the same pointer in two such roles is refused.
  * K_dev, V_dev and table_dev must not be NULL.  Otherwise, and in its status codes, amskv_append_scale. */
 int32_t amskv_append_scale_rotary(amskv_cache* cache, int32_t layer, int32_t s, const amskv_rope* rope, const float* table_dev,
                                   const void* Q_dev, int64_t q_token_stride, void* Q_out_dev, void* K_dev, const void* V_dev,

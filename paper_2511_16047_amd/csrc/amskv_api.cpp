@@ -810,6 +810,11 @@ int append_step(amskv_cache* c, int32_t layer, int32_t s, const void* K_dev, con
   LayerState& L = c->layer[layer];
   if (s != L.last_scale + 1) return AMSKV_ERR_ORDER;
   if (K_dev && !c->arena) return AMSKV_ERR_NO_DEVICE_MEMORY;
+  if (turn) {  // what one wave of the launch writes, another must not read
+    const bool in_place = c->mode == AMSKV_MODE_TOKEN_BUDGET || c->fuse != 0 || !stored(L.pol, s, c->n_scales, c->borrow != 0);
+    if (turn->q_out && (turn->q_out == K_dev || turn->q_out == V_dev)) return AMSKV_ERR_INVALID_ARG;
+    if (in_place && (K_dev == V_dev || K_dev == turn->q)) return AMSKV_ERR_INVALID_ARG;
+  }
 
   const int bh = c->batch * c->heads;
   const int row_bytes = c->head_dim * c->elem_bytes;
