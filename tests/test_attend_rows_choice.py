@@ -77,12 +77,13 @@ def test_every_form_that_is_built_and_no_other(choose, cross):
     assert taken == built
 
 
-# (b,h), queries, keys of the step, as the tests of test_gpu_cache_in_8_bits.py drive them, and the forms they are there for
+# (b,h), queries, keys of the step, as the tests of test_gpu_cache_in_8_bits.py and test_gpu_operators_reach.py drive them, and the forms they are there for
 @pytest.mark.parametrize("launch,form", [
     ((64, 3, 300, 800), (1, 8)), ((128, 3, 300, 1600), (1, 8)), ((64, 3, 257, 290), (1, 4)), ((128, 3, 257, 290), (1, 4)),
     ((64, 6, 1, 1), (1, 1)), ((64, 2080, 169, 205), (1, 1)), ((128, 2080, 100, 104), (4, 1)), ((64, 150, 256, 456), (8, 1)),
     ((128, 150, 256, 456), (8, 1)), ((128, 150, 225, 425), (8, 1)), ((128, 272, 225, 1056), (4, 1)), ((64, 150, 128, 328), (4, 1)),
-    ((128, 150, 128, 328), (4, 1)), ((64, 75, 500, 700), (8, 1)), ((128, 75, 500, 700), (8, 1)), ((128, 130, 257, 457), (4, 1))])
+    ((128, 150, 128, 328), (4, 1)), ((64, 75, 500, 700), (8, 1)), ((128, 75, 500, 700), (8, 1)), ((128, 130, 257, 457), (4, 1)),
+    ((64, 150, 256, 2756), (8, 1)), ((128, 150, 256, 2756), (8, 1)), ((64, 150, 256, 2816), (8, 1)), ((128, 150, 256, 2816), (8, 1))])
 def test_launches_of_the_gpu_tests_over_codes(choose, launch, form):
     assert choose(0, [launch]) == [form + (1,)]
 
