@@ -343,12 +343,9 @@ hipError_t take(const Take& t, hipStream_t st) {
   const dim3 g((unsigned)grid, n), block(64 * kWaves);
   if constexpr (sizeof(T) == 2) {
     if (t.eight_bits && t.moves != nullptr && t.moves->n > 0) {
-      // us an append, at once / in two launches, units x tokens.  D 64: 16 x 16 3.6 / 4.6, 16 x 256 4.9 / 5.1, 16 x 512 7.1 / 5.8, 256 x 64
-      // 4.8 / 6.4, 256 x 256 9.4 / 13.1, 256 x 512 16.3 / 20.4 (turned: 29.8 / 28.3), 960 x 16 9.1 / 6.8, 960 x 256 30.7 / 32.8.  D 128: 16 x
-      // 128 4.6 / 5.4, 16 x 256 6.2 / 6.1, 256 x 128 10.8 / 11.6, 256 x 256 20.3 / 20.2, 960 x 64 21.2 / 17.3.  So: where a workgroup to a
-      // (b,h) and tensor has few blocks to a wave, and there are no more of them than the chip holds at once.
-      if (t.batch * t.heads <= 256 && t.tokens * D <= 16384) {
-        hipLaunchKernelGGL((slide_and_take_kernel<D>), dim3(t.batch * t.heads, n), dim3(64 * kOwners), 0, st, a, block_list(*t.moves));
+      const BlockList list = block_list(*t.moves);
+      if (slides_at_once(t.batch * t.heads, t.tokens, list.total, D)) {
+        hipLaunchKernelGGL((slide_and_take_kernel<D>), dim3(t.batch * t.heads, n), dim3(64 * kOwners), 0, st, a, list);
         return hipGetLastError();
       }
       const hipError_t e = launch_move_codes(t.codes, t.batch * t.heads, t.head_dim, t.cap_tokens, *t.moves, st);

@@ -12,8 +12,9 @@ PROGRAM = r"""
 using namespace amskv;
 int main() {
   char what;
-  long long a, b, c;
-  while (std::scanf(" %c %lld %lld %lld", &what, &a, &b, &c) == 4) {
+  long long a, b, c, d;
+  while (std::scanf(" %c %lld %lld %lld %lld", &what, &a, &b, &c, &d) == 5) {
+    if (what == 's') std::printf("%d\n", slides_at_once((int)a, b, c, (int)d));
     if (what == 'm') std::printf("%d\n", move_threads(a, (int)b, (int)c));
     if (what == 'e') {
       const ExportGrid g = export_grid((int)c, a, (int)b);
@@ -38,7 +39,7 @@ def ask(tmp_path_factory):
     assert b.returncode == 0, b.stdout[-4000:]
 
     def run(what, launches):
-        r = subprocess.run([exe], input="".join("%s %d %d %d\n" % (what, *x) for x in launches), stdout=subprocess.PIPE, text=True, timeout=120, check=True)
+        r = subprocess.run([exe], input="".join("%s %d %d %d %d\n" % (what, *x, *(0,) * (4 - len(x))) for x in launches), stdout=subprocess.PIPE, text=True, timeout=120, check=True)
         return [tuple(int(y) for y in line.split()) for line in r.stdout.splitlines()]
 
     return run
@@ -63,3 +64,12 @@ def test_a_read_back_is_a_launch(ask):
         assert parts * units * 256 < 1 << 32 and 1 <= layers <= 65535
         assert (layers - 1) * units < bh <= layers * units
         assert layers == 1 or parts * bh * 256 >= 1 << 32
+
+
+# (b,h), tokens of the new scale, blocks of 16 that slide, head dim; as timed, at once or in two launches
+@pytest.mark.parametrize("bh,tokens,blocks,d,at_once", [
+    (16, 16, 1, 64, 1), (16, 256, 16, 64, 1), (16, 512, 16, 64, 0), (256, 256, 16, 64, 1), (16, 128, 8, 128, 1), (16, 256, 16, 128, 0),
+    (960, 16, 1, 64, 0), (16, 16, 32, 64, 1), (16, 16, 64, 64, 0), (1, 1, 256, 64, 0), (256, 16, 256, 64, 0), (16, 16, 16, 128, 1),
+    (16, 16, 32, 128, 0), (256, 1, 256, 128, 0)])
+def test_a_short_scale_behind_long_survivors_has_a_launch_of_its_own(ask, bh, tokens, blocks, d, at_once):
+    assert ask("s", [(bh, tokens, blocks, d)]) == [(at_once,)]
