@@ -88,3 +88,11 @@ def test_queries_that_look_at_the_far_end():
             weight = torch.softmax(q[b, h].double() @ kk.T / math.sqrt(D), dim=-1)
             assert bool((weight[torch.arange(len(aims)), aims] > 0.99).all())
             assert bool(((o[b, h].double() - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H", [2, 40])
+@pytest.mark.parametrize("long", [255, 512, 513, 1500, 5000])
+def test_long_survivors_behind_short_scales(D, H, long):
+    """Survivors that slide by one block in one pass and in many, in the launch of the append and in one of their own."""
+    _drive([(1, 16), (1, long), (1, 5), (1, 40)], 1, H, D, [(0, 2, False), (0, 1, False)] if H == 2 else [(0, 2, False)], seed=long)
