@@ -186,10 +186,11 @@ typedef struct {
  * power of two per (b, h) and tensor.  With m the largest magnitude of such a block of tokens x D and e the least integer
  * >= -100 with m <= 448 * 2^e, an element x is held as the e4m3 number nearest to x / 2^e (4 significant bits, ties to
  * even; x must be finite; beyond 1.875 * 2^127 as that), which stands for that number times 2^e -- a bf16 number exactly,
- * so that nothing else is lost on the way into the attention: relative error at most 2^-4, absolute error at most 2^(e-10)
+ * so that nothing else is lost between the cache and the attention's products: relative error at most 2^-4, absolute error at most 2^(e-10)
  * below 2^(e-6), elements below 2^-110 become 0.
  * amskv_attend reads the cached values, the current scale's included, unless that scale is read in place
- * (borrow_unretained), in which case its bf16 K and V are read as they are.  amskv_cache_export writes the values as bf16.
+ * (borrow_unretained), in which case its bf16 K and V are read as they are; from there on it is what it is for a bf16 cache (weights
+ * rounded to bf16 before the second product, and added up as rounded).  amskv_cache_export writes the values as bf16.
  * Scale-window mode in either layout, either io layout (kv_token_stride below 2^23 elements); fuse_append must be 0.
  * Slots start at multiples of AMSKV_KV8_BLOCK tokens and capacities are multiples of it.  amskv_cache_bytes_held counts one
  * byte per element and four per block and tensor.  The similarity and density calls are for 16- and 32-bit caches: they
@@ -473,7 +474,8 @@ int32_t amskv_append_scale_rotary(amskv_cache* cache, int32_t layer, int32_t s, 
  * The token strides of K and V are below 2^23 elements; batch * heads is up to 2^24, q_tokens up to 2^22 (2^26 with the heads
  * that share a kv head), kv_tokens up to 2^26, and blocks of 32 queries -- of all heads that share a kv head together -- over all
  * (b, kv head) up to 2^26 - 8.  O overlaps none of the others.
- * bf16: finite Q, K and V, fp32 accumulation and softmax, P rounded to bf16 before the second product, O rounded to bf16. */
+ * bf16: finite Q, K and V, fp32 accumulation and softmax, P rounded to bf16 before the second product and added up as rounded, O
+ * rounded to bf16; |V| as for amskv_attend: below the largest float by a factor of 2^10 times the number of states. */
 typedef struct {
   int32_t batch, heads, kv_heads; /* heads a multiple of kv_heads                            */
   int32_t head_dim;               /* 64 or 128                                               */

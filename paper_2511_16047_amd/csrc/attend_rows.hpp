@@ -12,9 +12,9 @@
 // itself (kTeamWaves 1) takes K straight to registers and has one tile of V in LDS, no barriers; kTeams such waves of a
 // workgroup hold the same rows, take every kTeams-th tile, and their results meet in LDS at the end.
 //
-// Bound: where keys are many the matrix and vector pipes and what power leaves of them (head dim 128, 64 units 4096 x 6421, codes: 802
-// us, 1.07 PFLOP/s, with the staging of codes 8% behind keys that are bf16 rows already; a large library product reaches 1.22;
-// head dim 64, 3840 units 256 x 530: 190 us, 0.70 PFLOP/s, the exponentials' share is twice as large); where they are few, the
+// Bound: where keys are many the matrix and vector pipes and what power leaves of them (head dim 128, 64 units 4096 x 6421, codes: 772
+// to 800 us from card to card, 1.12 to 1.08 PFLOP/s; a large library product reaches 1.22;
+// head dim 64, 3840 units 256 x 530: 190 to 195 us, 0.70 to 0.68 PFLOP/s, the exponentials' share is twice as large); where they are few, the
 // latency of arguments, Q, the first tiles and O in turn: 3.5 to 7 us.
 #pragma once
 #include "codes.hpp"
@@ -323,8 +323,8 @@ struct Unit {
   // follows the new reference at the top of the next step.
   //
   // Codes at head dim 128: the first block, which has none before it, is no question but weights of 0 for what lies in its
-  // slot, and O^T follows at once: one basic block from K to the weights (64 units 2304 x 3925 363 -> 349 us, 32 units 209 -> 196, 4096 x
-  // 6421 808 -> 784).  Elsewhere walks are short for four products more, and their registers (head dim 64, 256 x 530 188 -> 193).
+  // slot, and O^T follows at once: one basic block from K to the weights (both sides on one card: 64 units 2304 x 3925 363 -> 349 us, 32
+  // units 209 -> 196, 4096 x 6421 808 -> 784).  Elsewhere walks are short for four products more, and their registers (head dim 64, 256 x 530 188 -> 193).
   static constexpr bool kOneBlock = D == 128 && kEight;
   struct Behind {
     bf16x8 pf[2];
@@ -333,7 +333,7 @@ struct Unit {
     bool rescale, first;
   };
   // Where a team of eight has the CU to itself (head dim 128), the softmax goes before the score products of the wave it shares a SIMD
-  // with, so that the two come to differ in what they do: 64 units 4096 x 6421 834 -> 802 us.  Waves of two teams on a SIMD hold each
+  // with, so that the two come to differ in what they do: 64 units 4096 x 6421 834 -> 802 us, before the one basic block above.  Waves of two teams on a SIMD hold each
   // other up instead: teams of four, 80 units 1024 x 2000, 121 -> 134, of eight at head dim 64, 150 units 1100 x 2000, 112 -> 125.
   // `between`, behind the score products, replaces kf by the next block's fragments: they arrive beside the softmax.
   template <bool kFull, class Between>
