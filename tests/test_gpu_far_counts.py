@@ -48,9 +48,10 @@ class Cache8:
         amskv.amskv_cache_destroy(self.h)
 
 
-def test_compaction_of_very_many_units():
-    """2^22 (b,h): the scale that stays slides to the front, step after step."""
-    B, H, D, tokens = 1 << 18, 16, 64, (1, 1, 2, 1)
+@pytest.mark.parametrize("B", [1 << 18, 1 << 20])
+def test_compaction_of_very_many_units(B):
+    """2^22 and 2^24 (b,h): the scale that stays slides to the front, step after step."""
+    H, D, tokens = 16, 64, (1, 1, 2, 1)
     some = [slice(0, 3), slice(B // 2 - 2, B // 2 + 2), slice(B - 3, B)]
     with Cache8(B, H, D, tokens, (0, 1, False)) as h:
         kept = []
