@@ -23,8 +23,8 @@
  *                           arena; the kept scales sit back to back in ascending scale
  *                           order (AMSKV_LAYOUT_COMPACT) or at offsets fixed at create
  *                           time (AMSKV_LAYOUT_PLANNED); amskv_cache_layout reports them
- * Element type: float (dtype 0) or bfloat16 (dtype 1), the same for every tensor; with dtype 2 the tensors are bfloat16 and
- * the cache holds K and V in 8 bits (see "8-bit cache").
+ * Element type: float (dtype 0) or bfloat16 (dtype 1), the same for every tensor; with dtype 2 or 3 the tensors are
+ * bfloat16 and the cache holds K and V in 8 or 4 bits (see "8-bit cache", "4-bit cache").
  *
  * Every function returns an amskv_status (0 = ok, negative = error) unless stated.
  * On error nothing has been enqueued and the cache state is unchanged; the one exception is
@@ -51,8 +51,14 @@ typedef enum {
   AMSKV_ERR_NO_HOST_MEMORY = -8   /* a host allocation failed; destroy the cache             */
 } amskv_status;
 
-enum { AMSKV_DTYPE_F32 = 0, AMSKV_DTYPE_BF16 = 1, AMSKV_DTYPE_BF16_KV8 = 2 /* see "8-bit cache" below */ };
+enum {
+  AMSKV_DTYPE_F32 = 0,
+  AMSKV_DTYPE_BF16 = 1,
+  AMSKV_DTYPE_BF16_KV8 = 2, /* see "8-bit cache" below */
+  AMSKV_DTYPE_BF16_KV4 = 3  /* see "4-bit cache" below */
+};
 enum { AMSKV_KV8_BLOCK = 16 }; /* tokens of a scale that share a power of two in an 8-bit cache */
+enum { AMSKV_KV4_GROUP = 32 }; /* channels of a token that share a power of two in a 4-bit cache */
 enum { AMSKV_ROPE_HALF = 0, AMSKV_ROPE_INTERLEAVED = 1 };
 enum { AMSKV_LAYOUT_COMPACT = 0, AMSKV_LAYOUT_PLANNED = 1 };
 enum { AMSKV_MODE_SCALE_WINDOW = 0, AMSKV_MODE_TOKEN_BUDGET = 1, AMSKV_MODE_TOKEN_WINDOW = 2 };
@@ -70,7 +76,7 @@ typedef struct {
   const int32_t* side_h;  /* host, [n_scales], each >= 1                  */
   const int32_t* side_w;  /* host, [n_scales], each >= 1                  */
   int32_t batch;          /* B >= 1                                       */
-  int32_t dtype;          /* AMSKV_DTYPE_F32, _BF16 or _BF16_KV8          */
+  int32_t dtype;          /* AMSKV_DTYPE_F32, _BF16, _BF16_KV8 or _KV4    */
 } amskv_schedule;
 
 /* Per-layer policy in scale units (Section 4.3; Algorithm 2 with budgets counted in whole
@@ -195,6 +201,16 @@ typedef struct {
  * Slots start at multiples of AMSKV_KV8_BLOCK tokens and capacities are multiples of it.  amskv_cache_bytes_held counts one
  * byte per element and four per block and tensor.  The similarity and density calls are for 16- and 32-bit caches: they
  * return AMSKV_ERR_INVALID_ARG (a model is profiled on one of those). */
+
+/* 4-bit cache (dtype = AMSKV_DTYPE_BF16_KV4).  As the 8-bit cache, but for what an element is held as.  The AMSKV_KV4_GROUP
+ * channels 32 i .. 32 i + 31 of one token of a (b, h) and tensor share one power of two.  With m their largest magnitude and e the
+ * least integer, -100 <= e <= 125, with m <= 7 * 2^e, an element x is held as the e2m1 number (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives) nearest to x / 2^e, ties to even (x must be finite; beyond 6 as 6), which stands for that number times 2^e, a bf16
+ * number exactly: off by at most 2^(e-2) below 2^(e+1), 2^(e-1) below 2^(e+2) and 2^e above (elements beyond 7 * 2^125 apart), which
+ * is at most 2/7 of m; elements of at most 2^-102 become 0.  4.25 bits an element.
+ * A token's values depend on nothing but the token: slots may start at any token and capacities are any number of them.
+ * amskv_cache_bytes_held counts half a byte per element and one per group.  The modes, layouts and limits of the 8-bit
+ * cache, the similarity and density calls among them. */
 
 /* mode = AMSKV_MODE_TOKEN_WINDOW.  The sliding-window and sink-plus-window kept sets that the
  * comparison with other cache strategies (Section 5, the table of SWA / H2O / STA) sets against
@@ -479,7 +495,7 @@ int32_t amskv_append_scale_rotary(amskv_cache* cache, int32_t layer, int32_t s, 
 typedef struct {
   int32_t batch, heads, kv_heads; /* heads a multiple of kv_heads                            */
   int32_t head_dim;               /* 64 or 128                                               */
-  int32_t dtype;                  /* AMSKV_DTYPE_BF16                                        */
+  int32_t dtype;                  /* AMSKV_DTYPE_BF16, or _BF16_KV4: held states (see below) */
   int32_t q_tokens;               /* queries of a batch element and head; 0: nothing to do   */
   int32_t kv_tokens;              /* most states of a batch element                          */
   int64_t kv_rows;                /* rows of packed K and V (offsets_dev); else not read     */
@@ -497,6 +513,28 @@ int32_t amskv_cross_workspace_bytes(const amskv_cross* cross, uint64_t* bytes_ou
 int32_t amskv_cross_attend(const amskv_cross* cross, const void* Q_dev, const void* K_dev, const void* V_dev, void* O_dev,
                            const int32_t* lengths_dev, const int32_t* offsets_dev, void* workspace_dev,
                            uint64_t workspace_bytes, void* stream);
+
+/* States held in 4 bits (amskv_cross.dtype = AMSKV_DTYPE_BF16_KV4).  A prompt's K and V are made once and read by every step: they can
+ * be held in 4 bits, in the format of the 4-bit cache, 4.25 bits an element.  A held tensor is a caller's buffer of
+ * amskv_cross_held_bytes bytes (packed 0: batch * kv_heads units of kv_tokens rows; 1: kv_heads units of kv_rows rows, for offsets_dev),
+ * 16-byte aligned, of which no other call writes anything.  Host only. */
+int32_t amskv_cross_held_bytes(const amskv_cross* cross, int32_t packed, uint64_t* bytes_out);
+
+/* K_dev and V_dev (bf16, strides cross->k and cross->v) into held tensors; either pair may be NULL.  Rows that hold states are
+ * read and written: row j < length of b where padded, rows offsets[0] .. offsets[batch] - 1 of the axis where packed, all of
+ * them if neither is given; the others stay as they were.  Elements of those rows must be finite.  Of *cross the queries' members and
+ * strides q and o are not used here.  What is written overlaps nothing else that is passed; the same pointer in two such roles is
+ * refused.  One launch.  Asynchronous on `stream`. */
+int32_t amskv_cross_hold(const amskv_cross* cross, const void* K_dev, const void* V_dev, void* K_held_dev, void* V_held_dev,
+                         const int32_t* lengths_dev, const int32_t* offsets_dev, void* stream);
+
+/* The values of held tensors as bf16, the same rows, at the strides of cross->k and cross->v (which have to nest, as of all tensors that
+ * are written).  Rows without states are left as they were. */
+int32_t amskv_cross_export(const amskv_cross* cross, const void* K_held_dev, const void* V_held_dev, void* K_out_dev, void* V_out_dev,
+                           const int32_t* lengths_dev, const int32_t* offsets_dev, void* stream);
+
+/* amskv_cross_attend over held states: K_dev and V_dev are the held tensors, cross->k and cross->v are not read, lengths_dev and
+ * offsets_dev as they were held with; all else is as above. */
 
 /* Static text for a status code. */
 const char* amskv_status_string(int32_t status);

@@ -25,8 +25,9 @@ AMSKV_ERR_NO_DEVICE_MEMORY = -6
 AMSKV_ERR_STATIC_LIMIT = -7
 AMSKV_ERR_NO_HOST_MEMORY = -8
 AMSKV_STATIC_MAX_UNITS = 16384
-AMSKV_DTYPE_F32, AMSKV_DTYPE_BF16, AMSKV_DTYPE_BF16_KV8 = 0, 1, 2
+AMSKV_DTYPE_F32, AMSKV_DTYPE_BF16, AMSKV_DTYPE_BF16_KV8, AMSKV_DTYPE_BF16_KV4 = 0, 1, 2, 3
 AMSKV_KV8_BLOCK = 16
+AMSKV_KV4_GROUP = 32
 AMSKV_ROPE_HALF, AMSKV_ROPE_INTERLEAVED = 0, 1
 AMSKV_LAYOUT_COMPACT, AMSKV_LAYOUT_PLANNED = 0, 1
 AMSKV_MODE_SCALE_WINDOW, AMSKV_MODE_TOKEN_BUDGET, AMSKV_MODE_TOKEN_WINDOW = 0, 1, 2
@@ -44,6 +45,7 @@ EXPORTED = [
     "amskv_cache_set_io_layout", "amskv_interscale_similarity_enqueue", "amskv_interscale_similarity_collect",
     "amskv_interscale_similarity_enqueue_static",
     "amskv_rope_table", "amskv_rotate", "amskv_append_scale_rotary", "amskv_cross_workspace_bytes", "amskv_cross_attend",
+    "amskv_cross_held_bytes", "amskv_cross_hold", "amskv_cross_export",
 ]
 
 
@@ -170,6 +172,12 @@ def load_library() -> C.CDLL:
     lib.amskv_cross_workspace_bytes.restype = i32
     lib.amskv_cross_attend.argtypes = [px, vp, vp, vp, vp, vp, vp, vp, u64, vp]
     lib.amskv_cross_attend.restype = i32
+    lib.amskv_cross_held_bytes.argtypes = [px, i32, C.POINTER(u64)]
+    lib.amskv_cross_held_bytes.restype = i32
+    lib.amskv_cross_hold.argtypes = [px, vp, vp, vp, vp, vp, vp, vp]
+    lib.amskv_cross_hold.restype = i32
+    lib.amskv_cross_export.argtypes = [px, vp, vp, vp, vp, vp, vp, vp]
+    lib.amskv_cross_export.restype = i32
 
     try:
         from . import _pycalls
@@ -497,7 +505,8 @@ def amskv_cross_workspace_bytes(cross) -> int:
 
 
 def amskv_cross_attend(cross, Q, K, V, O, lengths=None, offsets=None, workspace=None, workspace_bytes=None, stream=None):
-    """lengths: device int32 [batch]; offsets: device int32 [batch + 1]; workspace: device tensor (its size is taken from it) or,
+    """K, V: the states, or with dtype AMSKV_DTYPE_BF16_KV4 their held tensors (amskv_cross_hold).
+    lengths: device int32 [batch]; offsets: device int32 [batch + 1]; workspace: device tensor (its size is taken from it) or,
     with workspace_bytes, an address."""
     if workspace is None:
         workspace_bytes = 0
@@ -512,3 +521,22 @@ def amskv_cross_attend(cross, Q, K, V, O, lengths=None, offsets=None, workspace=
                                          workspace_bytes, _stream(stream))
     if status:
         _check(status, "amskv_cross_attend")
+
+
+def amskv_cross_held_bytes(cross, packed=False) -> int:
+    """Bytes of a held tensor; packed: states back to back, located by offsets."""
+    out = C.c_uint64(0)
+    _check(load_library().amskv_cross_held_bytes(cross, int(bool(packed)), C.byref(out)), "amskv_cross_held_bytes")
+    return int(out.value)
+
+
+def amskv_cross_hold(cross, K, V, K_held, V_held, lengths=None, offsets=None, stream=None):
+    """K, V: bf16 states at the strides of `cross`; K_held, V_held: device tensors of amskv_cross_held_bytes bytes each."""
+    _check(load_library().amskv_cross_hold(cross, _ptr(K), _ptr(V), _ptr(K_held), _ptr(V_held), _ptr(lengths), _ptr(offsets), _stream(stream)),
+           "amskv_cross_hold")
+
+
+def amskv_cross_export(cross, K_held, V_held, K_out, V_out, lengths=None, offsets=None, stream=None):
+    """The held values as bf16, at the strides of `cross`."""
+    _check(load_library().amskv_cross_export(cross, _ptr(K_held), _ptr(V_held), _ptr(K_out), _ptr(V_out), _ptr(lengths), _ptr(offsets),
+                                             _stream(stream)), "amskv_cross_export")

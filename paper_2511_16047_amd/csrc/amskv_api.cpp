@@ -34,7 +34,7 @@ struct LayerState {
   int64_t cap = 0;         // tokens
   uint64_t k_off = 0;      // byte offset of the K region inside the arena
   uint64_t v_off = 0;
-  uint64_t k_scale = 0, v_scale = 0;  // 8-bit cache: of the powers of two of their blocks
+  uint64_t k_scale = 0, v_scale = 0;  // 8 or 4 bits: of the powers of two of their blocks or groups
   int32_t last_scale = -1;
   std::vector<Segment> segs;        // ascending scale id
   std::vector<int32_t> last_evicted;
@@ -80,6 +80,8 @@ constexpr uint64_t kAlign = 256;
 inline uint64_t align_up(uint64_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 inline bool eight_bits(int32_t dtype) { return dtype == AMSKV_DTYPE_BF16_KV8; }
+inline bool four_bits(int32_t dtype) { return dtype == AMSKV_DTYPE_BF16_KV4; }
+inline bool coded(int32_t dtype) { return eight_bits(dtype) || four_bits(dtype); }
 // tokens a slot for t tokens takes: whole blocks in an 8-bit cache
 inline int32_t slot_tokens(int32_t dtype, int32_t t) {
   return eight_bits(dtype) ? (t + AMSKV_KV8_BLOCK - 1) / AMSKV_KV8_BLOCK * AMSKV_KV8_BLOCK : t;
@@ -112,8 +114,8 @@ int validate(int32_t layers, int32_t heads, int32_t head_dim, const amskv_schedu
   if (sc->n_scales < 1 || sc->n_scales > AMSKV_MAX_SCALES || !sc->side_h || !sc->side_w)
     return AMSKV_ERR_INVALID_ARG;
   if (sc->batch < 1) return AMSKV_ERR_INVALID_ARG;
-  if (sc->dtype != AMSKV_DTYPE_F32 && sc->dtype != AMSKV_DTYPE_BF16 && !eight_bits(sc->dtype)) return AMSKV_ERR_INVALID_ARG;
-  if (eight_bits(sc->dtype) && (po->mode != AMSKV_MODE_SCALE_WINDOW || po->fuse_append != 0)) return AMSKV_ERR_INVALID_ARG;
+  if (sc->dtype != AMSKV_DTYPE_F32 && sc->dtype != AMSKV_DTYPE_BF16 && !coded(sc->dtype)) return AMSKV_ERR_INVALID_ARG;
+  if (coded(sc->dtype) && (po->mode != AMSKV_MODE_SCALE_WINDOW || po->fuse_append != 0)) return AMSKV_ERR_INVALID_ARG;
   int64_t total = 0;
   for (int i = 0; i < sc->n_scales; ++i) {
     if (sc->side_h[i] < 1 || sc->side_w[i] < 1) return AMSKV_ERR_INVALID_ARG;
@@ -259,8 +261,8 @@ void build_plan(int32_t layers, int32_t heads, int32_t head_dim, const amskv_sch
                 const amskv_policy* po, Plan* pl) {
   int32_t tokens[AMSKV_MAX_SCALES];
   for (int i = 0; i < sc->n_scales; ++i) tokens[i] = slot_tokens(sc->dtype, sc->side_h[i] * sc->side_w[i]);
-  const uint64_t eb = eight_bits(sc->dtype) ? 1 : sc->dtype == AMSKV_DTYPE_BF16 ? 2 : 4;
-  const uint64_t row = (uint64_t)head_dim * eb;
+  const uint64_t bits = four_bits(sc->dtype) ? 4 : eight_bits(sc->dtype) ? 8 : sc->dtype == AMSKV_DTYPE_BF16 ? 16 : 32;
+  const uint64_t row = (uint64_t)head_dim * bits / 8;
   const uint64_t bh = (uint64_t)sc->batch * heads;
   const bool borrow = po->borrow_unretained != 0;
   uint64_t at = 0;
@@ -283,14 +285,16 @@ void build_plan(int32_t layers, int32_t heads, int32_t head_dim, const amskv_sch
     at = align_up(at + bh * (uint64_t)cap * row);
     pl->v_off[l] = at;
     at = align_up(at + bh * (uint64_t)cap * row);
-    if (eight_bits(sc->dtype)) {
+    if (coded(sc->dtype)) {
+      const uint64_t scales = eight_bits(sc->dtype) ? bh * (uint64_t)cap / AMSKV_KV8_BLOCK * sizeof(float)
+                                                    : bh * (uint64_t)cap * (head_dim / AMSKV_KV4_GROUP);
       pl->k_scale[l] = at;
-      at = align_up(at + bh * (uint64_t)cap / AMSKV_KV8_BLOCK * sizeof(float));
+      at = align_up(at + scales);
       pl->v_scale[l] = at;
-      at = align_up(at + bh * (uint64_t)cap / AMSKV_KV8_BLOCK * sizeof(float));
+      at = align_up(at + scales);
     }
   }
-  if (eight_bits(sc->dtype)) {  // neither similarity nor density: no workspaces
+  if (coded(sc->dtype)) {  // neither similarity nor density: no workspaces
     pl->ws_off = pl->dens_off = pl->total = at;
     return;
   }
@@ -324,6 +328,11 @@ inline RowMap arena_map(const amskv_cache* c, const LayerState& L) {
 inline amskv::Codes codes(const amskv_cache* c, const LayerState& L) {
   char* a = c->arena;
   return {(unsigned char*)a + L.k_off, (unsigned char*)a + L.v_off, (float*)(a + L.k_scale), (float*)(a + L.v_scale)};
+}
+
+inline amskv::Codes4 codes4(const amskv_cache* c, const LayerState& L) {
+  unsigned char* a = (unsigned char*)c->arena;
+  return {a + L.k_off, a + L.v_off, a + L.k_scale, a + L.v_scale};
 }
 
 inline bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
@@ -780,6 +789,7 @@ amskv::Take take_of(const amskv_cache* c, int32_t tokens) {
   t.head_dim = c->head_dim;
   t.dtype = c->dtype == AMSKV_DTYPE_F32 ? AMSKV_DTYPE_F32 : AMSKV_DTYPE_BF16;
   t.eight_bits = eight_bits(c->dtype);
+  t.four_bits = four_bits(c->dtype);
   return t;
 }
 
@@ -797,7 +807,7 @@ void add_turn(const amskv_cache* c, const Turn& turn, int32_t tokens, amskv::Tak
 int turn_in_place(const amskv_cache* c, const Turn& turn, int32_t tokens, const void* K_dev, hipStream_t st) {
   amskv::Take t = take_of(c, tokens);
   add_turn(c, turn, tokens, &t);
-  t.eight_bits = false;
+  t.eight_bits = t.four_bits = false;
   t.k = K_dev;
   t.k_out = const_cast<void*>(K_dev);  // amskv_append_scale_rotary's K_dev
   t.kv_map = t.out_map = caller_map(c, tokens, c->kv_tok);
@@ -886,12 +896,13 @@ int append_step(amskv_cache* c, int32_t layer, int32_t s, const void* K_dev, con
   const bool copy_now = keep_copy && !defer;
   if (turn && !copy_now)
     if (int rc = turn_in_place(c, *turn, cur.len, K_dev, (hipStream_t)stream)) return rc;
-  if (K_dev && (eight_bits(c->dtype) || (turn && copy_now))) {
-    // the survivors first, then (in an 8-bit cache at once) the new scale: turned, quantised or both on the way to its slot
+  if (K_dev && (coded(c->dtype) || (turn && copy_now))) {
+    // the survivors first, then (in a cache of 8 or 4 bits at once) the new scale: turned, quantised or both on the way to its slot
     const hipStream_t st = (hipStream_t)stream;
     hipError_t e = hipSuccess;
-    if (mv.n > 0 && !(eight_bits(c->dtype) && copy_now))
-      e = eight_bits(c->dtype) ? amskv::launch_move_codes(codes(c, L), bh, c->head_dim, L.cap, mv, st)
+    if (mv.n > 0 && !(coded(c->dtype) && copy_now))
+      e = eight_bits(c->dtype)  ? amskv::launch_move_codes(codes(c, L), bh, c->head_dim, L.cap, mv, st)
+          : four_bits(c->dtype) ? amskv::launch_move_codes4(codes4(c, L), bh, c->head_dim, L.cap, mv, st)
                                : amskv::launch_append(c->arena + L.k_off, c->arena + L.v_off, nullptr, nullptr, bh, row_bytes, L.cap, mv,
                                                       cur.len, 0, 0, caller_map(c, cur.len, c->kv_tok), c->heads, st);
     if (e == hipSuccess && copy_now) {
@@ -902,8 +913,11 @@ int append_step(amskv_cache* c, int32_t layer, int32_t s, const void* K_dev, con
       t.kv_map = caller_map(c, cur.len, c->kv_tok);
       t.cap_tokens = L.cap;
       t.dst_new = cur.off;
-      if (t.eight_bits) {
-        t.codes = codes(c, L);
+      if (t.eight_bits || t.four_bits) {
+        if (t.eight_bits)
+          t.codes = codes(c, L);
+        else
+          t.codes4 = codes4(c, L);
         t.moves = &mv;
       } else {
         t.out_map = arena_map(c, L);
@@ -970,7 +984,7 @@ static int attend_step(amskv_cache* c, int32_t layer, int32_t s, const void* Q_d
   if (s != L.last_scale) return AMSKV_ERR_ORDER;
   // token-budget mode: once the scale's iteration of Algorithm 1 has run it is no longer whole
   if (c->mode == AMSKV_MODE_TOKEN_BUDGET && !L.roll_pending) return AMSKV_ERR_ORDER;
-  if (mass_out_dev && eight_bits(c->dtype)) return AMSKV_ERR_INVALID_ARG;
+  if (mass_out_dev && coded(c->dtype)) return AMSKV_ERR_INVALID_ARG;
   if (!c->arena) return AMSKV_ERR_NO_DEVICE_MEMORY;
   ExtKV ext;
   const SegTable t = seg_table(L, &ext);
@@ -1079,6 +1093,9 @@ static int attend_step(amskv_cache* c, int32_t layer, int32_t s, const void* Q_d
   else if (eight_bits(c->dtype))
     e = amskv::launch_attend_codes(Q_dev, O_dev, codes(c, L), bh, c->tokens[s], c->head_dim, L.cap, t, ext, io, c->softmax_scale,
                                    (hipStream_t)stream);
+  else if (four_bits(c->dtype))
+    e = amskv::launch_attend_codes4(Q_dev, O_dev, codes4(c, L), bh, c->tokens[s], c->head_dim, L.cap, t, ext, io, c->softmax_scale,
+                                    (hipStream_t)stream);
   else
     e = amskv::launch_attend_f32(Q_dev, O_dev, c->arena + L.k_off, c->arena + L.v_off, bh,
                                  c->tokens[s], c->head_dim, L.cap, t, ext, io, c->softmax_scale,
@@ -1109,7 +1126,7 @@ int32_t amskv_attend_density(amskv_cache* c, int32_t layer, int32_t s, const voi
 
 // Checks shared by the two ways of asking for Eq. 3; on success cur/prev point at the two whole scales.
 static int similarity_operands(amskv_cache* c, int32_t layer, int32_t s, const Segment** cur, const Segment** prev) {
-  if (bad_layer(c, layer) || s < 1 || s >= c->n_scales || eight_bits(c->dtype)) return AMSKV_ERR_INVALID_ARG;
+  if (bad_layer(c, layer) || s < 1 || s >= c->n_scales || coded(c->dtype)) return AMSKV_ERR_INVALID_ARG;
   if (int rc = finish_iteration(c, layer)) return rc;
   LayerState& L = c->layer[layer];
   if (s > L.last_scale) return AMSKV_ERR_ORDER;
@@ -1181,7 +1198,7 @@ int32_t amskv_interscale_similarity_enqueue_static(amskv_cache* c, int32_t layer
 
 int32_t amskv_interscale_similarity_collect(amskv_cache* c, float* cosK_host, float* cosV_host, float* sums_host,
                                             void* stream) try {
-  if (!c || !cosK_host || eight_bits(c->dtype)) return AMSKV_ERR_INVALID_ARG;
+  if (!c || !cosK_host || coded(c->dtype)) return AMSKV_ERR_INVALID_ARG;
   if (!c->arena) return AMSKV_ERR_NO_DEVICE_MEMORY;
   const size_t per_layer = 2 * (size_t)c->heads * 4;
   std::vector<float> host(per_layer * c->layers);
@@ -1214,7 +1231,7 @@ int32_t amskv_interscale_similarity_collect(amskv_cache* c, float* cosK_host, fl
 // is null, inside the arena's workspace; *totals is where, and *table describes the groups.
 static int density_launch(amskv_cache* c, int32_t layer, int32_t s, const void* Q_dev, hipStream_t st, SegTable* table,
                           float** totals, float* out_dev) {
-  if (bad_layer(c, layer) || s < 0 || s >= c->n_scales || !Q_dev || misaligned(Q_dev) || eight_bits(c->dtype))
+  if (bad_layer(c, layer) || s < 0 || s >= c->n_scales || !Q_dev || misaligned(Q_dev) || coded(c->dtype))
     return AMSKV_ERR_INVALID_ARG;
   if (int rc = finish_iteration(c, layer)) return rc;
   LayerState& L = c->layer[layer];
@@ -1345,17 +1362,19 @@ int64_t amskv_cache_bytes_held(const amskv_cache* c, int32_t layer, int32_t incl
   if (bad_layer(c, layer)) return AMSKV_ERR_INVALID_ARG;
   if (int rc = finish_iteration(c, layer)) return rc;
   const LayerState& L = c->layer[layer];
-  int64_t tok = 0, held = 0, blocks = 0;  // held, blocks: of an 8-bit cache
+  int64_t tok = 0, held = 0, blocks = 0;  // held, blocks: of a cache of 8 or 4 bits
   for (const Segment& g : L.segs)
     if (include_current || g.scale != L.last_scale) {
-      if (eight_bits(c->dtype) && g.off >= 0) {
+      if (coded(c->dtype) && g.off >= 0) {
         held += g.len;
         blocks += slot_tokens(c->dtype, g.len) / AMSKV_KV8_BLOCK;
       } else {
         tok += g.len;
       }
     }
-  return 2 * (int64_t)c->batch * c->heads * (held * c->head_dim + blocks * (int64_t)sizeof(float)) +
+  const int64_t codes = four_bits(c->dtype) ? held * (c->head_dim / 2 + c->head_dim / AMSKV_KV4_GROUP)
+                                            : held * c->head_dim + blocks * (int64_t)sizeof(float);
+  return 2 * (int64_t)c->batch * c->heads * codes +
          2 * (int64_t)c->elem_bytes * c->batch * c->heads * c->head_dim * tok;
 }
 
@@ -1379,6 +1398,11 @@ int32_t amskv_cache_export(const amskv_cache* c, int32_t layer, void* K_out_dev,
                                               caller_map(c, L.segs.back().len, c->kv_tok), c->heads, (hipStream_t)stream);
     return e == hipSuccess ? AMSKV_OK : AMSKV_ERR_HIP;
   }
+  if (four_bits(c->dtype)) {
+    hipError_t e = amskv::launch_export_codes4(codes4(c, L), K_out_dev, V_out_dev, c->batch * c->heads, c->head_dim, L.cap, t, ext,
+                                               caller_map(c, L.segs.back().len, c->kv_tok), c->heads, (hipStream_t)stream);
+    return e == hipSuccess ? AMSKV_OK : AMSKV_ERR_HIP;
+  }
   hipError_t e = amskv::launch_export(c->arena + L.k_off, c->arena + L.v_off, K_out_dev, V_out_dev,
                                       c->batch * c->heads, c->head_dim * c->elem_bytes, L.cap, t, ext,
                                       caller_map(c, L.segs.back().len, c->kv_tok), c->heads, (hipStream_t)stream);
@@ -1396,7 +1420,7 @@ int32_t amskv_cache_set_io_layout(amskv_cache* c, int32_t io_layout, int64_t q_t
     const int64_t width = (int64_t)c->heads * c->head_dim, per16 = 16 / c->elem_bytes;
     for (int64_t st : {q_token_stride, kv_token_stride, o_token_stride})
       if (st < width || st % per16 != 0 || st > ((int64_t)1 << 40)) return AMSKV_ERR_INVALID_ARG;
-    if (eight_bits(c->dtype) && kv_token_stride >= (1 << 23)) return AMSKV_ERR_INVALID_ARG;  // 64 rows of a tile by 32-bit offsets
+    if (coded(c->dtype) && kv_token_stride >= (1 << 23)) return AMSKV_ERR_INVALID_ARG;  // 64 rows of a tile by 32-bit offsets
     c->q_tok = q_token_stride;
     c->kv_tok = kv_token_stride;
     c->o_tok = o_token_stride;

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "amskv.h"
 
 namespace amskv {
@@ -296,6 +298,14 @@ struct Codes {
   float *k_scale, *v_scale;
 };
 
+// A layer's K and V in 4 bits: codes [BH][cap][D / 2], and the byte (exponent + 127) that every 32 channels of a row share,
+// [BH][cap][D / 32].  Rows stand by themselves: slots are any tokens.
+struct Codes4 {
+  unsigned char *k, *v, *k_group, *v_group;
+};
+template <int kBits>
+using CodesOf = typename std::conditional<kBits == 8, Codes, Codes4>::type;
+
 // What becomes of a scale's tensors in one launch (take_kernels.hip): Q is turned, K is turned and put in its place, V is put
 // in its place.  A tensor whose source is null is left out.
 struct Take {
@@ -311,7 +321,9 @@ struct Take {
   int32_t rot_dim, pairing, inverse;
   int32_t batch, heads, tokens, head_dim, dtype;  // dtype: of the sources, AMSKV_DTYPE_F32 or _BF16
   bool eight_bits;
-  const MoveList* moves;            // eight_bits: survivors that slide to their new places first (launch_move_codes), or null
+  const MoveList* moves;            // eight_bits, four_bits: survivors that slide to their new places first (launch_move_codes), or null
+  bool four_bits;                   // K and V become codes4 from token dst_new on
+  Codes4 codes4;
 };
 hipError_t launch_take(const Take& t, hipStream_t st) AMSKV_OPTIONAL;
 // The survivors of a compaction slide to their new places (mv in tokens, whole blocks of 16).
@@ -321,6 +333,12 @@ hipError_t launch_export_codes(const Codes& c, void* k_out, void* v_out, int bh,
                                const ExtKV& ext, const RowMap& ext_map, int heads, hipStream_t st) AMSKV_OPTIONAL;
 hipError_t launch_attend_codes(const void* q, void* o, const Codes& c, int bh, int t_q, int head_dim, int64_t cap_tokens,
                                const SegTable& seg, const ExtKV& ext, const CallerIo& io, float softmax_scale, hipStream_t st) AMSKV_OPTIONAL;
+// The same for a cache in 4 bits.
+hipError_t launch_move_codes4(const Codes4& c, int bh, int head_dim, int64_t cap_tokens, const MoveList& mv, hipStream_t st) AMSKV_OPTIONAL;
+hipError_t launch_export_codes4(const Codes4& c, void* k_out, void* v_out, int bh, int head_dim, int64_t cap_tokens, const SegTable& seg,
+                                const ExtKV& ext, const RowMap& ext_map, int heads, hipStream_t st) AMSKV_OPTIONAL;
+hipError_t launch_attend_codes4(const void* q, void* o, const Codes4& c, int bh, int t_q, int head_dim, int64_t cap_tokens,
+                                const SegTable& seg, const ExtKV& ext, const CallerIo& io, float softmax_scale, hipStream_t st) AMSKV_OPTIONAL;
 
 hipError_t launch_rope_table(const double* frequency, int pairs, int axes, double amplitude, const double* positions, int64_t n,
                              float* table, hipStream_t st) AMSKV_OPTIONAL;
@@ -335,10 +353,24 @@ struct CrossCall {
   int64_t kv_rows;
   float softmax_scale;
   float* workspace;                   // null: not split
+  bool four_bits;                     // k and v are held tensors; k_map and v_map are not read
 };
 // Bytes of the workspace that a call of this shape uses (0: none).
 uint64_t cross_workspace_bytes(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) AMSKV_OPTIONAL;
 hipError_t launch_cross(const CrossCall& c, hipStream_t st) AMSKV_OPTIONAL;
+
+// An encoder's K and V and their held forms in 4 bits: a held tensor is codes [units][rows][D / 2], then, behind all of them, the bytes
+// of their groups [units][rows][D / 32]; units are (b, kv head) with `rows` = kv_tokens, or (packed: offsets) kv heads with kv_rows.
+struct HoldCall {
+  void *k, *v;                        // bf16: read by launch_hold, written by launch_unhold; either may be null
+  unsigned char *k_held, *v_held;
+  RowMap k_map, v_map;                // bytes
+  const int32_t *lengths, *offsets;
+  int32_t batch, kv_heads, head_dim, kv_tokens;
+  int64_t kv_rows;
+};
+hipError_t launch_hold(const HoldCall& c, hipStream_t st) AMSKV_OPTIONAL;
+hipError_t launch_unhold(const HoldCall& c, hipStream_t st) AMSKV_OPTIONAL;
 
 // What is wrong with a rotary description for rows of head_dim channels: AMSKV_OK or AMSKV_ERR_INVALID_ARG.
 inline int check_turn(const amskv_rope* r, int head_dim) {

@@ -36,13 +36,14 @@ constexpr float kMaxLag = 6.0f, kTripSum = 1024.0f;
 // the reference before any key: finite, so that a block whose scores are all -inf (products beyond fp32) weighs nothing
 constexpr float kNoKeys = -0x1.fffffep127f;
 
-// Keys of a unit: n8 rows of codes, located by the segment table, then nx rows of bf16 at a fixed stride.
+// Keys of a unit: n_codes rows of codes in 8 or 4 bits, located by the segment table, then n_rows rows of bf16 at a fixed stride.
 struct Keys {
-  const unsigned char *k8, *v8;
-  const float *k_scale, *v_scale;  // of every 16 rows of codes
+  const unsigned char *k_codes, *v_codes;
+  const float *k_scale, *v_scale;  // 8 bits: of every 16 rows of codes
   const char *kx, *vx;
   long long k_tok, v_tok;  // bytes, below 2^24
-  int n8, nx;
+  int n_codes, n_rows;
+  const unsigned char *k_group, *v_group;  // 4 bits: of every 32 channels of a row
 };
 
 // chunk c (16 bytes) of row `row` of a tile sits at chunk c ^ swizzle(row): fragment reads of 32 rows and transposing reads of
@@ -61,38 +62,44 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 __device__ __forceinline__ void settle_mfma(f32x16& acc) { asm volatile("s_nop 11" : "+v"(acc)); }
 
-template <int D, int kTeamWaves, int kTeams, bool kEight>
+// kBits: of an element of the codes that keys may be (8 or 4), or 16: there are none
+template <int D, int kTeamWaves, int kTeams, int kBits>
 struct Unit {
-  static constexpr int RB = 2 * D, KS = D / 16, DB = D / 32, CPR = D / 8, CP8 = D / 16;
+  static constexpr bool kCoded = kBits != 16;
+  static constexpr int RB = 2 * D, KS = D / 16, DB = D / 32, CPR = D / 8;
   static_assert(kTeamWaves == 1 || kTeams == 1, "a team of several waves has the workgroup to itself");
   static constexpr int kTile = kTeamWaves == 8 ? 64 : 32;
   static constexpr int kStages = 4;
   static constexpr bool kAlone = kTeamWaves == 8 && D == 128;  // 128 KB of LDS
   static constexpr int kThreads = 64 * kTeamWaves;
-  static constexpr int kItems = 2 * kTile * CPR / kThreads, kItems8 = kItems / 2;
+  // a piece of codes: 16 of 8 bits, or a quarter of a row of 4 bits (a wave by itself: 32)
+  static constexpr int kPiece = kBits == 8 ? 16 : kTeamWaves == 1 ? 32 : D / 4, kPieces = D / kPiece;
+  static constexpr int kItems = 2 * kTile * CPR / kThreads, kItemsC = kTeamWaves == 1 ? 2 * kTile * kPieces / 64 : kBits == 8 ? kItems / 2 : 1;
   // rows from a thread's piece to its next one of the same tensor; with one piece of codes, half of the waves bring K and half V
-  static constexpr int kStep = kThreads / CPR, kStep8 = kItems8 == 1 ? kTile : 2 * kStep;
-  static constexpr int kRows8 = kItems8 == 1 ? 1 : kItems8 / 2;
+  static constexpr int kStep = kThreads / CPR, kStepC = kItemsC == 1 ? kTile : 2 * kStep;
+  static constexpr int kRowsC = kItemsC == 1 ? 1 : kItemsC / 2;
   static constexpr int kTensor = kTile * RB, kStage = 2 * kTensor;
   // a wave by itself has a block of V there; afterwards teams park their O^T
   static constexpr int kTeamLds = kTeamWaves > 1 ? kStages * kStage : kTeams > 1 ? 32 * D * 4 : kTensor;
   static constexpr int kLds = kTeams * kTeamLds;
   static constexpr int kRows = 32 * kTeamWaves;
   // K fragments of the next block are asked for while the softmax of this one runs, where there are registers for them
-  static constexpr bool kAhead = D == 128 || !kEight;
+  static constexpr bool kAhead = D == 128 || !kCoded;
   static_assert(kTeams == 1 || kTeamLds >= kTeamWaves * 32 * D * 4, "a wave parks its O^T in its share of the tiles");
 
-  // A thread's part of a tile: 16 bytes each of 8 bf16 channels (kItems of them, the first half K) or of 16 codes (kItems8).
+  // A thread's part of a tile: 16 bytes each of 8 bf16 channels (kItems of them, the first half K) or pieces of codes (kItemsC) with
+  // their powers of two (8 bits: as fp32; 4 bits: as bytes).
+  typedef typename std::conditional<kBits == 4, unsigned, float>::type Scale;
   struct Staged {
     u32x4 x[kItems];
-    float scale[kEight ? kItems8 : 1];
+    Scale scale[kCoded ? kItemsC : 1];
   };
   // Where the pieces of the next tile lie: uniform bases of bf16 rows, and a row per piece.  Found at the top of a tile, so that the table walk at
   // a segment's end does not stand between matrix instructions.
   struct Aim {
     const char *kb, *vb;
     unsigned k_step, v_step;     // bytes from row to row
-    unsigned row[kItems / 2];    // (of codes: the first kRows8)
+    unsigned row[kItems / 2];    // (of codes: the first kRowsC)
     int end = 0, delta = 0;      // codes: segment of the tile's first row, its end, from virtual row to row
   };
   // Kinds of tile a loop meets: kAny is found out (uniformly), kCodes and kRows are known.
@@ -103,15 +110,15 @@ struct Unit {
   };
   template <Kind kKind>
   __device__ static __forceinline__ bool is_codes(const Keys& k, int it) {
-    return kEight && (kKind == kCodes || (kKind == kAny && it < tiles8(k)));
+    return kCoded && (kKind == kCodes || (kKind == kAny && it < tiles_of_codes(k)));
   }
 
-  // tiles [0, tiles8) are codes, [tiles8, tiles) bf16 rows
-  __device__ static __forceinline__ int tiles8(const Keys& k) { return kEight ? (k.n8 + kTile - 1) / kTile : 0; }
-  __device__ static __forceinline__ int tiles(const Keys& k) { return tiles8(k) + (k.nx + kTile - 1) / kTile; }
+  // tiles [0, tiles_of_codes) are codes, [tiles_of_codes, tiles) bf16 rows
+  __device__ static __forceinline__ int tiles_of_codes(const Keys& k) { return kCoded ? (k.n_codes + kTile - 1) / kTile : 0; }
+  __device__ static __forceinline__ int tiles(const Keys& k) { return tiles_of_codes(k) + (k.n_rows + kTile - 1) / kTile; }
   __device__ static __forceinline__ int valid(const Keys& k, int it) {
-    const int t8 = tiles8(k);
-    return kEight && it < t8 ? min(kTile, k.n8 - it * kTile) : min(kTile, k.nx - (it - t8) * kTile);
+    const int t8 = tiles_of_codes(k);
+    return kCoded && it < t8 ? min(kTile, k.n_codes - it * kTile) : min(kTile, k.n_rows - (it - t8) * kTile);
   }
 
   // `member`: thread inside the team.  (Through an empty asm, so that what is derived from it is not kept in registers from
@@ -121,14 +128,14 @@ struct Unit {
     return x;
   }
   // row inside a tile of a thread's first piece of codes, its channel group, and whether it is V's (one piece: by the wave)
-  __device__ static __forceinline__ bool is_v8(int i, int member) {
-    return kItems8 == 1 ? __builtin_amdgcn_readfirstlane(member) >= kThreads / 2 : i >= kItems8 / 2;
+  __device__ static __forceinline__ bool is_vC(int i, int member) {
+    return kItemsC == 1 ? __builtin_amdgcn_readfirstlane(member) >= kThreads / 2 : i >= kItemsC / 2;
   }
-  __device__ static __forceinline__ int member8(int member) { return kItems8 == 1 ? member & (kThreads / 2 - 1) : member; }
+  __device__ static __forceinline__ int memberC(int member) { return kItemsC == 1 ? member & (kThreads / 2 - 1) : member; }
   template <Kind kKind>
   __device__ static __forceinline__ void aim(Aim& a, const Keys& k, const SegTable& seg, int it, int member) {
     const bool codes = is_codes<kKind>(k, it);  // uniform
-    const int first = (codes ? it : it - tiles8(k)) * kTile, last = (codes ? k.n8 : k.nx) - 1;
+    const int first = (codes ? it : it - tiles_of_codes(k)) * kTile, last = (codes ? k.n_codes : k.n_rows) - 1;
     member = fresh(member);
     if (codes) {
       if (first >= a.end)  // a handful of times: the segment that holds `first`
@@ -137,13 +144,13 @@ struct Unit {
             a.end = seg.virt_start[g] + seg.len[g];
             a.delta = seg.phys_off[g] - seg.virt_start[g];
           }
-      const int row0 = first + member8(member) / CP8;
+      const int row0 = first + memberC(member) / kPieces;
 #pragma unroll
-      for (int i = 0; i < kRows8; ++i) a.row[i] = min(row0 + i * kStep8, last) + a.delta;
+      for (int i = 0; i < kRowsC; ++i) a.row[i] = min(row0 + i * kStepC, last) + a.delta;
       if (min(first + kTile - 1, last) >= a.end) {  // rows of several segments
 #pragma unroll
-        for (int i = 0; i < kRows8; ++i) {
-          const int j = min(row0 + i * kStep8, last);
+        for (int i = 0; i < kRowsC; ++i) {
+          const int j = min(row0 + i * kStepC, last);
           for (int g = 0; g < seg.n; ++g)
             if (j >= seg.virt_start[g]) a.row[i] = j + seg.phys_off[g] - seg.virt_start[g];
         }
@@ -162,13 +169,25 @@ struct Unit {
   __device__ static __forceinline__ void fetch(Staged& s, const Aim& a, const Keys& k, int it, int member) {
     member = fresh(member);
     if (is_codes<kKind>(k, it)) {
-      const unsigned in_row = 16 * (member8(member) % CP8);
+      const unsigned piece = memberC(member) % kPieces;
 #pragma unroll
-      for (int i = 0; i < kItems8; ++i) {
-        const bool v = is_v8(i, member);
-        const unsigned row = a.row[kItems8 == 1 ? 0 : i % kRows8];
-        s.x[i] = *reinterpret_cast<const u32x4*>((v ? k.v8 : k.k8) + (row * D + in_row));
-        s.scale[i] = (v ? k.v_scale : k.k_scale)[row / AMSKV_KV8_BLOCK];
+      for (int i = 0; i < kItemsC; ++i) {
+        const bool v = is_vC(i, member);
+        const unsigned row = a.row[kItemsC == 1 ? 0 : i % kRowsC];
+        const unsigned char* from = (v ? k.v_codes : k.k_codes) + (row * (D * kBits / 8) + kPiece * kBits / 8 * piece);
+        if constexpr (kBits == 4) {
+          if constexpr (D == 64) {
+            const u32x2 x = *reinterpret_cast<const u32x2*>(from);
+            s.x[i][0] = x[0];
+            s.x[i][1] = x[1];
+          } else {
+            s.x[i] = *reinterpret_cast<const u32x4*>(from);
+          }
+          s.scale[i] = (v ? k.v_group : k.k_group)[row * (D / AMSKV_KV4_GROUP) + piece * kPiece / AMSKV_KV4_GROUP];
+        } else {
+          s.x[i] = *reinterpret_cast<const u32x4*>(from);
+          s.scale[i] = (v ? k.v_scale : k.k_scale)[row / AMSKV_KV8_BLOCK];
+        }
       }
       return;
     }
@@ -185,20 +204,30 @@ struct Unit {
     fetch<kKind>(s, a, k, it, member);
   }
 
+  // a piece of codes as bf16, 8 channels to a chunk; chunk j of it at `to` ^ 16 j
+  __device__ static __forceinline__ void put_piece(char* lds, int to, const u32x4& x, Scale scale) {
+    if constexpr (kBits == 4) {
+      const float by = power_of_byte(scale);
+#pragma unroll
+      for (int j = 0; j < kPiece / 8; ++j) *reinterpret_cast<u32x4*>(lds + (to ^ (16 * j))) = values4(x[j], by);
+    } else {
+      *reinterpret_cast<u32x4*>(lds + to) = values8(u32x2{x[0], x[1]}, scale);
+      *reinterpret_cast<u32x4*>(lds + (to ^ 16)) = values8(u32x2{x[2], x[3]}, scale);
+    }
+  }
   // `lds`: byte offset of the tile.  (Offsets of a lane's pieces differ from the first one's by a constant and by the flip of
   // address bits that the swizzle of a constant number of rows makes -- swizzle() moves bits, so the swizzles of bits apart add up.)
   template <Kind kKind>
   __device__ static __forceinline__ void store(const Staged& s, char* lds_all, int lds, const Keys& k, int it, int member) {
     member = fresh(member);
     if (is_codes<kKind>(k, it)) {
-      const int m = member8(member), row = m / CP8, c = 2 * (m % CP8), at = lds + row * RB + 16 * (c ^ swizzle<D>(row));
+      const int m = memberC(member), row = m / kPieces, c = kPiece / 8 * (m % kPieces), at = lds + row * RB + 16 * (c ^ swizzle<D>(row));
 #pragma unroll
-      for (int i = 0; i < kItems8; ++i) {
-        const int n = kItems8 == 1 ? 0 : i % kRows8;
-        const int to = (at ^ (16 * swizzle<D>(n * kStep8))) + n * kStep8 * RB;
-        const int tensor = is_v8(i, member) ? kTensor : 0;
-        *reinterpret_cast<u32x4*>(lds_all + to + tensor) = values8(u32x2{s.x[i][0], s.x[i][1]}, s.scale[i]);
-        *reinterpret_cast<u32x4*>(lds_all + (to ^ 16) + tensor) = values8(u32x2{s.x[i][2], s.x[i][3]}, s.scale[i]);
+      for (int i = 0; i < kItemsC; ++i) {
+        const int n = kItemsC == 1 ? 0 : i % kRowsC;
+        const int to = (at ^ (16 * swizzle<D>(n * kStepC))) + n * kStepC * RB;
+        const int tensor = is_vC(i, member) ? kTensor : 0;
+        put_piece(lds_all + tensor, to, s.x[i], s.scale[i]);
       }
       return;
     }
@@ -325,7 +354,7 @@ struct Unit {
   // Codes at head dim 128: the first block, which has none before it, is no question but weights of 0 for what lies in its
   // slot, and O^T follows at once: one basic block from K to the weights (both sides on one card: 64 units 2304 x 3925 363 -> 349 us, 32
   // units 209 -> 196, 4096 x 6421 808 -> 784).  Elsewhere walks are short for four products more, and their registers (head dim 64, 256 x 530 188 -> 193).
-  static constexpr bool kOneBlock = D == 128 && kEight;
+  static constexpr bool kOneBlock = D == 128 && kCoded;
   struct Behind {
     bf16x8 pf[2];
     float alpha;
@@ -392,37 +421,46 @@ struct Unit {
   // are taken in the same order (q_at), which the sum over channels does not mind.  V goes through LDS, where it is transposed.
   struct Brought {
     u32x4 k[KS], v[kItems / 2];
-    float k_scale, v_scale[kEight ? kItems8 / 2 : 1];
+    Scale k_scale[D / 64], v_scale[kCoded ? kItemsC / 2 : 1];  // (8 bits: K's row has one)
   };
   // byte offset in a row of Q (and of bf16 K, for a wave by itself) of fragment t
-  static constexpr bool kHalves = kTeamWaves == 1 && kEight;
+  static constexpr bool kHalves = kTeamWaves == 1 && kCoded;
   __device__ static __forceinline__ int q_at(int t, int h) { return kHalves ? h * D + 16 * t : 32 * t + 16 * h; }
   template <bool kCodesNow>
   __device__ static __forceinline__ void bring(Brought& n, const Keys& k, const SegTable& seg, int it, int lane) {
     const int r = lane & 31, h = lane >> 5;
     if constexpr (kCodesNow) {
-      const int first = it * kTile, last = k.n8 - 1;
-      constexpr int kV = kItems8 / 2, kVStep = 64 / CP8;
+      const int first = it * kTile, last = k.n_codes - 1;
+      constexpr int kV = kItemsC / 2, kVStep = 64 / kPieces;
       // rows of the lane's pieces, K's and V's, in one walk of the table
       int row[kV + 1], at[kV + 1];
 #pragma unroll
-      for (int i = 0; i <= kV; ++i) row[i] = at[i] = min(first + (i < kV ? i * kVStep + lane / CP8 : r), last);
+      for (int i = 0; i <= kV; ++i) row[i] = at[i] = min(first + (i < kV ? i * kVStep + lane / kPieces : r), last);
       for (int g = 0; g < seg.n; ++g) {
         const int from = seg.virt_start[g], by = seg.phys_off[g] - seg.virt_start[g];
 #pragma unroll
         for (int i = 0; i <= kV; ++i) row[i] = at[i] >= from ? at[i] + by : row[i];
       }
-      const unsigned k_from = (unsigned)row[kV] * D + h * (D / 2);
+      constexpr int kRowBytes = D * kBits / 8, kGroups = D / AMSKV_KV4_GROUP;
+      const unsigned k_from = (unsigned)row[kV] * kRowBytes + h * (kRowBytes / 2);
 #pragma unroll
-      for (int i = 0; i < KS / 2; ++i) n.k[i] = *reinterpret_cast<const u32x4*>(k.k8 + (k_from + 16 * i));
-      n.k_scale = k.k_scale[(unsigned)row[kV] / AMSKV_KV8_BLOCK];
+      for (int i = 0; i < kRowBytes / 32; ++i) n.k[i] = *reinterpret_cast<const u32x4*>(k.k_codes + (k_from + 16 * i));
+      if constexpr (kBits == 4) {
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) n.k_scale[i] = k.k_group[(unsigned)row[kV] * kGroups + h * (kGroups / 2) + i];
+      } else {
+        n.k_scale[0] = k.k_scale[(unsigned)row[kV] / AMSKV_KV8_BLOCK];
+      }
 #pragma unroll
       for (int i = 0; i < kV; ++i) {
-        n.v[i] = *reinterpret_cast<const u32x4*>(k.v8 + ((unsigned)row[i] * D + 16 * (lane % CP8)));
-        n.v_scale[i] = k.v_scale[(unsigned)row[i] / AMSKV_KV8_BLOCK];
+        n.v[i] = *reinterpret_cast<const u32x4*>(k.v_codes + ((unsigned)row[i] * kRowBytes + 16 * (lane % kPieces)));
+        if constexpr (kBits == 4)
+          n.v_scale[i] = k.v_group[(unsigned)row[i] * kGroups + lane % kPieces];
+        else
+          n.v_scale[i] = k.v_scale[(unsigned)row[i] / AMSKV_KV8_BLOCK];
       }
     } else {
-      const int first = (it - tiles8(k)) * kTile, last = k.nx - 1;
+      const int first = (it - tiles_of_codes(k)) * kTile, last = k.n_rows - 1;
       const char *kb = k.kx + first * k.k_tok, *vb = k.vx + first * k.v_tok;
       const unsigned k_from = (unsigned)min(r, last - first) * (unsigned)k.k_tok;
 #pragma unroll
@@ -435,16 +473,19 @@ struct Unit {
   template <bool kCodesNow>
   __device__ static __forceinline__ void put_down(const Brought& n, bf16x8 (&kf)[KS], char* lds, int lane) {
     if constexpr (kCodesNow) {
-      constexpr int kVStep = 64 / CP8;
-      const int row = lane / CP8, c = 2 * (lane % CP8), at = row * RB + 16 * (c ^ swizzle<D>(row));
+      constexpr int kVStep = 64 / kPieces;
+      const int row = lane / kPieces, c = kPiece / 8 * (lane % kPieces), at = row * RB + 16 * (c ^ swizzle<D>(row));
 #pragma unroll
-      for (int i = 0; i < KS; ++i)
-        kf[i] = __builtin_bit_cast(bf16x8, values8(u32x2{n.k[i / 2][2 * (i & 1)], n.k[i / 2][2 * (i & 1) + 1]}, n.k_scale));
+      for (int i = 0; i < KS; ++i) {
+        if constexpr (kBits == 4)
+          kf[i] = __builtin_bit_cast(bf16x8, values4(n.k[i / 4][i % 4], power_of_byte(n.k_scale[i / 4])));
+        else
+          kf[i] = __builtin_bit_cast(bf16x8, values8(u32x2{n.k[i / 2][2 * (i & 1)], n.k[i / 2][2 * (i & 1) + 1]}, n.k_scale[0]));
+      }
 #pragma unroll
-      for (int i = 0; i < kItems8 / 2; ++i) {
+      for (int i = 0; i < kItemsC / 2; ++i) {
         const int to = (at ^ (16 * swizzle<D>(i * kVStep))) + i * kVStep * RB;
-        *reinterpret_cast<u32x4*>(lds + to) = values8(u32x2{n.v[i][0], n.v[i][1]}, n.v_scale[i]);
-        *reinterpret_cast<u32x4*>(lds + (to ^ 16)) = values8(u32x2{n.v[i][2], n.v[i][3]}, n.v_scale[i]);
+        put_piece(lds, to, n.v[i], n.v_scale[i]);
       }
     } else {
       constexpr int kVStep = 64 / CPR;
@@ -458,8 +499,8 @@ struct Unit {
   __device__ static __forceinline__ void alone(Result& x, const bf16x8 (&qf)[KS], char* lds, const Keys& k, const SegTable& seg, int it, int to,
                                                float c, int lane) {
     Brought n;
-    const int t8 = min(tiles8(k), to), va = v_lane(lane) - kTensor;
-    if (kEight && it < t8) bring<kEight>(n, k, seg, it, lane);
+    const int t8 = min(tiles_of_codes(k), to), va = v_lane(lane) - kTensor;
+    if (kCoded && it < t8) bring<kCoded>(n, k, seg, it, lane);
     else if (it < to) bring<false>(n, k, seg, it, lane);
     settle(qf);
     auto block = [&](auto now, auto next, bool more) {
@@ -480,7 +521,7 @@ struct Unit {
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
       it += kTeams;
     };
-    if constexpr (kEight) {
+    if constexpr (kCoded) {
       while (it + kTeams < t8) block(Of<kCodes>{}, Of<kCodes>{}, true);
       if (it < t8) block(Of<kCodes>{}, Of<kRowsOnly>{}, it + kTeams < to);
     }
@@ -569,8 +610,8 @@ struct Unit {
             next_tile();
           }
         };
-        const int t8 = min(tiles8(k), to);
-        if constexpr (kEight) known(Of<kCodes>{}, t8);
+        const int t8 = min(tiles_of_codes(k), to);
+        if constexpr (kCoded) known(Of<kCodes>{}, t8);
         while (it < to) {
           if (it - 1 >= t8 || (it >= t8 && it == from)) known(Of<kRowsOnly>{}, to);
           if (it + 3 < to) aim<kRowsOnly>(to_come, k, seg, it + 3, member);  // (codes: all brought above)

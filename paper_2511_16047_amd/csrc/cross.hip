@@ -24,6 +24,8 @@ struct CrossArgs {
   long long kv_rows;
   float* workspace;
   float scale_log2e;
+  long long held_rows;  // 4 bits: rows of a unit of the held tensors, and where the bytes of their groups begin
+  long long groups_at;
   int kv_heads, group, q_tokens, kv_tokens, n_units, row_tiles, splits, n_whole;
 };
 
@@ -38,10 +40,10 @@ __device__ __forceinline__ int states(const CrossArgs& a, unsigned b, long long&
   return a.lengths != nullptr ? min(max(a.lengths[b], 0), a.kv_tokens) : a.kv_tokens;
 }
 
-template <int D, int kTeamWaves, int kTeams, int kMinWavesPerSimd>
+template <int D, int kTeamWaves, int kTeams, int kMinWavesPerSimd, int kBits>
 __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cross_kernel(CrossArgs a) {
   fetch_arguments<sizeof(CrossArgs)>();
-  using U = rows::Unit<D, kTeamWaves, kTeams, false>;
+  using U = rows::Unit<D, kTeamWaves, kTeams, kBits>;
   __shared__ __align__(1024) char lds[U::kLds];
   const int tiles = a.row_tiles * a.splits;
   Place at{(int)blockIdx.x, 0};
@@ -66,9 +68,22 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
 #pragma unroll
   for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + U::q_at(t, h));
 
-  const long long kb = a.offsets ? first * a.k_map.tok : b * a.k_map.batch, vb = a.offsets ? first * a.v_map.tok : b * a.v_map.batch;
-  const rows::Keys keys{nullptr, nullptr, nullptr, nullptr, a.k + kb + g * a.k_map.head, a.v + vb + g * a.v_map.head,
-                        a.k_map.tok, a.v_map.tok, 0, n};
+  rows::Keys keys{};
+  if constexpr (kBits == 16) {
+    const long long kb = a.offsets ? first * a.k_map.tok : b * a.k_map.batch, vb = a.offsets ? first * a.v_map.tok : b * a.v_map.batch;
+    keys.kx = a.k + kb + g * a.k_map.head;
+    keys.vx = a.v + vb + g * a.v_map.head;
+    keys.k_tok = a.k_map.tok;
+    keys.v_tok = a.v_map.tok;
+    keys.n_rows = n;
+  } else {
+    const long long row = a.offsets ? g * a.held_rows + first : (long long)at.bh * a.held_rows;
+    keys.k_codes = (const unsigned char*)a.k + row * (D / 2);
+    keys.v_codes = (const unsigned char*)a.v + row * (D / 2);
+    keys.k_group = (const unsigned char*)a.k + a.groups_at + row * (D / AMSKV_KV4_GROUP);
+    keys.v_group = (const unsigned char*)a.v + a.groups_at + row * (D / AMSKV_KV4_GROUP);
+    keys.n_codes = n;
+  }
   const int n_tiles = U::tiles(keys), each = (n_tiles + a.splits - 1) / a.splits;
   const int from = min(split * each, n_tiles), to = min(from + each, n_tiles);
   typename U::Result x;
@@ -137,13 +152,13 @@ __global__ __launch_bounds__(256) void cross_meet_kernel(CrossArgs a, int rows_o
   *reinterpret_cast<rows::bf16x4*>(a.o + b * a.o_map.batch + ((long long)g * a.group + head) * a.o_map.head + token * a.o_map.tok + 8 * c) = w;
 }
 
-template <int D, int kTeamWaves, int kTeams, int kMinWavesPerSimd>
+template <int D, int kTeamWaves, int kTeams, int kMinWavesPerSimd, int kBits = 16>
 hipError_t go(CrossArgs& a, hipStream_t st) {
   const int n_rows = a.group * a.q_tokens;
   a.row_tiles = (n_rows + 32 * kTeamWaves - 1) / (32 * kTeamWaves);
   const int tiles = a.row_tiles * a.splits;
   a.n_whole = whole_units(a.n_units, tiles, kMostWhole);
-  hipLaunchKernelGGL((cross_kernel<D, kTeamWaves, kTeams, kMinWavesPerSimd>), dim3(tiles == 1 ? a.n_units : placed_grid(a.n_units, tiles, a.n_whole)),
+  hipLaunchKernelGGL((cross_kernel<D, kTeamWaves, kTeams, kMinWavesPerSimd, kBits>), dim3(tiles == 1 ? a.n_units : placed_grid(a.n_units, tiles, a.n_whole)),
                      dim3(64 * kTeamWaves * kTeams), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
@@ -183,9 +198,22 @@ hipError_t launch_cross(const CrossCall& c, hipStream_t st) {
   a.q_tokens = c.q_tokens;
   a.kv_tokens = c.kv_tokens;
   a.n_units = c.batch * c.kv_heads;
+  if (c.four_bits) {
+    const long long units = c.offsets ? c.kv_heads : a.n_units;
+    a.held_rows = c.offsets ? c.kv_rows : c.kv_tokens;
+    a.groups_at = units * a.held_rows * (c.head_dim / 2);
+  }
   if (a.n_units == 0 || a.group * a.q_tokens == 0) return hipSuccess;
   const rows::Division d = rows::divide(c.head_dim, a.n_units, a.group * a.q_tokens, a.kv_tokens);
   a.splits = a.workspace ? d.splits : 1;
+  if (c.four_bits) {
+    if (c.head_dim == 64) {
+      if (d.team_waves == 1) return d.teams == 1 ? go<64, 1, 1, 3, 4>(a, st) : go<64, 1, 4, 3, 4>(a, st);
+      return d.team_waves == 4 ? go<64, 4, 1, 4, 4>(a, st) : go<64, 8, 1, 4, 4>(a, st);
+    }
+    if (d.team_waves == 1) return d.teams == 1 ? go<128, 1, 1, 2, 4>(a, st) : go<128, 1, 4, 2, 4>(a, st);
+    return go<128, 4, 1, 2, 4>(a, st);
+  }
   if (c.head_dim == 64) {
     if (d.team_waves == 1) return d.teams == 1 ? go<64, 1, 1, 4>(a, st) : go<64, 1, 4, 4>(a, st);
     return d.team_waves == 4 ? go<64, 4, 1, 4>(a, st) : go<64, 8, 1, 4>(a, st);

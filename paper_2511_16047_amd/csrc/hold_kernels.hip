@@ -1,0 +1,131 @@
+// An encoder's K and V put into 4 bits, and read back (codes.hpp has the format; the attention over them is cross.hip).
+//
+// A lane has 8 channels of a row: 16 bytes of bf16, 4 bytes of codes, and a group's 4 lanes are a quad, so its largest element takes two
+// steps on the vector ALU.  A wave's lanes follow the rows of one unit, whose codes lie back to back; a lane has kRows of them under way.
+// Bound: HBM.
+#include "codes.hpp"
+
+namespace amskv {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kRows = 4;               // rows of a lane under way
+constexpr long long kMostGroups = 1 << 20;  // workgroups; beyond that they take several blocks of rows
+
+struct HoldArgs {
+  char *x[2];
+  unsigned char* held[2];
+  RowMap map[2];
+  const int *lengths, *offsets;
+  long long rows, units, blocks, groups_at;  // rows of a unit, blocks of rows to a unit, bytes of codes
+  int kv_heads, batch, kv_tokens;
+};
+
+// rows [first, end) of a unit that hold states
+__device__ __forceinline__ void live_rows(const HoldArgs& a, long long unit, long long& first, long long& end) {
+  first = 0;
+  end = a.rows;
+  if (a.offsets != nullptr) {
+    first = min(max((long long)a.offsets[0], 0ll), a.rows);
+    end = min(max((long long)a.offsets[a.batch], 0ll), a.rows);
+  } else if (a.lengths != nullptr) {
+    end = min(max(a.lengths[unit / a.kv_heads], 0), a.kv_tokens);
+  }
+}
+
+// the largest of a quad's four values
+__device__ __forceinline__ float quad_max(float m) {
+  m = fmaxf(m, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(m), 0xB1, 0xf, 0xf, true)));  // quad_perm 1 0 3 2
+  return fmaxf(m, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(m), 0x4E, 0xf, 0xf, true)));  // 2 3 0 1
+}
+
+template <int D, bool kBack>
+__global__ __launch_bounds__(256) void hold_kernel(HoldArgs a) {
+  constexpr int kLanes = D / 8, kAtOnce = 256 / kLanes;  // lanes of a row, rows of a workgroup at a time
+  const int tensor = blockIdx.y;
+  if (a.x[tensor] == nullptr) return;
+  const int c = threadIdx.x % kLanes, r = threadIdx.x / kLanes;
+  const RowMap& m = a.map[tensor];
+  for (long long block = blockIdx.x; block < a.units * a.blocks; block += gridDim.x) {
+    const long long unit = block / a.blocks, row0 = (block - unit * a.blocks) * (kAtOnce * kRows) + r;
+    long long first, end;
+    live_rows(a, unit, first, end);
+    const long long b = a.offsets != nullptr ? 0 : unit / a.kv_heads, g = unit - b * a.kv_heads;
+    char* x = a.x[tensor] + b * m.batch + g * m.head + 16 * c;
+    unsigned char* codes = a.held[tensor] + unit * a.rows * (D / 2) + 4 * c;
+    unsigned char* groups = a.held[tensor] + a.groups_at + unit * a.rows * (D / AMSKV_KV4_GROUP) + c / 4;
+    auto live = [&](int i) {
+      const long long row = row0 + i * kAtOnce;
+      return row >= first && row < end;
+    };
+    if constexpr (kBack) {
+      unsigned in[kRows], byte[kRows];
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (live(i)) {
+          const long long row = row0 + i * kAtOnce;
+          in[i] = *reinterpret_cast<const unsigned*>(codes + row * (D / 2));
+          byte[i] = groups[row * (D / AMSKV_KV4_GROUP)];
+        }
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (live(i)) *reinterpret_cast<u32x4*>(x + (row0 + i * kAtOnce) * m.tok) = values4(in[i], power_of_byte(byte[i]));
+    } else {
+      bf16x8 in[kRows];
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        in[i] = {};
+        if (live(i)) in[i] = *reinterpret_cast<const bf16x8*>(x + (row0 + i * kAtOnce) * m.tok);
+      }
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        float y[8], largest = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          y[e] = (float)in[i][e];
+          largest = fmaxf(largest, fabsf(y[e]));
+        }
+        const unsigned byte = group_exponent(quad_max(largest)) + 127;
+        if (live(i)) {
+          const long long row = row0 + i * kAtOnce;
+          *reinterpret_cast<unsigned*>(codes + row * (D / 2)) = codes4(y, power_of_byte(byte));
+          if (c % 4 == 0) groups[row * (D / AMSKV_KV4_GROUP)] = (unsigned char)byte;
+        }
+      }
+    }
+  }
+}
+
+template <bool kBack>
+hipError_t go(const HoldCall& c, hipStream_t st) {
+  HoldArgs a{};
+  a.x[0] = (char*)c.k;
+  a.x[1] = (char*)c.v;
+  a.held[0] = c.k_held;
+  a.held[1] = c.v_held;
+  a.map[0] = c.k_map;
+  a.map[1] = c.v_map;
+  a.lengths = c.lengths;
+  a.offsets = c.offsets;
+  a.rows = c.offsets ? c.kv_rows : c.kv_tokens;
+  a.units = c.offsets ? c.kv_heads : (long long)c.batch * c.kv_heads;
+  a.groups_at = a.units * a.rows * (c.head_dim / 2);
+  a.kv_heads = c.kv_heads;
+  a.batch = c.batch;
+  a.kv_tokens = c.kv_tokens;
+  const int per = 256 / (c.head_dim / 8) * kRows;
+  a.blocks = (a.rows + per - 1) / per;
+  if (a.units * a.blocks == 0) return hipSuccess;
+  const dim3 grid((unsigned)(a.units * a.blocks < kMostGroups ? a.units * a.blocks : kMostGroups), 2);
+  auto kernel = c.head_dim == 64 ? hold_kernel<64, kBack> : hold_kernel<128, kBack>;
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_hold(const HoldCall& c, hipStream_t st) { return go<false>(c, st); }
+hipError_t launch_unhold(const HoldCall& c, hipStream_t st) { return go<true>(c, st); }
+
+}  // namespace amskv

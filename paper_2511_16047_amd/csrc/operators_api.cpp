@@ -1,4 +1,4 @@
-// C ABI of the calls that need no cache: rotary tables, turning a tensor, cross attention.  Checks and the conversion of
+// C ABI of the calls that need no cache: rotary tables, turning a tensor, cross attention, encoder states in 4 bits.  Checks and the conversion of
 // strides to bytes; everything else is in the kernels' files.
 #include <algorithm>
 #include <cmath>
@@ -44,7 +44,7 @@ bool positive(double x) { return std::isfinite(x) && x > 0; }
 int check_cross(const amskv_cross* x) {
   if (!x || x->batch < 0 || x->heads < 0 || x->kv_heads < 0 || x->q_tokens < 0 || x->kv_tokens < 0) return AMSKV_ERR_INVALID_ARG;
   if (x->head_dim != 64 && x->head_dim != 128) return AMSKV_ERR_INVALID_ARG;
-  if (x->dtype != AMSKV_DTYPE_BF16 || !(x->softmax_scale >= 0.f) || !std::isfinite(x->softmax_scale)) return AMSKV_ERR_INVALID_ARG;
+  if ((x->dtype != AMSKV_DTYPE_BF16 && x->dtype != AMSKV_DTYPE_BF16_KV4) || !(x->softmax_scale >= 0.f) || !std::isfinite(x->softmax_scale)) return AMSKV_ERR_INVALID_ARG;
   if (x->heads > 0 && (x->kv_heads == 0 || x->heads % x->kv_heads != 0)) return AMSKV_ERR_INVALID_ARG;
   // grids count (b, head, block of rows) in 32 bits, rows of a unit too
   if ((int64_t)x->batch * x->heads > (1 << 24) || x->q_tokens > (1 << 22) || x->kv_tokens > (1 << 26)) return AMSKV_ERR_INVALID_ARG;
@@ -56,6 +56,54 @@ int check_cross(const amskv_cross* x) {
     if ((int64_t)x->batch * x->kv_heads * ((rows + 31) / 32) > (1 << 26) - 8) return AMSKV_ERR_INVALID_ARG;
   }
   return AMSKV_OK;
+}
+
+// Bytes of a held tensor of this shape in 4 bits.
+int64_t held_bytes(const amskv_cross* x, bool packed) {
+  const int64_t units = packed ? x->kv_heads : (int64_t)x->batch * x->kv_heads;
+  return units * (packed ? x->kv_rows : x->kv_tokens) * (x->head_dim / 2 + x->head_dim / AMSKV_KV4_GROUP);
+}
+
+// The shape of a call about held tensors, and where the batch elements' states are.
+int check_held(const amskv_cross* x, const int32_t* lengths_dev, const int32_t* offsets_dev) {
+  if (int rc = check_cross(x)) return rc;
+  if (x->dtype != AMSKV_DTYPE_BF16_KV4) return AMSKV_ERR_INVALID_ARG;
+  if ((lengths_dev && offsets_dev) || ((uintptr_t)lengths_dev & 3) != 0 || ((uintptr_t)offsets_dev & 3) != 0) return AMSKV_ERR_INVALID_ARG;
+  if (offsets_dev && (x->kv_rows < 0 || x->kv_rows > INT32_MAX)) return AMSKV_ERR_INVALID_ARG;
+  if ((int64_t)x->batch * x->kv_heads > (1 << 24)) return AMSKV_ERR_INVALID_ARG;  // (heads may be 0)
+  return AMSKV_OK;
+}
+
+// Both directions between bf16 states and held tensors.
+int hold(const amskv_cross* x, const void* k, const void* v, const void* k_held, const void* v_held, const int32_t* lengths_dev,
+         const int32_t* offsets_dev, bool back, void* stream) {
+  if (int rc = check_held(x, lengths_dev, offsets_dev)) return rc;
+  const int64_t n[3] = {offsets_dev ? 1 : x->batch, x->kv_heads, offsets_dev ? x->kv_rows : x->kv_tokens};
+  amskv::HoldCall c{};
+  // (the strides of a tensor that is left out are not looked at)
+  if ((k && !map_of(&x->k, n, x->head_dim, 2, back, &c.k_map)) || (v && !map_of(&x->v, n, x->head_dim, 2, back, &c.v_map)))
+    return AMSKV_ERR_INVALID_ARG;
+  if (misaligned(k) || misaligned(v) || misaligned(k_held) || misaligned(v_held)) return AMSKV_ERR_INVALID_ARG;
+  if (held_bytes(x, offsets_dev != nullptr) == 0 || (offsets_dev && x->batch == 0)) return AMSKV_OK;
+  if ((!k && !v) || (k && !k_held) || (v && !v_held)) return AMSKV_ERR_INVALID_ARG;
+  // what is written is no other tensor of the call
+  if (k && v && (back ? k == v : k_held == v_held)) return AMSKV_ERR_INVALID_ARG;
+  for (const void* a : {k, v})
+    for (const void* b : {k_held, v_held})
+      if (a && a == b) return AMSKV_ERR_INVALID_ARG;
+  c.k = const_cast<void*>(k);
+  c.v = const_cast<void*>(v);
+  c.k_held = (unsigned char*)const_cast<void*>(k_held);
+  c.v_held = (unsigned char*)const_cast<void*>(v_held);
+  c.lengths = lengths_dev;
+  c.offsets = offsets_dev;
+  c.batch = x->batch;
+  c.kv_heads = x->kv_heads;
+  c.head_dim = x->head_dim;
+  c.kv_tokens = x->kv_tokens;
+  c.kv_rows = x->kv_rows;
+  return (back ? amskv::launch_unhold(c, (hipStream_t)stream) : amskv::launch_hold(c, (hipStream_t)stream)) == hipSuccess ? AMSKV_OK
+                                                                                                                        : AMSKV_ERR_HIP;
 }
 
 }  // namespace
@@ -126,6 +174,24 @@ int32_t amskv_cross_workspace_bytes(const amskv_cross* x, uint64_t* bytes_out) {
   return AMSKV_OK;
 }
 
+int32_t amskv_cross_held_bytes(const amskv_cross* x, int32_t packed, uint64_t* bytes_out) {
+  if (!bytes_out || (packed != 0 && packed != 1)) return AMSKV_ERR_INVALID_ARG;
+  if (int rc = check_held(x, nullptr, nullptr)) return rc;
+  if (packed && (x->kv_rows < 0 || x->kv_rows > INT32_MAX)) return AMSKV_ERR_INVALID_ARG;
+  *bytes_out = (uint64_t)held_bytes(x, packed != 0);
+  return AMSKV_OK;
+}
+
+int32_t amskv_cross_hold(const amskv_cross* x, const void* K_dev, const void* V_dev, void* K_held_dev, void* V_held_dev,
+                         const int32_t* lengths_dev, const int32_t* offsets_dev, void* stream) {
+  return hold(x, K_dev, V_dev, K_held_dev, V_held_dev, lengths_dev, offsets_dev, false, stream);
+}
+
+int32_t amskv_cross_export(const amskv_cross* x, const void* K_held_dev, const void* V_held_dev, void* K_out_dev, void* V_out_dev,
+                           const int32_t* lengths_dev, const int32_t* offsets_dev, void* stream) {
+  return hold(x, K_out_dev, V_out_dev, K_held_dev, V_held_dev, lengths_dev, offsets_dev, true, stream);
+}
+
 int32_t amskv_cross_attend(const amskv_cross* x, const void* Q_dev, const void* K_dev, const void* V_dev, void* O_dev,
                            const int32_t* lengths_dev, const int32_t* offsets_dev, void* workspace_dev, uint64_t workspace_bytes,
                            void* stream) {
@@ -136,8 +202,9 @@ int32_t amskv_cross_attend(const amskv_cross* x, const void* Q_dev, const void* 
   // packed: one axis of rows, whatever the batch strides say
   const int64_t nk[3] = {offsets_dev ? 1 : x->batch, x->kv_heads, offsets_dev ? x->kv_rows : x->kv_tokens};
   amskv::CrossCall c{};
+  c.four_bits = x->dtype == AMSKV_DTYPE_BF16_KV4;  // held tensors have no strides
   if (!map_of(&x->q, nq, x->head_dim, 2, false, &c.q_map) || !map_of(&x->o, nq, x->head_dim, 2, true, &c.o_map) ||
-      !map_of(&x->k, nk, x->head_dim, 2, false, &c.k_map) || !map_of(&x->v, nk, x->head_dim, 2, false, &c.v_map))
+      (!c.four_bits && (!map_of(&x->k, nk, x->head_dim, 2, false, &c.k_map) || !map_of(&x->v, nk, x->head_dim, 2, false, &c.v_map))))
     return AMSKV_ERR_INVALID_ARG;
   if (c.k_map.tok >= (1 << 24) || c.v_map.tok >= (1 << 24)) return AMSKV_ERR_INVALID_ARG;  // 64 rows of a tile by 32-bit offsets
   if (misaligned(Q_dev) || misaligned(K_dev) || misaligned(V_dev) || misaligned(O_dev) || misaligned(workspace_dev)) return AMSKV_ERR_INVALID_ARG;

@@ -1,6 +1,6 @@
 // What happens to the tensors of a scale between the projection and the attention (the step that Section 3.1's attention takes
 // as given): queries and keys turned by their tokens' positions, keys and values put into the cache, in its own type or in 8
-// bits.  And the other two kernels of an 8-bit cache that only move data: compaction and read-back.
+// or 4 bits.  And the other two kernels of such a cache that only move data: compaction and read-back.
 //
 // Turn.  Pair (x, y) -> (x c - y s, y c + x s), c and s from a table of the scale's tokens.  Both channels of a pair belong to one
 // lane: an item is 16 channels of a row -- 8 pairs -- held as two pieces of 8, which are pieces j and j + rot_dim/16 of the
@@ -13,6 +13,9 @@
 // code times it is a bf16 number: the attention gets exactly the held values, and e4m3, a floating format over 2^17, would gain
 // nothing from a finer scale.  A wave owns the 16 tokens of a block, 4 lanes to a row, so the block's maximum is one
 // reduction over its lanes; scales of 8 tokens and fewer put 2 to 16 heads into a wave.
+//
+// 4 bits: codes.hpp.  A row's groups of 32 channels are reduced over its 4 lanes, each group by itself, since a turned item's two pieces
+// may lie in two groups.
 //
 // Bound: HBM at the fine scales, 4.5 to 5.1 TB/s read + write (a device copy 4.9): 8 x 4096 rows of 16 heads out of a fused projection, head
 // dim 128 59 us (270 MB); K and V of 3840 (b,h), 169 tokens, head dim 64, to codes 48.6 us (249 MB); Q and K turned, K and V to codes,
@@ -95,12 +98,17 @@ __device__ __forceinline__ u32x2 codes8(const Piece& p, float by) {
   return r;
 }
 
+// the bytes of a row's groups, together
+template <int D>
+using RowGroups = typename std::conditional<D == 64, unsigned short, unsigned>::type;
+
 struct TakeArgs {
   int which[3];        // tensor of each blockIdx.y
   const char* src[3];  // K, V, Q
   char* dst[3];
   RowMap from[3], to[3];
-  float* scales[2];
+  float* scales[2];           // 8 bits
+  unsigned char* group_bytes[2];  // 4 bits
   const float* table;
   long long table_batch, cap_tokens;
   int dst_new, pieces_turned, half, inverse;
@@ -109,7 +117,7 @@ struct TakeArgs {
 
 // One wave: a block of 16 tokens of heads [first, end) of batch element b, in 16 row slots of 4 lanes.  A slot is a token of one
 // head (T > 8) or of one of 16 / 2^row_shift heads at once.
-template <typename T, int D, bool kEight>
+template <typename T, int D, int kBits>
 __device__ __forceinline__ void take_block(const TakeArgs& a, int tensor, unsigned b, int block, int first, int end) {
   constexpr int kItems = D / 64;  // per lane
   const int lane = threadIdx.x & 63;
@@ -157,14 +165,46 @@ __device__ __forceinline__ void take_block(const TakeArgs& a, int tensor, unsign
       }
     }
     int back = 0;
-    if constexpr (!kEight) {
+    if constexpr (kBits == 16) {
       back = a.inverse ? (int)0x80000000 : 0;
       asm volatile("" : "+v"(back));  // (formed here, so that the rows are asked for before the table is waited for)
     }
 #pragma unroll
     for (int i = 0; i < kItems; ++i)
       if (turned[i]) turn_item(x[i][0], x[i][1], tab[i], a.half, back);
-    if (kEight && tensor < 2) {
+    if (kBits == 4 && tensor < 2) {
+      constexpr int kGroups = D / AMSKV_KV4_GROUP;
+      float largest[kGroups];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) largest[g] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kItems; ++i)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          float of_piece = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) of_piece = fmaxf(of_piece, fabsf(x[i][p].x[e]));
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) largest[g] = fmaxf(largest[g], at[i][p] / AMSKV_KV4_GROUP == g ? of_piece : 0.f);
+        }
+      unsigned bytes = 0;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        largest[g] = fmaxf(largest[g], __shfl_xor(largest[g], 1, 64));
+        largest[g] = fmaxf(largest[g], __shfl_xor(largest[g], 2, 64));
+        bytes |= (unsigned)(group_exponent(largest[g]) + 127) << (8 * g);
+      }
+      if (live) {
+        const long long row_of_cache = ((long long)b * a.heads + h) * a.cap_tokens + a.dst_new + t;
+        char* row = a.dst[tensor] + row_of_cache * (D / 2);
+#pragma unroll
+        for (int i = 0; i < kItems; ++i)
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+            *reinterpret_cast<unsigned*>(row + at[i][p] / 2) = codes4(x[i][p].x, power_of_byte(bytes >> (8 * (at[i][p] / AMSKV_KV4_GROUP)) & 0xff));
+        if ((lane & 3) == 0) *reinterpret_cast<RowGroups<D>*>(a.group_bytes[tensor] + row_of_cache * kGroups) = (RowGroups<D>)bytes;
+      }
+    } else if (kBits == 8 && tensor < 2) {
 #pragma unroll
       for (int i = 0; i < kItems; ++i)
 #pragma unroll
@@ -204,7 +244,7 @@ __device__ __forceinline__ void take_block(const TakeArgs& a, int tensor, unsign
   }
 }
 
-template <typename T, int D, bool kEight>
+template <typename T, int D, int kBits>
 __global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
   fetch_arguments<sizeof(TakeArgs)>();
   const unsigned wave = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -212,11 +252,16 @@ __global__ __launch_bounds__(64 * kWaves) void take_kernel(TakeArgs a) {
   const unsigned b = unit / (unsigned)a.blocks, block = unit - b * a.blocks;
   if (b >= (unsigned)a.batch) return;
   const int first = group * a.heads_per_wave;
-  take_block<T, D, kEight>(a, a.which[blockIdx.y], b, block, first, min(first + a.heads_per_wave, a.heads));
+  take_block<T, D, kBits>(a, a.which[blockIdx.y], b, block, first, min(first + a.heads_per_wave, a.heads));
 }
 
-// Blocks that slide to lower places, in the order of their offsets: begin[i] .. begin[i+1] of the list come from src[i] and go to
-// dst[i] (all in blocks).
+// Blocks (8 bits: 16 tokens; 4 bits: a token) that slide to lower places, in the order of their offsets: begin[i] .. begin[i+1] of the
+// list come from src[i] and go to dst[i] (all in blocks).  A block is kChunks pieces of 16 bytes and a Scale.
+template <int D, int kBits>
+struct Blocks {
+  static constexpr int kTokens = kBits == 8 ? AMSKV_KV8_BLOCK : 1, kChunks = kBits == 8 ? D : D / 32;
+  typedef typename std::conditional<kBits == 8, float, RowGroups<D>>::type Scale;
+};
 struct BlockList {
   int32_t n, total;
   int32_t begin[AMSKV_MAX_SCALES], src[AMSKV_MAX_SCALES], dst[AMSKV_MAX_SCALES];
@@ -225,9 +270,10 @@ struct BlockList {
 // has arrived before any of it is written, and it is written below where it and all that follows is read.  Behind the last
 // barrier nothing is left to read.  Bound: HBM where the (b,h) are many, else one workgroup's passes, a trip to memory each: 3 to 7 us
 // at the coarse scales, 21.6 us at the last of ten scales, 960 (b,h), head dim 64.
-template <int D>
-__device__ __forceinline__ void slide(unsigned char* rows, float* scales, const BlockList& list) {
-  constexpr int kChunks = 4;  // of 16 bytes a thread and pass; a block of 16 tokens is D of them
+template <int D, int kBits>
+__device__ __forceinline__ void slide(unsigned char* rows, typename Blocks<D, kBits>::Scale* scales, const BlockList& list) {
+  constexpr int kChunks = 4;  // of 16 bytes a thread and pass
+  constexpr int kPer = Blocks<D, kBits>::kChunks;
   auto place = [&](int i, int& src, int& dst) {
     src = dst = 0;
     for (int r = 0; r < list.n; ++r)
@@ -236,7 +282,7 @@ __device__ __forceinline__ void slide(unsigned char* rows, float* scales, const 
         dst = list.dst[r] + i - list.begin[r];
       }
   };
-  const long long total = (long long)list.total * D;
+  const long long total = (long long)list.total * kPer;
   for (long long c0 = 0; c0 < total; c0 += (long long)blockDim.x * kChunks) {
     u32x4 buf[kChunks];
     long long to[kChunks];
@@ -246,9 +292,9 @@ __device__ __forceinline__ void slide(unsigned char* rows, float* scales, const 
       to[u] = -1;
       if (i < total) {
         int src, dst;
-        place((int)(i / D), src, dst);
-        buf[u] = *reinterpret_cast<const u32x4*>(rows + ((long long)src * D + i % D) * 16);
-        to[u] = ((long long)dst * D + i % D) * 16;
+        place((int)(i / kPer), src, dst);
+        buf[u] = *reinterpret_cast<const u32x4*>(rows + ((long long)src * kPer + i % kPer) * 16);
+        to[u] = ((long long)dst * kPer + i % kPer) * 16;
       }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -260,14 +306,14 @@ __device__ __forceinline__ void slide(unsigned char* rows, float* scales, const 
   for (int c0 = 0; c0 < list.total; c0 += (int)blockDim.x) {
     const int i = c0 + (int)threadIdx.x;
     int src = 0, dst = 0;
-    float x = 0.f;
+    typename std::conditional<kBits == 8, float, unsigned>::type x = 0;
     if (i < list.total) {
       place(i, src, dst);
       x = scales[src];
     }
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(x) : : "memory");
     __syncthreads();
-    if (i < list.total) scales[dst] = x;
+    if (i < list.total) scales[dst] = (typename Blocks<D, kBits>::Scale)x;
   }
 }
 
@@ -275,30 +321,43 @@ template <int D>
 __global__ __launch_bounds__(1024) void move_codes_kernel(Codes c, long long cap_tokens, BlockList list) {
   fetch_arguments<sizeof(Codes) + 8 + sizeof(BlockList)>();
   const long long bh = blockIdx.x;
-  slide<D>((blockIdx.y ? c.v : c.k) + bh * cap_tokens * D, (blockIdx.y ? c.v_scale : c.k_scale) + bh * (cap_tokens / AMSKV_KV8_BLOCK), list);
+  slide<D, 8>((blockIdx.y ? c.v : c.k) + bh * cap_tokens * D, (blockIdx.y ? c.v_scale : c.k_scale) + bh * (cap_tokens / AMSKV_KV8_BLOCK), list);
+}
+
+template <int D>
+__global__ __launch_bounds__(1024) void move_codes4_kernel(Codes4 c, long long cap_tokens, BlockList list) {
+  fetch_arguments<sizeof(Codes4) + 8 + sizeof(BlockList)>();
+  const long long first = (long long)blockIdx.x * cap_tokens;
+  slide<D, 4>((blockIdx.y ? c.v : c.k) + first * (D / 2), reinterpret_cast<RowGroups<D>*>(blockIdx.y ? c.v_group : c.k_group) + first, list);
 }
 
 // Both in one launch: the workgroup that owns a (b,h) of a tensor slides what stays of it, then its waves take the blocks of the
 // new scale, whose place may be where the survivors lay.
-template <int D>
+template <int D, int kBits>
 __global__ __launch_bounds__(64 * kOwners) void slide_and_take_kernel(TakeArgs a, BlockList list) {
   fetch_arguments<sizeof(TakeArgs) + sizeof(BlockList)>();
   const int tensor = a.which[blockIdx.y];
   const long long bh = blockIdx.x;
   const unsigned b = (unsigned)bh / (unsigned)a.heads;
   const int h = (int)(bh - (long long)b * a.heads);
-  if (tensor < 2) slide<D>((unsigned char*)a.dst[tensor] + bh * a.cap_tokens * D, a.scales[tensor] + bh * (a.cap_tokens / AMSKV_KV8_BLOCK), list);
+  if (tensor < 2) {
+    unsigned char* rows = (unsigned char*)a.dst[tensor] + bh * a.cap_tokens * (D * kBits / 8);
+    if constexpr (kBits == 8)
+      slide<D, 8>(rows, a.scales[tensor] + bh * (a.cap_tokens / AMSKV_KV8_BLOCK), list);
+    else
+      slide<D, 4>(rows, reinterpret_cast<RowGroups<D>*>(a.group_bytes[tensor]) + bh * a.cap_tokens, list);
+  }
   for (int block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); block < a.blocks; block += kOwners)
-    take_block<__bf16, D, true>(a, tensor, b, block, h, h + 1);
+    take_block<__bf16, D, kBits>(a, tensor, b, block, h, h + 1);
 }
 
-BlockList block_list(const MoveList& mv) {
+BlockList block_list(const MoveList& mv, int tokens) {
   BlockList list{};
   for (int i = 0; i < mv.n; ++i) {
     list.begin[list.n] = list.total;
-    list.src[list.n] = mv.src[i] / AMSKV_KV8_BLOCK;
-    list.dst[list.n] = mv.dst[i] / AMSKV_KV8_BLOCK;
-    list.total += mv.len[i] / AMSKV_KV8_BLOCK;
+    list.src[list.n] = mv.src[i] / tokens;
+    list.dst[list.n] = mv.dst[i] / tokens;
+    list.total += mv.len[i] / tokens;
     ++list.n;
   }
   return list;
@@ -317,11 +376,13 @@ hipError_t take(const Take& t, hipStream_t st) {
     a.from[i] = i == 2 ? t.q_map : t.kv_map;
     a.to[i] = i == 2 ? t.q_out_map : t.out_map;
   }
-  a.dst[0] = t.eight_bits ? (char*)t.codes.k : (char*)t.k_out;
-  a.dst[1] = t.eight_bits ? (char*)t.codes.v : (char*)t.v_out;
+  a.dst[0] = t.eight_bits ? (char*)t.codes.k : t.four_bits ? (char*)t.codes4.k : (char*)t.k_out;
+  a.dst[1] = t.eight_bits ? (char*)t.codes.v : t.four_bits ? (char*)t.codes4.v : (char*)t.v_out;
   a.dst[2] = (char*)t.q_out;
   a.scales[0] = t.codes.k_scale;
   a.scales[1] = t.codes.v_scale;
+  a.group_bytes[0] = t.codes4.k_group;
+  a.group_bytes[1] = t.codes4.v_group;
   a.table = t.table;
   a.table_batch = t.table_batch;
   a.cap_tokens = t.cap_tokens;
@@ -343,20 +404,32 @@ hipError_t take(const Take& t, hipStream_t st) {
   const dim3 g((unsigned)grid, n), block(64 * kWaves);
   if constexpr (sizeof(T) == 2) {
     if (t.eight_bits && t.moves != nullptr && t.moves->n > 0) {
-      const BlockList list = block_list(*t.moves);
+      const BlockList list = block_list(*t.moves, AMSKV_KV8_BLOCK);
       if (slides_at_once(t.batch * t.heads, t.tokens, list.total, D)) {
-        hipLaunchKernelGGL((slide_and_take_kernel<D>), dim3(t.batch * t.heads, n), dim3(64 * kOwners), 0, st, a, list);
+        hipLaunchKernelGGL((slide_and_take_kernel<D, 8>), dim3(t.batch * t.heads, n), dim3(64 * kOwners), 0, st, a, list);
         return hipGetLastError();
       }
       const hipError_t e = launch_move_codes(t.codes, t.batch * t.heads, t.head_dim, t.cap_tokens, *t.moves, st);
       if (e != hipSuccess) return e;
     }
-    if (t.eight_bits) {
-      hipLaunchKernelGGL((take_kernel<T, D, true>), g, block, 0, st, a);
+    if (t.four_bits && t.moves != nullptr && t.moves->n > 0) {
+      const BlockList list = block_list(*t.moves, 1);
+      if (slides_at_once(t.batch * t.heads, t.tokens, (list.total + 15) / 16, D)) {
+        hipLaunchKernelGGL((slide_and_take_kernel<D, 4>), dim3(t.batch * t.heads, n), dim3(64 * kOwners), 0, st, a, list);
+        return hipGetLastError();
+      }
+      const hipError_t e = launch_move_codes4(t.codes4, t.batch * t.heads, t.head_dim, t.cap_tokens, *t.moves, st);
+      if (e != hipSuccess) return e;
+    }
+    if (t.eight_bits || t.four_bits) {
+      if (t.eight_bits)
+        hipLaunchKernelGGL((take_kernel<T, D, 8>), g, block, 0, st, a);
+      else
+        hipLaunchKernelGGL((take_kernel<T, D, 4>), g, block, 0, st, a);
       return hipGetLastError();
     }
   }
-  hipLaunchKernelGGL((take_kernel<T, D, false>), g, block, 0, st, a);
+  hipLaunchKernelGGL((take_kernel<T, D, 16>), g, block, 0, st, a);
   return hipGetLastError();
 }
 
@@ -378,8 +451,8 @@ __global__ __launch_bounds__(256) void rope_table_kernel(const double* __restric
 
 // The values of the resident segments, ascending and back to back, as bf16 [BH][T_kept][D]; a lane takes 16 channels of a row.
 // Bound: HBM (960 (b,h), up to 640 tokens, head dim 64: 44 us, about 5 TB/s).
-template <int D>
-__global__ __launch_bounds__(256) void export_codes_kernel(Codes c, __bf16* __restrict__ k_out, __bf16* __restrict__ v_out, long long cap_tokens,
+template <int D, int kBits>
+__global__ __launch_bounds__(256) void export_codes_kernel(CodesOf<kBits> c, __bf16* __restrict__ k_out, __bf16* __restrict__ v_out, long long cap_tokens,
                                                            SegTable seg, ExtKV ext_kv, RowMap ext_map, int heads, int parts, int units,
                                                            int n_bh) {
   __bf16* out = blockIdx.y ? v_out : k_out;
@@ -398,6 +471,12 @@ __global__ __launch_bounds__(256) void export_codes_kernel(Codes c, __bf16* __re
     const char* row = (const char*)(blockIdx.y ? ext_kv.v : ext_kv.k) + unit_offset(ext_map, bh, heads) + at * ext_map.tok + piece * 32;
     w[0] = *reinterpret_cast<const u32x4*>(row);
     w[1] = *reinterpret_cast<const u32x4*>(row + 16);
+  } else if constexpr (kBits == 4) {
+    const long long row = bh * cap_tokens + at;
+    const u32x2 x = *reinterpret_cast<const u32x2*>((blockIdx.y ? c.v : c.k) + row * (D / 2) + piece * 8);
+    const float scale = power_of_byte((blockIdx.y ? c.v_group : c.k_group)[row * (D / AMSKV_KV4_GROUP) + piece / 2]);
+    w[0] = values4(x[0], scale);
+    w[1] = values4(x[1], scale);
   } else {
     const unsigned char* codes = (blockIdx.y ? c.v : c.k) + (bh * cap_tokens + at) * D + piece * 16;
     const u32x4 x = *reinterpret_cast<const u32x4*>(codes);
@@ -428,7 +507,7 @@ hipError_t launch_rope_table(const double* frequency, int pairs, int axes, doubl
 }
 
 hipError_t launch_move_codes(const Codes& c, int bh, int head_dim, int64_t cap_tokens, const MoveList& mv, hipStream_t st) {
-  const BlockList list = block_list(mv);
+  const BlockList list = block_list(mv, AMSKV_KV8_BLOCK);
   if (list.total == 0) return hipSuccess;
   const int threads = move_threads(list.total, head_dim, bh);
   auto kernel = head_dim == 64 ? move_codes_kernel<64> : move_codes_kernel<128>;
@@ -436,15 +515,35 @@ hipError_t launch_move_codes(const Codes& c, int bh, int head_dim, int64_t cap_t
   return hipGetLastError();
 }
 
-hipError_t launch_export_codes(const Codes& c, void* k_out, void* v_out, int bh, int head_dim, int64_t cap_tokens, const SegTable& seg,
+hipError_t launch_move_codes4(const Codes4& c, int bh, int head_dim, int64_t cap_tokens, const MoveList& mv, hipStream_t st) {
+  const BlockList list = block_list(mv, 1);
+  if (list.total == 0) return hipSuccess;
+  const int threads = move_threads((list.total + 31) / 32, head_dim, bh);  // (as many chunks as so many blocks of 8 bits)
+  auto kernel = head_dim == 64 ? move_codes4_kernel<64> : move_codes4_kernel<128>;
+  hipLaunchKernelGGL(kernel, dim3(bh, 2), dim3(threads), 0, st, c, (long long)cap_tokens, list);
+  return hipGetLastError();
+}
+
+template <int kBits>
+static hipError_t export_codes(const CodesOf<kBits>& c, void* k_out, void* v_out, int bh, int head_dim, int64_t cap_tokens, const SegTable& seg,
                                const ExtKV& ext, const RowMap& ext_map, int heads, hipStream_t st) {
   if (seg.total == 0) return hipSuccess;
   const ExportGrid g = export_grid(bh, seg.total, head_dim);
   if (g.layers > 65535) return hipErrorInvalidValue;
-  auto kernel = head_dim == 64 ? export_codes_kernel<64> : export_codes_kernel<128>;
+  auto kernel = head_dim == 64 ? export_codes_kernel<64, kBits> : export_codes_kernel<128, kBits>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(g.parts * g.units), 2, (unsigned)g.layers), dim3(256), 0, st, c, (__bf16*)k_out, (__bf16*)v_out,
                      (long long)cap_tokens, seg, ext, ext_map, heads, (int)g.parts, (int)g.units, bh);
   return hipGetLastError();
+}
+
+hipError_t launch_export_codes(const Codes& c, void* k_out, void* v_out, int bh, int head_dim, int64_t cap_tokens, const SegTable& seg,
+                               const ExtKV& ext, const RowMap& ext_map, int heads, hipStream_t st) {
+  return export_codes<8>(c, k_out, v_out, bh, head_dim, cap_tokens, seg, ext, ext_map, heads, st);
+}
+
+hipError_t launch_export_codes4(const Codes4& c, void* k_out, void* v_out, int bh, int head_dim, int64_t cap_tokens, const SegTable& seg,
+                                const ExtKV& ext, const RowMap& ext_map, int heads, hipStream_t st) {
+  return export_codes<4>(c, k_out, v_out, bh, head_dim, cap_tokens, seg, ext, ext_map, heads, st);
 }
 
 }  // namespace amskv

@@ -1,0 +1,59 @@
+"""K and V in 4 bits written out in 64 bits, and how far an attention over them may lie from the formula.
+
+A rounding is off by at most half a step: 2^-8 of the value in bf16, 2^-24 in fp32."""
+import math
+
+import torch
+
+import plain_operators as plain
+
+GROUP = 32
+NUMBERS = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]   # e2m1
+_two_to = plain._two_to
+
+
+def _least_exponent(m, most, lo, hi):
+    """The least e in [lo, hi] with m <= most * 2^e, as fp64."""
+    e = torch.frexp(m)[1].double() - 5
+    for _ in range(5):
+        e = torch.where(m > most * _two_to(e.clamp(-900, 900)), e + 1, e)
+    return e.clamp(lo, hi)
+
+
+def exponents(x):
+    """x [..., D] -> the exponent of each group, fp64 [..., D / 32, 1]."""
+    m = x.double().unflatten(-1, (-1, GROUP)).abs().amax(dim=-1, keepdim=True)
+    return _least_exponent(m, 7.0, -100, 125)
+
+
+def held(x):
+    """x [..., D] as 4 bits hold it, fp64."""
+    y = x.double().unflatten(-1, (-1, GROUP))
+    scale = _two_to(exponents(x))
+    numbers = torch.tensor(NUMBERS, dtype=torch.float64, device=x.device)
+    z = (y.abs() / scale).clamp(max=6.0)
+    hi = torch.searchsorted(numbers, z).clamp(max=7)
+    lo = (hi - 1).clamp(min=0)
+    up, down = numbers[hi] - z, z - numbers[lo]
+    out = torch.where((up < down) | ((up == down) & (hi % 2 == 0)), numbers[hi], numbers[lo])
+    return (out * scale * torch.sign(y)).flatten(-2)
+
+
+def attention(q, k, v, scale):
+    """As plain.attention, over held k and v, with the products' rounding of Q: an element of a group whose largest is m, 2^a the least
+    power with m <= 7.5 * 2^a, is exact if it is 2^a at least or a multiple of 2^(a - 7), else off by 2^(a - 8) at most; that moves a
+    score by at most the sum of these times |k|, and a weight, relative to the others', by exp of twice as much.
+
+    Weights of 2^-120 of the largest and less may vanish: a reference that is up to 2^6 below the largest weight of its time is left for
+    one more than 2^126 above it by a factor that fp32 flushes to 0 (held values may be 0 where the weight is 1, so that this shows)."""
+    q, k, v = (x.double() for x in (q, k, v))
+    o, bound = plain.attention(q, k, v, scale)
+    y = q.unflatten(-1, (-1, GROUP))
+    a = _least_exponent(y.abs().amax(dim=-1, keepdim=True), 7.5, -120, 130)
+    step = _two_to(a - 7)
+    off = torch.where((y.abs() >= 128 * step) | (torch.remainder(y, step) == 0), torch.zeros_like(y), step / 2).flatten(-2)
+    far = (off @ k.abs().transpose(-1, -2)).amax(dim=-1, keepdim=True) * scale
+    s = q @ k.transpose(-1, -2) * scale
+    p, rel = torch.softmax(s, dim=-1), torch.exp(s - s.amax(dim=-1, keepdim=True))
+    size, lost = p @ v.abs(), torch.where(rel <= 1.01 * 2.0 ** -120, p, torch.zeros_like(p)) @ v.abs()
+    return o, bound * torch.exp(2 * far) + torch.expm1(2 * far) * (size + o.abs()) + lost
