@@ -8,7 +8,7 @@
 // hides (8 x 16 heads, 4096 x up to 512, head dim 128: 120 us, 0.57 PFLOP/s and 2.4 TB/s).
 // A launch over few rows and many states does not fill the chip with one workgroup to 32 or 128 rows; then `splits` workgroups
 // take equal runs of key tiles each, leave their sums unnormalised in the workspace, and a second launch puts them together.
-#include "attend_rows.hpp"
+#include "attend_four.hpp"
 #include "attend_rows_choice.hpp"
 
 namespace amskv {
@@ -44,7 +44,9 @@ template <int D, int kTeamWaves, int kTeams, int kMinWavesPerSimd, int kBits>
 __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cross_kernel(CrossArgs a) {
   fetch_arguments<sizeof(CrossArgs)>();
   using U = rows::Unit<D, kTeamWaves, kTeams, kBits>;
-  __shared__ __align__(1024) char lds[U::kLds];
+  constexpr bool kParts = kBits == 4 && kTeamWaves > 1;  // K goes to the matrix cores in 4 bits
+  using Team = rows::FourBitTeam<D, kTeamWaves == 1 ? 4 : kTeamWaves, false>;
+  __shared__ __align__(1024) char lds[kParts ? Team::kLds : U::kLds];
   const int tiles = a.row_tiles * a.splits;
   Place at{(int)blockIdx.x, 0};
   if (tiles > 1) at = place<true>(blockIdx.x, a.n_units, tiles, a.n_whole);
@@ -63,11 +65,7 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
     return b * m.batch + ((long long)g * a.group + head) * m.head + token * m.tok;
   };
 
-  rows::bf16x8 qf[U::KS];
   const char* q_row = a.q + row_at(a.q_map, lane);
-#pragma unroll
-  for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + U::q_at(t, h));
-
   rows::Keys keys{};
   if constexpr (kBits == 16) {
     const long long kb = a.offsets ? first * a.k_map.tok : b * a.k_map.batch, vb = a.offsets ? first * a.v_map.tok : b * a.v_map.batch;
@@ -90,7 +88,16 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   U::clear(x);
   SegTable none;
   none.n = 0;
-  U::walk(x, qf, lds, keys, none, from, to, a.scale_log2e, active);
+  if constexpr (kParts) {
+    rows::QueryParts<D> parts;
+    rows::split_query<D>(parts, q_row, h);
+    Team::walk(x, parts, [&]() { return q_row; }, lds, keys, none, from, to, a.scale_log2e, active);
+  } else {
+    rows::bf16x8 qf[U::KS];
+#pragma unroll
+    for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + U::q_at(t, h));
+    U::walk(x, qf, lds, keys, none, from, to, a.scale_log2e, active);
+  }
   U::meet(x, lds);
   const int late = U::fresh(threadIdx.x) & 63;
   if (a.splits == 1) {
