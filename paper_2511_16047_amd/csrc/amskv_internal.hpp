@@ -357,6 +357,7 @@ struct CrossCall {
 };
 // Bytes of the workspace that a call of this shape uses (0: none).
 uint64_t cross_workspace_bytes(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) AMSKV_OPTIONAL;
+uint64_t cross_workspace_bytes4(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) AMSKV_OPTIONAL;  // held states
 hipError_t launch_cross(const CrossCall& c, hipStream_t st) AMSKV_OPTIONAL;
 
 // An encoder's K and V and their held forms in 4 bits: a held tensor is codes [units][rows][D / 2], then, behind all of them, the bytes

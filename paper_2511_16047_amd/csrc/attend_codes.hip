@@ -43,8 +43,8 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void att
   typename U::Result x;
   U::clear(x);
   if constexpr (kParts) {
-    rows::QueryParts<D> parts;
-    rows::split_query<D>(parts, q_row(lane), h);
+    typename Team::Query parts;
+    rows::split_query(parts, q_row(lane), h, scale_log2e);
     Team::walk(x, parts, [&]() { return q_row(U::fresh(threadIdx.x)); }, lds, keys, seg, 0, Team::tiles(keys), scale_log2e, active);
   } else {
     rows::bf16x8 qf[U::KS];
@@ -55,7 +55,9 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void att
   }
   U::meet(x, lds);
   const int row = base + (U::fresh(threadIdx.x) & 31);  // (not kept over the walk)
-  U::put(x, reinterpret_cast<__bf16*>(o + unit_offset(io.o, bh, io.heads) + min(row, t_q - 1) * io.o.tok), active && row < t_q);
+  int heads = io.heads;
+  if constexpr (kParts) asm volatile("" : "+s"(heads));  // (nor what divides by them)
+  U::put(x, reinterpret_cast<__bf16*>(o + unit_offset(io.o, bh, heads) + min(row, t_q - 1) * io.o.tok), active && row < t_q);
 }
 
 template <int D, int kTeamWaves, int kTeams, int kMinWavesPerSimd, int kBits = 8, bool kMixed = true>
@@ -88,7 +90,7 @@ hipError_t launch_attend_codes4(const void* q, void* o, const Codes4& c, int bh,
                                 const SegTable& seg, const ExtKV& ext, const CallerIo& io, float softmax_scale, hipStream_t st) {
   const float s = softmax_scale * 1.4426950408889634f;
   auto run = [&](auto f) { return f(q, o, c, bh, t_q, cap_tokens, seg, ext, io, s, st); };
-  const rows::Form f = rows::choose_codes(head_dim, bh, t_q, seg.total);
+  const rows::Division f = rows::divide4(head_dim, bh, t_q, seg.total, 1);
   const bool mixed = seg.ext_start < seg.total;
   if (head_dim == 64) {
     if (f.team_waves == 1) return f.teams == 1 ? run(go<64, 1, 1, 3, 4>) : f.teams == 4 ? run(go<64, 1, 4, 3, 4>) : run(go<64, 1, 8, 2, 4>);
@@ -97,7 +99,7 @@ hipError_t launch_attend_codes4(const void* q, void* o, const Codes4& c, int bh,
   }
   if (f.team_waves == 1) return f.teams == 1 ? run(go<128, 1, 1, 2, 4>) : f.teams == 4 ? run(go<128, 1, 4, 2, 4>) : run(go<128, 1, 8, 2, 4>);
   if (mixed) return f.team_waves == 4 ? run(go<128, 4, 1, 2, 4>) : run(go<128, 8, 1, 2, 4>);
-  return f.team_waves == 4 ? run(go<128, 4, 1, 2, 4, false>) : run(go<128, 8, 1, 2, 4, false>);
+  return f.team_waves == 4 ? run(go<128, 4, 1, 3, 4, false>) : run(go<128, 8, 1, 2, 4, false>);
 }
 
 }  // namespace amskv

@@ -23,14 +23,28 @@ typedef unsigned u32x6 __attribute__((ext_vector_type(6)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// Q of a lane: channels 64 c + 32 h .. + 31 of its row in two parts, and the bytes of their powers (0: hi, 1: lo).
-template <int D>
+// Q of a lane times the factor of its scores: channels 64 c + 32 h .. + 31 of its row in kParts parts, largest first, and the bytes of
+// their powers.
+template <int D, int kParts>
 struct QueryParts {
-  u32x6 hi[D / 64], lo[D / 64];
-  unsigned power[D / 64];
+  u32x6 part[D / 64][kParts];
+  unsigned powers[D / 64];
 };
-template <int D>
-__device__ __forceinline__ void split_query(QueryParts<D>& q, const char* row, int h) {
+// 32 numbers as e2m3 times a power of two, even and odd ones by turns, and back.  Written out: the conversions write their first results
+// before they have read all operands, and the compiler's own may let the two overlap, which gave wrong parts of Q in some builds.  (The
+// wait is for what reads the results: the compiler does not see into inline assembly.)
+__device__ __forceinline__ u32x6 parts_of(const f32x16& even, const f32x16& odd, float by) {
+  u32x6 r;
+  asm("v_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, %3\n\ts_nop 7" : "=&v"(r) : "v"(even), "v"(odd), "v"(by));
+  return r;
+}
+__device__ __forceinline__ f32x32 values_of(const u32x6& x, float by) {
+  f32x32 r;
+  asm("v_cvt_scalef32_pk32_f32_fp6 %0, %1, %2\n\ts_nop 7" : "=&v"(r) : "v"(x), "v"(by));
+  return r;
+}
+template <int D, int kParts>
+__device__ __forceinline__ void split_query(QueryParts<D, kParts>& q, const char* row, int h, float factor) {
   u32x4 raw[D / 64][4];
 #pragma unroll
   for (int c = 0; c < D / 64; ++c)
@@ -42,25 +56,28 @@ __device__ __forceinline__ void split_query(QueryParts<D>& q, const char* row, i
     float m = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      even[i] = __builtin_bit_cast(float, raw[c][i / 4][i % 4] << 16);
-      odd[i] = __builtin_bit_cast(float, raw[c][i / 4][i % 4] & 0xffff0000u);
+      even[i] = __builtin_bit_cast(float, raw[c][i / 4][i % 4] << 16) * factor;
+      odd[i] = __builtin_bit_cast(float, raw[c][i / 4][i % 4] & 0xffff0000u) * factor;
       m = max3(m, __builtin_fabsf(even[i]), __builtin_fabsf(odd[i]));
     }
     const int bits = __builtin_bit_cast(int, m);  // 7.5 = 1.875 * 2^2
-    const int a = min(max((bits >> 23) - 127 - 2 + ((bits & 0x7fffff) > 0x700000 ? 1 : 0), -120), 126);
-    q.power[c] = (unsigned)(a + 127) | (unsigned)(a + 123) << 8;
-    const float by = power_of_byte(a + 127);
-    q.hi[c] = __builtin_bit_cast(u32x6, __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, by));
-    const f32x32 held = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q.hi[c], by);
+    const int a = min(max((bits >> 23) - 127 - 2 + ((bits & 0x7fffff) > 0x700000 ? 1 : 0), -110), 126);
+    q.powers[c] = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      even[i] -= held[2 * i];
-      odd[i] -= held[2 * i + 1];
+    for (int p = 0; p < kParts; ++p) {
+      const int byte = a - 4 * p + 127;
+      const float by = power_of_byte(byte);
+      q.powers[c] |= (unsigned)byte << (8 * p);
+      q.part[c][p] = parts_of(even, odd, by);
+      if (p + 1 < kParts) {
+        const f32x32 held = values_of(q.part[c][p], by);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          even[i] -= held[2 * i];
+          odd[i] -= held[2 * i + 1];
+        }
+      }
     }
-    q.lo[c] = __builtin_bit_cast(u32x6, __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, power_of_byte(a + 123)));
-    // (the conversion writes its first results before it has read all operands, and the compiler lets the two overlap where the
-    // operands are not read again: here they are)
-    asm volatile("" ::"v"(even), "v"(odd));
   }
 }
 
@@ -68,7 +85,6 @@ template <int D, int kTeamWaves, bool kExt>
 struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
   typedef Unit<D, kTeamWaves, 1, 4> Base;
   typedef typename Base::Result Result;
-  typedef typename Base::Behind Behind;
   typedef typename Base::Staged Staged;
   typedef typename Base::Aim Aim;
   static constexpr int RB = Base::RB, KS = Base::KS, kTile = Base::kTile, kThreads = Base::kThreads;
@@ -77,6 +93,11 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
   static constexpr int kOfK = kExt ? Base::kTensor : kPowers + 32 * kTile;
   static constexpr int kStage = kOfK + Base::kTensor;
   static constexpr int kLds = 4 * kStage;
+  static constexpr int kParts = 2;
+  // The products start from the references: S^T - ref comes out of the matrix cores, 16 multiply-adds of a block's 90 vector
+  // instructions fewer, for 16 registers that hold -ref.
+  static constexpr bool kFolds = D == 64 || kTeamWaves == 8;
+  typedef QueryParts<D, kParts> Query;
   static_assert(kPowers + 32 * kTile <= kOfK && kThreads == 8 * kTile, "eight threads bring a row of K and of V");
 
   __device__ static __forceinline__ int tiles(const Keys& k) { return kExt ? Base::tiles(k) : Base::tiles_of_codes(k); }
@@ -86,7 +107,7 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
 
   // ---- from memory to LDS.  A thread has an eighth of a row of K and the same of V: D / 8 channels each, and their powers.
   // Where chunk c (16 bytes) of a row of K's codes sits: reads of 8 rows then spread over all banks
-  __device__ static __forceinline__ int chunk_of_k(int row, int c) { return D == 64 ? c ^ ((row >> 3) & 1) : c ^ ((row >> 2) & 3); }
+  __device__ static __forceinline__ unsigned chunk_of_k(unsigned row, unsigned c) { return D == 64 ? c ^ ((row >> 3) & 1) : c ^ ((row >> 2) & 3); }
   __device__ static __forceinline__ void aim_codes(Aim& a, const Keys& k, const SegTable& seg, int it, int member) {
     const int first = it * kTile, last = k.n_codes - 1;
     member = Base::fresh(member);
@@ -96,16 +117,15 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
           a.end = seg.virt_start[g] + seg.len[g];
           a.delta = seg.phys_off[g] - seg.virt_start[g];
         }
-    const int j = min(first + member / 8, last);
+    const int j = min(first + (int)((unsigned)member / 8), last);
     a.row[0] = j + a.delta;
     if (min(first + kTile - 1, last) >= a.end)  // rows of several segments
       for (int g = 0; g < seg.n; ++g)
         if (j >= seg.virt_start[g]) a.row[0] = j + seg.phys_off[g] - seg.virt_start[g];
   }
   // (x[0]: K's codes, V's; x[1]: the powers of K's row, of V's piece)
-  __device__ static __forceinline__ void fetch_codes(Staged& s, const Aim& a, const Keys& k, int member) {
-    member = Base::fresh(member);
-    const unsigned piece = member % 8, at = a.row[0] * kRowK + piece * (D / 16), group = a.row[0] * (D / AMSKV_KV4_GROUP);
+  __device__ static __forceinline__ void fetch_codes(Staged& s, const Aim& a, const Keys& k, int thread) {
+    const unsigned member = Base::fresh(thread), piece = member % 8, at = a.row[0] * kRowK + piece * (D / 16), group = a.row[0] * (D / AMSKV_KV4_GROUP);
     if constexpr (D == 64) {
       s.x[0][0] = *reinterpret_cast<const unsigned*>(k.k_codes + at);
       s.x[0][2] = *reinterpret_cast<const unsigned*>(k.v_codes + at);
@@ -117,19 +137,18 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
     }
     s.x[1][1] = k.v_group[group + piece * (D / 8) / AMSKV_KV4_GROUP];
   }
-  __device__ static __forceinline__ void store_codes(const Staged& s, char* lds_all, int lds, int member) {
-    member = Base::fresh(member);
-    const int row = member / 8, piece = member % 8;
+  __device__ static __forceinline__ void store_codes(const Staged& s, char* lds_all, int lds, int thread) {
+    const unsigned member = Base::fresh(thread), row = member / 8, piece = member % 8;
     char* tile = lds_all + lds;
     *reinterpret_cast<unsigned*>(tile + kPowers + 32 * row + 4 * piece) = s.x[1][0];  // (eight times: no lane stands aside)
     const float by = power_of_byte(s.x[1][1]);
     if constexpr (D == 64) {
       *reinterpret_cast<unsigned*>(tile + row * kRowK + 16 * chunk_of_k(row, piece / 4) + 4 * (piece % 4)) = s.x[0][0];
-      *reinterpret_cast<u32x4*>(tile + kOfK + row * RB + 16 * (piece ^ swizzle<D>(row))) = values4(s.x[0][2], by);
+      *reinterpret_cast<u32x4*>(tile + kOfK + row * RB + 16 * (piece ^ (unsigned)swizzle<D>((int)row))) = values4(s.x[0][2], by);
     } else {
       *reinterpret_cast<u32x2*>(tile + row * kRowK + 16 * chunk_of_k(row, piece / 2) + 8 * (piece % 2)) = u32x2{s.x[0][0], s.x[0][1]};
       char* v = tile + kOfK + row * RB;
-      const int at = 16 * ((2 * piece) ^ swizzle<D>(row));
+      const unsigned at = 16 * ((2 * piece) ^ (unsigned)swizzle<D>((int)row));
       *reinterpret_cast<u32x4*>(v + at) = values4(s.x[0][2], by);
       *reinterpret_cast<u32x4*>(v + (at ^ 16)) = values4(s.x[0][3], by);
     }
@@ -161,45 +180,111 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
   };
   __device__ static __forceinline__ int k_lane4(int lane) { return (lane & 31) * kRowK + 16 * chunk_of_k(lane & 31, lane >> 5); }
   // block: of 32 keys inside the tile at `slot`
-  __device__ static __forceinline__ void load_codes(KeyCodes& kc, const char* lds_all, int slot, int block, int ka, int lane) {
-    const int r = lane & 31;
+  __device__ static __forceinline__ void load_codes(KeyCodes& kc, const char* lds_all, int slot, int block, int ka, int kp, int lane) {
     const char* at = lds_all + slot + block * 32 * kRowK;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) kc.code[c] = *reinterpret_cast<const u32x4*>(at + (ka ^ (32 * c)));
-    kc.powers = *reinterpret_cast<const unsigned*>(lds_all + slot + kPowers + 32 * 32 * block + 32 * r + 4 * (r >> 3)) >> (8 * (lane >> 5));
+    kc.powers = *reinterpret_cast<const unsigned*>(lds_all + slot + 32 * 32 * block + kp) >> (8 * (lane >> 5));
   }
-  __device__ static __forceinline__ f32x16 product(const KeyCodes& kc, const QueryParts<D>& q) {
-    f32x16 s;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) s[v] = 0.f;
-    auto wide4 = [](const u32x4& x) { return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0}; };
-    auto wide6 = [](const u32x6& x) { return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0}; };
+  // scores times the factor, less the references of the exponentials
+  template <int kPart, int kChunk>
+  __device__ static __forceinline__ f32x16 multiply(const KeyCodes& kc, const Query& q, const f32x16& add) {
+    const u32x4& k = kc.code[kChunk];
+    const u32x6& x = q.part[kChunk][kPart];
     // (4: e2m1, 2: e2m3; the bytes of the powers are picked by constants)
-    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide4(kc.code[0]), wide6(q.lo[0]), s, 4, 2, 0, kc.powers, 1, q.power[0]);
-    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide4(kc.code[0]), wide6(q.hi[0]), s, 4, 2, 0, kc.powers, 0, q.power[0]);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(i32x8{(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0},
+                                                           i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0}, add, 4, 2,
+                                                           2 * kChunk, kc.powers, kPart, q.powers[kChunk]);
+  }
+  __device__ static __forceinline__ f32x16 product(const KeyCodes& kc, const Query& q, const f32x16& less_ref) {
+    f32x16 s = multiply<0, 0>(kc, q, less_ref);
+    s = multiply<1, 0>(kc, q, s);
+    if constexpr (kParts == 3) s = multiply<2, 0>(kc, q, s);
     if constexpr (D == 128) {
-      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide4(kc.code[1]), wide6(q.lo[1]), s, 4, 2, 2, kc.powers, 1, q.power[1]);
-      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide4(kc.code[1]), wide6(q.hi[1]), s, 4, 2, 2, kc.powers, 0, q.power[1]);
+      s = multiply<0, 1>(kc, q, s);
+      s = multiply<1, 1>(kc, q, s);
+      if constexpr (kParts == 3) s = multiply<2, 1>(kc, q, s);
     }
     return s;
   }
+  // weights of keys 16u .. 16u + 15 against a reference (kFolds: that s already is without); the lane's sum
+  __device__ static __forceinline__ float weights(const f32x16& s, u32x4& pf, float ref, int u) {
+    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 8; v += 2) {
+      const float a = s[8 * u + v], b = s[8 * u + v + 1];
+      const bf16x2 pk = {(__bf16)__builtin_amdgcn_exp2f(kFolds ? a : a - ref), (__bf16)__builtin_amdgcn_exp2f(kFolds ? b : b - ref)};
+      sum = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, sum, false);
+      pf[v / 2] = __builtin_bit_cast(unsigned, pk);
+    }
+    return sum;
+  }
+  // Unit::Behind.  kFolds: less_ref is what the references are taken off by, -0 for a reference of 0 and +0 in a lane that has none yet
+  // (and Result::ref is kept there); else it is 0 and Result::ref the reference.
+  struct Behind {
+    u32x4 pf[2];
+    f32x16 less_ref;
+    int block;
+    float most;  // a larger sum moves the references: kTripSum; kFolds: -1 while a lane has none (uniform)
+  };
+  __device__ static __forceinline__ float reference(const Result& x, const Behind& w) {
+    if constexpr (!kFolds) return x.ref;
+    return __builtin_bit_cast(unsigned, w.less_ref[0]) == 0 ? kNoKeys : -w.less_ref[0];
+  }
+  // Unit::step in one basic block: the first block, which has none before it, takes weights of 0 for what lies in its slot.
   template <bool kFull, class Between>
-  __device__ static __forceinline__ void step_codes(Result& x, Behind& w, KeyCodes& kc, const QueryParts<D>& q, const char* lds_all, int va, int block,
-                                                    int n_valid, float c, int lane, Between between) {
-    if (!Base::kOneBlock && __builtin_expect(w.rescale, 0)) Base::scale_by(x, w.alpha);
-    f32x16 s = product(kc, q);
+  __device__ static __forceinline__ void step_codes(Result& x, Behind& w, KeyCodes& kc, const Query& q, const char* lds_all, int va, int block,
+                                                    int n_valid, int lane, Between between) {
+    f32x16 s = product(kc, q, w.less_ref);
     between();
-    Base::template behind_scores<kFull>(x, w, s, lds_all, va, block, n_valid, c, lane);
+    if constexpr (!kFull) Base::mask(s, n_valid, lane);
+    if constexpr (Base::kAlone) __builtin_amdgcn_s_setprio(1);
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      Base::add_values(x, __builtin_bit_cast(bf16x8, w.pf[u]), lds_all, w.block + va, u);
+      sum += weights(s, w.pf[u], x.ref, u);
+    }
+    const bool trip = __builtin_amdgcn_ballot_w64(!(sum <= w.most)) != 0;
+    if (__builtin_expect(trip, 0)) {
+      const float top = Base::largest(s, 1.f), old = reference(x, w);
+      const bool without = old == kNoKeys;
+      const float above = kFolds && without ? top : kFolds ? top + old : top;  // the block's largest score
+      const float ref = above - old > kMaxLag ? above : old, alpha = __builtin_amdgcn_exp2f(old - ref);
+      x.sum *= alpha;
+      Base::scale_by(x, alpha);
+      if constexpr (kFolds) {
+        const float by = ref == kNoKeys ? 0.f : without ? ref : ref - old, less = ref == kNoKeys ? 0.f : ref == 0.f ? -0.f : -ref;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          s[v] -= by;
+          w.less_ref[v] = less;
+        }
+        asm volatile("" : "+v"(w.less_ref));  // (16 registers: one would be copied to them in every step)
+        w.most = __builtin_amdgcn_ballot_w64(ref == kNoKeys) != 0 ? -1.f : kTripSum;
+      } else {
+        x.ref = ref;
+      }
+      sum = weights(s, w.pf[0], ref, 0);
+      sum += weights(s, w.pf[1], ref, 1);
+    }
+    if constexpr (Base::kAlone) __builtin_amdgcn_s_setprio(0);
+    x.sum += sum;
+    w.block = block;
   }
 
   // Tiles [from, to) of the keys, as Unit::walk.  q_row(): the lane's row of Q, for rows of bf16 (asked for when it comes to them).
   template <class QueryRow>
-  __device__ static __forceinline__ void walk(Result& x, const QueryParts<D>& q, QueryRow q_row, char* lds_all, const Keys& k, const SegTable& seg,
+  __device__ static __forceinline__ void walk(Result& x, const Query& q, QueryRow q_row, char* lds_all, const Keys& k, const SegTable& seg,
                                               int from, int to, float c, bool active) {
-    const int lane = threadIdx.x & 63, member = threadIdx.x;
+    int lane = threadIdx.x & 63, member = threadIdx.x;
+    asm volatile("" : "+v"(lane));  // (not kept for what follows)
     const int t8 = min(Base::tiles_of_codes(k), to);
     int it = from;
     const int ka = k_lane4(lane), va = Base::v_lane(lane) - Base::kTensor + kOfK;
+    int kp = kPowers + 32 * (lane & 31) + 4 * ((lane & 31) >> 3);
+    asm volatile("" : "+v"(kp));  // (one register)
     Staged s;
     Aim to_come;
     auto load = [&](Staged& y, int i) {
@@ -241,27 +326,25 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
     }
     if (it >= to) return;
     Behind w;
-    w.rescale = false;
-    w.first = true;
-    w.alpha = 1.f;
-    w.block = 0;
+    w.block = 0;  // (weights of 0 for what lies there)
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) w.pf[u] = u32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w.pf[u][e] = (__bf16)0.f;
+    for (int v = 0; v < 16; ++v) w.less_ref[v] = 0.f;
+    w.most = kFolds ? -1.f : kTripSum;
     KeyCodes kc;
-    if (it < t8) load_codes(kc, lds_all, slot, 0, ka, lane);
+    if (it < t8) load_codes(kc, lds_all, slot, 0, ka, kp, lane);
     // tiles of which everything is known have no branch between their instructions
     while (it + 3 < t8) {
       aim_codes(to_come, k, seg, it + 3, member);
       if constexpr (kTile == 64)
-        step_codes<true>(x, w, kc, q, lds_all, va, slot, 32, c, lane, [&]() { load_codes(kc, lds_all, slot, 1, ka, lane); });
-      step_codes<true>(x, w, kc, q, lds_all, va, slot + (kTile - 32) * RB, 32, c, lane, [&]() {
+        step_codes<true>(x, w, kc, q, lds_all, va, slot, 32, lane, [&]() { load_codes(kc, lds_all, slot, 1, ka, kp, lane); });
+      step_codes<true>(x, w, kc, q, lds_all, va, slot + (kTile - 32) * RB, 32, lane, [&]() {
         if constexpr (kTile == 32) __syncthreads();
         store_codes(s, lds_all, after, member);
         fetch_codes(s, to_come, k, member);
         if constexpr (kTile == 64) __syncthreads();
-        load_codes(kc, lds_all, next, 0, ka, lane);
+        load_codes(kc, lds_all, next, 0, ka, kp, lane);
       });
       next_tile();
     }
@@ -269,17 +352,24 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
       if (it + 3 < to) aim_any(to_come, k, seg, it + 3, member);
       int left = valid(k, it), done = 0;
       if (kTile == 64 && left > 32) {
-        step_codes<true>(x, w, kc, q, lds_all, va, slot, 32, c, lane, [&]() { load_codes(kc, lds_all, slot, 1, ka, lane); });
+        step_codes<true>(x, w, kc, q, lds_all, va, slot, 32, lane, [&]() { load_codes(kc, lds_all, slot, 1, ka, kp, lane); });
         done = 32;
       }
-      step_codes<false>(x, w, kc, q, lds_all, va, slot + done * RB, left - done, c, lane, [&]() {
+      step_codes<false>(x, w, kc, q, lds_all, va, slot + done * RB, left - done, lane, [&]() {
         turn_over();
-        if (it + 1 < t8) load_codes(kc, lds_all, next, 0, ka, lane);
+        if (it + 1 < t8) load_codes(kc, lds_all, next, 0, ka, kp, lane);
       });
       next_tile();
     }
     if constexpr (kExt) {
       if (it < to) {
+        typename Base::Behind w2;
+        w2.pf[0] = __builtin_bit_cast(bf16x8, w.pf[0]);
+        w2.pf[1] = __builtin_bit_cast(bf16x8, w.pf[1]);
+        x.ref = reference(x, w);
+        w2.alpha = 1.f;
+        w2.block = w.block;
+        w2.rescale = w2.first = false;
         bf16x8 qf[KS], kf[KS];
         const char* row = q_row();
 #pragma unroll
@@ -292,10 +382,10 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
           while (it + 3 < to && (it - 1 >= t8 || it == from)) {  // (Unit::walk: behind a tile of two blocks)
             Base::template aim<Base::kRowsOnly>(to_come, k, seg, it + 3, member);
             if constexpr (kTile == 64)
-              Base::template step<true>(x, w, kf, qf, lds_all, kr, va, slot, 32, c, lane, [&]() {
+              Base::template step<true>(x, w2, kf, qf, lds_all, kr, va, slot, 32, c, lane, [&]() {
                 if constexpr (kAhead) Base::load_k(kf, lds_all, slot + kr + 32 * RB);
               });
-            Base::template step<true>(x, w, kf, qf, lds_all, kr, va, slot + (kTile - 32) * RB, 32, c, lane, [&]() {
+            Base::template step<true>(x, w2, kf, qf, lds_all, kr, va, slot + (kTile - 32) * RB, 32, c, lane, [&]() {
               if constexpr (kTile == 32) __syncthreads();
               Base::template store<Base::kRowsOnly>(s, lds_all, after, k, it + 2, member);
               Base::template fetch<Base::kRowsOnly>(s, to_come, k, it + 3, member);
@@ -307,12 +397,12 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
           if (it + 3 < to) Base::template aim<Base::kRowsOnly>(to_come, k, seg, it + 3, member);
           int left = valid(k, it), done = 0;
           if (kTile == 64 && left > 32) {
-            Base::template step<false>(x, w, kf, qf, lds_all, kr, va, slot, 32, c, lane, [&]() {
+            Base::template step<false>(x, w2, kf, qf, lds_all, kr, va, slot, 32, c, lane, [&]() {
               if constexpr (kAhead) Base::load_k(kf, lds_all, slot + kr + 32 * RB);
             });
             done = 32;
           }
-          Base::template step<false>(x, w, kf, qf, lds_all, kr, va, slot + done * RB, left - done, c, lane, [&]() {
+          Base::template step<false>(x, w2, kf, qf, lds_all, kr, va, slot + done * RB, left - done, c, lane, [&]() {
             __syncthreads();
             if (it + 2 < to) {
               Base::template store<Base::kRowsOnly>(s, lds_all, after, k, it + 2, member);
@@ -322,9 +412,13 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
           });
           next_tile();
         }
+        Base::finish(x, w2, lds_all, va);
+        return;
       }
     }
-    Base::finish(x, w, lds_all, va);
+    x.ref = reference(x, w);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) Base::add_values(x, __builtin_bit_cast(bf16x8, w.pf[u]), lds_all, w.block + va, u);
   }
 };
 

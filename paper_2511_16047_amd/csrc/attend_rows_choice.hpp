@@ -1,4 +1,4 @@
-// How the launches of attend_rows.hpp's two kernels are divided: plain host code.
+// How the launches of attend_rows.hpp's and attend_four.hpp's kernels are divided: plain host code.
 #pragma once
 #include <algorithm>
 #include <cmath>
@@ -112,6 +112,60 @@ inline Division divide(int head_dim, long long units, long long n, int keys) {
     }
   }
   return d;
+}
+
+// ---- keys in 4 bits (attend_codes.hip, cross.hip)
+// us that a launch of form f is estimated to take, whose workgroups share the keys of a row tile by `splits`.  A wave walks its blocks of 32
+// keys in rounds, a block taking a wave by itself `alone`, and waves that share a SIMD `shared` each once that is longer, `around` a workgroup:
+// arguments, Q and its parts, first tiles, O.  Beside it K, V, Q and O come from memory (5 TB/s) and K and V from the L2s again for every row
+// tile (lone waves 10 TB/s, teams 6.5); the three are added in squares.  Splits cost a launch and the way of their sums.
+// The constants are those that fit 322 shapes best, 310 of them drawn, 1 to 25 forms and splits each (MI355X; rms 0.14 of the time); the choice
+// then takes 1.019 of the best on average, the rule of 16-bit keys 1.078 (up to 2.97).  us, that rule / this: head dim 128, 64 units, 4 rows x 14400
+// 48 / 25; head dim 64, 1024 x 1 x 4000 115 / 45, 288 x 1 x 9266 101 / 42, 143 x 8 x 214 x 35 38 / 30.
+inline double estimate4(int head_dim, double units, double n, double keys, Form f, int splits) {
+  struct Times {
+    double alone, shared, around;
+  };
+  const bool wide = head_dim == 128;
+  const int w = f.team_waves, which = w == 1 ? (f.teams == 1 ? 0 : f.teams == 4 ? 1 : 2) : w == 4 ? 3 : 4;
+  static const Times times[2][5] = {{{0.52, 0.27, 1.5}, {0.48, 0.26, 2.2}, {0.42, 0.28, 1.5}, {0.40, 0.23, 2.6}, {0.32, 0.21, 2.9}},
+                                    {{0.68, 0.27, 1.6}, {0.65, 0.18, 3.3}, {0.50, 0.47, 3.4}, {0.48, 0.30, 3.4}, {0.38, 0.35, 3.7}}};
+  const Times& t = times[wide][which];
+  const int waves = w * f.teams, fit = (w == 1 ? (wide ? 8 : 12) : w == 4 ? (wide ? 12 : 16) : (wide ? 8 : 16)) / waves;
+  const double tiles = std::ceil(n / (32 * w)), groups = units * tiles, blocks = std::ceil(keys / 32), tile = w == 8 ? 2 : 1;
+  const double mine = w == 1 ? std::ceil(blocks / (f.teams * splits)) : std::ceil(std::ceil(blocks / tile) / splits) * tile;
+  const double to_a_cu = std::ceil(groups * splits / 256), places = fit < 1 ? 1 : fit, together = std::fmin(to_a_cu, places) * waves / 4;
+  const double busy = std::ceil(n / 32) / (tiles * w);  // waves of a team that have rows; the others bring keys
+  const double block = std::fmax(t.alone, together * (t.shared * busy + (w > 1 ? 0.01 : 0)));
+  const double walk = std::fmax(1, to_a_cu / places) * (mine * block + t.around);
+  const double kv = keys * head_dim * 1.0625, memory = units * (kv + 4 * n * head_dim) / 5e6, l2 = groups * kv / (w == 1 ? 10e6 : 6.5e6);
+  const double sums = splits == 1 ? 0 : 1.9 + 0.07 * splits + units * n * splits * (head_dim + 2) * 8 / 3e6;
+  return 2.4 + std::sqrt(walk * walk + memory * memory + l2 * l2) + sums;
+}
+
+// The form and the splits, up to `most`, that are estimated to be shortest.  Each team has a block, each wave of a split two.
+inline Division divide4(int head_dim, long long units, long long n, long long keys, int most) {
+  static const Form forms[5] = {{1, 1}, {1, 4}, {1, 8}, {4, 1}, {8, 1}};
+  static const int runs[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48};
+  Division best{1, 1, 1};
+  double least = 0;
+  const long long blocks = (keys + 31) / 32;
+  for (const Form& f : forms) {
+    const int w = f.team_waves, waves = w * f.teams;
+    const long long groups = units * ((n + 32 * w - 1) / (32 * w)), trips = (keys + (w == 8 ? 64 : 32) * f.teams - 1) / ((w == 8 ? 64 : 32) * f.teams);
+    if (f.teams > 1 && f.teams > blocks) continue;
+    // (a launch has fewer than 2^32 threads; waves by themselves have the fewest, and the caller sees to it that they fit)
+    if (waves > 1 && (groups + 7) * 64 * waves > 0xffffffffll) continue;
+    for (const int s : runs) {
+      if (s > 1 && (s > most || trips / s < 2 || groups > 1200 || groups * s > (waves == 1 ? 4096 : 2048))) break;
+      const double us = estimate4(head_dim, (double)units, (double)n, (double)keys, f, s);
+      if (least == 0 || us < least) {
+        least = us;
+        best = {w, f.teams, s};
+      }
+    }
+  }
+  return best;
 }
 
 }  // namespace rows

@@ -59,13 +59,13 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   const int n_rows = a.group * a.q_tokens, base = tile * U::kRows + 32 * (wave % kTeamWaves);
   const bool active = base < n_rows;
   // byte offset of the lane's row in Q or O (found twice, not kept over the walk)
-  auto row_at = [&](const RowMap& m, int of_lane) {
+  auto row_at = [&](const RowMap& m, int of_lane, int q_tokens) {
     const int row = min(base + (of_lane & 31), n_rows - 1);
-    const int head = a.group == 1 ? 0 : row / a.q_tokens, token = row - head * a.q_tokens;
+    const int head = a.group == 1 ? 0 : row / q_tokens, token = row - head * q_tokens;
     return b * m.batch + ((long long)g * a.group + head) * m.head + token * m.tok;
   };
 
-  const char* q_row = a.q + row_at(a.q_map, lane);
+  const char* q_row = a.q + row_at(a.q_map, lane, a.q_tokens);
   rows::Keys keys{};
   if constexpr (kBits == 16) {
     const long long kb = a.offsets ? first * a.k_map.tok : b * a.k_map.batch, vb = a.offsets ? first * a.v_map.tok : b * a.v_map.batch;
@@ -89,8 +89,8 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   SegTable none;
   none.n = 0;
   if constexpr (kParts) {
-    rows::QueryParts<D> parts;
-    rows::split_query<D>(parts, q_row, h);
+    typename Team::Query parts;
+    rows::split_query(parts, q_row, h, a.scale_log2e);
     Team::walk(x, parts, [&]() { return q_row; }, lds, keys, none, from, to, a.scale_log2e, active);
   } else {
     rows::bf16x8 qf[U::KS];
@@ -101,12 +101,14 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   U::meet(x, lds);
   const int late = U::fresh(threadIdx.x) & 63;
   if (a.splits == 1) {
-    U::put(x, reinterpret_cast<__bf16*>(a.o + row_at(a.o_map, late)), active && base + (late & 31) < n_rows);
+    int q_tokens = a.q_tokens;
+    if constexpr (kParts) asm volatile("" : "+s"(q_tokens));
+    U::put(x, reinterpret_cast<__bf16*>(a.o + row_at(a.o_map, late, q_tokens)), active && base + (late & 31) < n_rows);
     return;
   }
   float* mine = a.workspace + (((long long)at.bh * a.row_tiles + tile) * a.splits + split) * rows::partial_floats(U::kRows, D);
   const int local = 32 * (wave % kTeamWaves) + (late & 31);
-  if (active) U::put_partial(x, mine + local * D);
+  if (active && base + (late & 31) < n_rows) U::put_partial(x, mine + local * D);
   if (wave < kTeamWaves && late < 32) *reinterpret_cast<float2*>(mine + U::kRows * D + 2 * local) = make_float2(x.ref, x.sum);
 }
 
@@ -176,13 +178,24 @@ hipError_t go(CrossArgs& a, hipStream_t st) {
 
 }  // namespace
 
-uint64_t cross_workspace_bytes(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) {
+static rows::Division division(bool four_bits, int head_dim, int units, int rows, int kv_tokens) {
+  return four_bits ? rows::divide4(head_dim, units, rows, kv_tokens, 48) : rows::divide(head_dim, units, rows, kv_tokens);
+}
+
+static uint64_t workspace_bytes(bool four_bits, int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) {
   const int units = batch * kv_heads, rows = heads / kv_heads * q_tokens;
   if (units == 0 || rows == 0 || kv_tokens == 0) return 0;
-  const rows::Division d = rows::divide(head_dim, units, rows, kv_tokens);
+  const rows::Division d = division(four_bits, head_dim, units, rows, kv_tokens);
   if (d.splits == 1) return 0;
   const uint64_t row_tiles = (rows + 32 * d.team_waves - 1) / (32 * d.team_waves);
   return (uint64_t)units * row_tiles * d.splits * rows::partial_floats(32 * d.team_waves, head_dim) * sizeof(float);
+}
+
+uint64_t cross_workspace_bytes(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) {
+  return workspace_bytes(false, batch, heads, kv_heads, head_dim, q_tokens, kv_tokens);
+}
+uint64_t cross_workspace_bytes4(int batch, int heads, int kv_heads, int head_dim, int q_tokens, int kv_tokens) {
+  return workspace_bytes(true, batch, heads, kv_heads, head_dim, q_tokens, kv_tokens);
 }
 
 hipError_t launch_cross(const CrossCall& c, hipStream_t st) {
@@ -211,15 +224,15 @@ hipError_t launch_cross(const CrossCall& c, hipStream_t st) {
     a.groups_at = units * a.held_rows * (c.head_dim / 2);
   }
   if (a.n_units == 0 || a.group * a.q_tokens == 0) return hipSuccess;
-  const rows::Division d = rows::divide(c.head_dim, a.n_units, a.group * a.q_tokens, a.kv_tokens);
+  const rows::Division d = division(c.four_bits, c.head_dim, a.n_units, a.group * a.q_tokens, a.kv_tokens);
   a.splits = a.workspace ? d.splits : 1;
   if (c.four_bits) {
     if (c.head_dim == 64) {
-      if (d.team_waves == 1) return d.teams == 1 ? go<64, 1, 1, 3, 4>(a, st) : go<64, 1, 4, 3, 4>(a, st);
+      if (d.team_waves == 1) return d.teams == 1 ? go<64, 1, 1, 3, 4>(a, st) : d.teams == 4 ? go<64, 1, 4, 3, 4>(a, st) : go<64, 1, 8, 2, 4>(a, st);
       return d.team_waves == 4 ? go<64, 4, 1, 4, 4>(a, st) : go<64, 8, 1, 4, 4>(a, st);
     }
-    if (d.team_waves == 1) return d.teams == 1 ? go<128, 1, 1, 2, 4>(a, st) : go<128, 1, 4, 2, 4>(a, st);
-    return go<128, 4, 1, 2, 4>(a, st);
+    if (d.team_waves == 1) return d.teams == 1 ? go<128, 1, 1, 2, 4>(a, st) : d.teams == 4 ? go<128, 1, 4, 2, 4>(a, st) : go<128, 1, 8, 2, 4>(a, st);
+    return d.team_waves == 4 ? go<128, 4, 1, 3, 4>(a, st) : go<128, 8, 1, 2, 4>(a, st);
   }
   if (c.head_dim == 64) {
     if (d.team_waves == 1) return d.teams == 1 ? go<64, 1, 1, 4>(a, st) : go<64, 1, 4, 4>(a, st);

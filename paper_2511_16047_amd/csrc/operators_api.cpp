@@ -58,6 +58,12 @@ int check_cross(const amskv_cross* x) {
   return AMSKV_OK;
 }
 
+uint64_t workspace_of(const amskv_cross* x) {
+  if (x->heads == 0) return 0;
+  auto bytes = x->dtype == AMSKV_DTYPE_BF16_KV4 ? amskv::cross_workspace_bytes4 : amskv::cross_workspace_bytes;
+  return bytes(x->batch, x->heads, x->kv_heads, x->head_dim, x->q_tokens, x->kv_tokens);
+}
+
 // Bytes of a held tensor of this shape in 4 bits.
 int64_t held_bytes(const amskv_cross* x, bool packed) {
   const int64_t units = packed ? x->kv_heads : (int64_t)x->batch * x->kv_heads;
@@ -170,7 +176,7 @@ int32_t amskv_rotate(const amskv_rope* rope, int32_t dtype, int32_t head_dim, in
 int32_t amskv_cross_workspace_bytes(const amskv_cross* x, uint64_t* bytes_out) {
   if (!bytes_out) return AMSKV_ERR_INVALID_ARG;
   if (int rc = check_cross(x)) return rc;
-  *bytes_out = x->heads == 0 ? 0 : amskv::cross_workspace_bytes(x->batch, x->heads, x->kv_heads, x->head_dim, x->q_tokens, x->kv_tokens);
+  *bytes_out = workspace_of(x);
   return AMSKV_OK;
 }
 
@@ -211,7 +217,7 @@ int32_t amskv_cross_attend(const amskv_cross* x, const void* Q_dev, const void* 
   if (x->batch == 0 || x->heads == 0 || x->q_tokens == 0) return AMSKV_OK;
   // (K and V may be absent where there can be no states)
   if (!Q_dev || !O_dev || ((!K_dev || !V_dev) && x->kv_tokens > 0 && (!offsets_dev || x->kv_rows > 0))) return AMSKV_ERR_INVALID_ARG;
-  if (workspace_dev && workspace_bytes < amskv::cross_workspace_bytes(x->batch, x->heads, x->kv_heads, x->head_dim, x->q_tokens, x->kv_tokens))
+  if (workspace_dev && workspace_bytes < workspace_of(x))
     return AMSKV_ERR_ARENA_TOO_SMALL;
   c.q = Q_dev;
   c.k = K_dev;

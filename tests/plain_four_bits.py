@@ -40,19 +40,23 @@ def held(x):
 
 
 def attention(q, k, v, scale):
-    """As plain.attention, over held k and v, with the products' rounding of Q: an element of a group whose largest is m, 2^a the least
-    power with m <= 7.5 * 2^a, is exact if it is 2^a at least or a multiple of 2^(a - 7), else off by 2^(a - 8) at most; that moves a
-    score by at most the sum of these times |k|, and a weight, relative to the others', by exp of twice as much.
+    """As plain.attention, over held k and v, with the products' rounding of Q: y = q * scale * log2(e), whose group's largest is m, 2^a the
+    least power with m <= 7.5 * 2^a, is held as the number of 4 significant bits next to y * 2^-a, times 2^a, and the number of 4 significant
+    bits (steps of 1/8 at least) next to 2^4 times what is left: off by at most 2^(a - 7) where |y| is about 4 * 2^a and more, else 2^(a - 8).
+    (A y on the grid that the two have there is off by its roundings in fp32 alone, 2^-20 of it at most.)  That moves a score, as a power of
+    two, by at most the sum of these times |k|, and a weight, relative to the others', by a factor of 2 to twice that.
 
     Weights of 2^-120 of the largest and less may vanish: a reference that is up to 2^6 below the largest weight of its time is left for
     one more than 2^126 above it by a factor that fp32 flushes to 0 (held values may be 0 where the weight is 1, so that this shows)."""
     q, k, v = (x.double() for x in (q, k, v))
     o, bound = plain.attention(q, k, v, scale)
-    y = q.unflatten(-1, (-1, GROUP))
-    a = _least_exponent(y.abs().amax(dim=-1, keepdim=True), 7.5, -120, 130)
-    step = _two_to(a - 7)
-    off = torch.where((y.abs() >= 128 * step) | (torch.remainder(y, step) == 0), torch.zeros_like(y), step / 2).flatten(-2)
-    far = (off @ k.abs().transpose(-1, -2)).amax(dim=-1, keepdim=True) * scale
+    y = (q * (scale * math.log2(math.e))).unflatten(-1, (-1, GROUP))
+    one = _two_to(_least_exponent(y.abs().amax(dim=-1, keepdim=True), 7.5, -110, 130))
+    size = y.abs() / one
+    grid = one * torch.where(size >= 3.99, 2.0 ** -5, torch.where(size >= 1.99, 2.0 ** -6, 2.0 ** -7))
+    on_it = (y - torch.round(y / grid) * grid).abs() <= 2.0 ** -20 * y.abs()
+    off = torch.where(on_it, 2.0 ** -20 * y.abs(), one * torch.where(size >= 3.9, 2.0 ** -7, 2.0 ** -8)).flatten(-2)
+    far = (off @ k.abs().transpose(-1, -2)).amax(dim=-1, keepdim=True) * math.log(2)
     s = q @ k.transpose(-1, -2) * scale
     p, rel = torch.softmax(s, dim=-1), torch.exp(s - s.amax(dim=-1, keepdim=True))
     size, lost = p @ v.abs(), torch.where(rel <= 1.01 * 2.0 ** -120, p, torch.zeros_like(p)) @ v.abs()

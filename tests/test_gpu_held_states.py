@@ -26,6 +26,7 @@ class Case:
         self.q = _normal(B, H, Tq, D, seed=seed)
         if sharp != 1.0:   # queries of few bits, which the products take as they are
             self.q = torch.round(self.q).clamp(-2, 2) * sharp
+        self.scale = 1 / math.sqrt(D) if sharp == 1.0 else 0.125 * math.log(2)   # (under which they are taken as they are)
         self.q = self.q.bfloat16()
         k, v = ((_normal(B, Tk, Hkv, D, seed=seed + i) * torch.exp(0.5 * _normal(Hkv, D, seed=8))).bfloat16() for i in (1, 2))
         for b, n in enumerate(lengths):    # nobody may look behind a batch element's last state
@@ -48,7 +49,8 @@ class Case:
             kw = {"lengths": torch.tensor(lengths, dtype=torch.int32, device="cuda")}
         self.kw = kw
         qs = amskv.Strides(H * Tq * D, Tq * D, D)
-        self.x = amskv.Cross(batch=B, heads=H, kv_heads=Hkv, head_dim=D, dtype=KV4, q_tokens=Tq, kv_tokens=Tk, kv_rows=rows, q=qs, k=st, v=st, o=qs)
+        self.x = amskv.Cross(batch=B, heads=H, kv_heads=Hkv, head_dim=D, dtype=KV4, q_tokens=Tq, kv_tokens=Tk, kv_rows=rows, q=qs, k=st, v=st, o=qs,
+                             softmax_scale=0.0 if sharp == 1.0 else self.scale)
         need = amskv.amskv_cross_held_bytes(self.x, packed=layout == "packed")
         assert need == (Hkv * rows if layout == "packed" else B * Hkv * Tk) * (D // 2 + D // 32)
         self.need, self.buffers = need, [torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(2)]
@@ -93,7 +95,7 @@ class Case:
                 assert bool((out[b] == 0).all())
                 continue
             k, v = (plain.held(x[b, :n]).transpose(0, 1).repeat_interleave(self.G, dim=0) for x in self.kv)
-            want, bound = plain.attention(self.q[b], k, v, 1 / math.sqrt(self.D))
+            want, bound = plain.attention(self.q[b], k, v, self.scale)
             off = (out[b].double() - want).abs()
             assert bool((off <= bound).all()), "batch element %d of %d states: %.3f of the bound" % (b, n, float((off / bound).max()))
 
