@@ -522,7 +522,7 @@ int32_t amskv_cross_held_bytes(const amskv_cross* cross, int32_t packed, uint64_
 
 /* K_dev and V_dev (bf16, strides cross->k and cross->v) into held tensors; either pair may be NULL.  Rows that hold states are
  * read and written: row j < length of b where padded, rows offsets[0] .. offsets[batch] - 1 of the axis where packed, all of
- * them if neither is given; the others stay as they were.  Elements of those rows must be finite.  Of *cross the queries' members and
+ * them if neither is given (up to 2^36 rows of all units); the others stay as they were.  Elements of those rows must be finite.  Of *cross the queries' members and
  * strides q and o are not used here.  What is written overlaps nothing else that is passed; the same pointer in two such roles is
  * refused.  One launch.  Asynchronous on `stream`. */
 int32_t amskv_cross_hold(const amskv_cross* cross, const void* K_dev, const void* V_dev, void* K_held_dev, void* V_held_dev,

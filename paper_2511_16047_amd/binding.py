@@ -97,11 +97,11 @@ class Cross(C.Structure):
 
 _lib = None
 _lookup = None   # torch's raw stream lookup, once asked for
-_append = _attend = _append_rotary = _rotate = _cross = None   # set by load_library
+_append = _attend = _append_rotary = _rotate = _cross = _hold = _export = None   # set by load_library
 
 
 def load_library() -> C.CDLL:
-    global _lib, _append, _attend, _append_rotary, _rotate, _cross
+    global _lib, _append, _attend, _append_rotary, _rotate, _cross, _hold, _export
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -183,13 +183,15 @@ def load_library() -> C.CDLL:
         from . import _pycalls
     except ImportError:   # not built for this interpreter: the same calls, 3 us slower each
         _append, _attend = _by_ctypes(lib.amskv_append_scale), _by_ctypes(lib.amskv_attend)
-        _append_rotary = _rotate = _cross = _not_built
+        _append_rotary = _rotate = _cross = _hold = _export = _not_built
     else:
         _append, _attend = _pycalls.append_scale, _pycalls.attend
         _pycalls.bind(C.cast(lib.amskv_append_scale, vp).value, C.cast(lib.amskv_attend, vp).value, _raw_stream_lookup)
         _append_rotary, _rotate, _cross = _pycalls.append_scale_rotary, _pycalls.rotate, _pycalls.cross_attend
         _pycalls.bind_operators(*(C.cast(f, vp).value for f in (lib.amskv_append_scale_rotary, lib.amskv_rotate, lib.amskv_cross_attend)),
                                 Rope, Strides, Cross)
+        _hold, _export = _pycalls.cross_hold, _pycalls.cross_export
+        _pycalls.bind_held(*(C.cast(f, vp).value for f in (lib.amskv_cross_hold, lib.amskv_cross_export)))
     _lib = lib
     return lib
 
@@ -532,11 +534,23 @@ def amskv_cross_held_bytes(cross, packed=False) -> int:
 
 def amskv_cross_hold(cross, K, V, K_held, V_held, lengths=None, offsets=None, stream=None):
     """K, V: bf16 states at the strides of `cross`; K_held, V_held: device tensors of amskv_cross_held_bytes bytes each."""
-    _check(load_library().amskv_cross_hold(cross, _ptr(K), _ptr(V), _ptr(K_held), _ptr(V_held), _ptr(lengths), _ptr(offsets), _stream(stream)),
-           "amskv_cross_hold")
+    if _lib is None:
+        load_library()
+    try:
+        status = _hold(cross, K, V, K_held, V_held, lengths, offsets, stream)
+    except _UNUSUAL:
+        status = _lib.amskv_cross_hold(cross, _ptr(K), _ptr(V), _ptr(K_held), _ptr(V_held), _ptr(lengths), _ptr(offsets), _stream(stream))
+    if status:
+        _check(status, "amskv_cross_hold")
 
 
 def amskv_cross_export(cross, K_held, V_held, K_out, V_out, lengths=None, offsets=None, stream=None):
     """The held values as bf16, at the strides of `cross`."""
-    _check(load_library().amskv_cross_export(cross, _ptr(K_held), _ptr(V_held), _ptr(K_out), _ptr(V_out), _ptr(lengths), _ptr(offsets),
-                                             _stream(stream)), "amskv_cross_export")
+    if _lib is None:
+        load_library()
+    try:
+        status = _export(cross, K_held, V_held, K_out, V_out, lengths, offsets, stream)
+    except _UNUSUAL:
+        status = _lib.amskv_cross_export(cross, _ptr(K_held), _ptr(V_held), _ptr(K_out), _ptr(V_out), _ptr(lengths), _ptr(offsets), _stream(stream))
+    if status:
+        _check(status, "amskv_cross_export")

@@ -11,26 +11,27 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kRows = 4;               // rows of a lane under way
-constexpr long long kMostGroups = 1 << 20;  // workgroups; beyond that they take several blocks of rows
+constexpr unsigned kMostGroups = 1 << 20;  // workgroups; beyond that they take several blocks of rows
 
 struct HoldArgs {
   char *x[2];
   unsigned char* held[2];
   RowMap map[2];
   const int *lengths, *offsets;
-  long long rows, units, blocks, groups_at;  // rows of a unit, blocks of rows to a unit, bytes of codes
+  long long rows, groups_at;  // rows of a unit, bytes of codes
+  unsigned blocks, all_blocks;  // blocks of rows to a unit, of all units
   int kv_heads, batch, kv_tokens;
 };
 
 // rows [first, end) of a unit that hold states
-__device__ __forceinline__ void live_rows(const HoldArgs& a, long long unit, long long& first, long long& end) {
+__device__ __forceinline__ void live_rows(const HoldArgs& a, unsigned b, long long& first, long long& end) {
   first = 0;
   end = a.rows;
   if (a.offsets != nullptr) {
     first = min(max((long long)a.offsets[0], 0ll), a.rows);
     end = min(max((long long)a.offsets[a.batch], 0ll), a.rows);
   } else if (a.lengths != nullptr) {
-    end = min(max(a.lengths[unit / a.kv_heads], 0), a.kv_tokens);
+    end = min(max(a.lengths[b], 0), a.kv_tokens);
   }
 }
 
@@ -42,16 +43,18 @@ __device__ __forceinline__ float quad_max(float m) {
 
 template <int D, bool kBack>
 __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a) {
+  fetch_arguments<sizeof(HoldArgs)>();
   constexpr int kLanes = D / 8, kAtOnce = 256 / kLanes;  // lanes of a row, rows of a workgroup at a time
   const int tensor = blockIdx.y;
   if (a.x[tensor] == nullptr) return;
   const int c = threadIdx.x % kLanes, r = threadIdx.x / kLanes;
   const RowMap& m = a.map[tensor];
-  for (long long block = blockIdx.x; block < a.units * a.blocks; block += gridDim.x) {
-    const long long unit = block / a.blocks, row0 = (block - unit * a.blocks) * (kAtOnce * kRows) + r;
+  for (unsigned block = blockIdx.x; block < a.all_blocks; block += gridDim.x) {
+    // the heads of a block of rows, which lie side by side in a token-major tensor, go to workgroups of one time
+    const unsigned rest = block / (unsigned)a.kv_heads, g = block - rest * a.kv_heads, b = rest / a.blocks;
+    const long long row0 = (long long)(rest - b * a.blocks) * (kAtOnce * kRows) + r, unit = (long long)b * a.kv_heads + g;
     long long first, end;
-    live_rows(a, unit, first, end);
-    const long long b = a.offsets != nullptr ? 0 : unit / a.kv_heads, g = unit - b * a.kv_heads;
+    live_rows(a, b, first, end);
     char* x = a.x[tensor] + b * m.batch + g * m.head + 16 * c;
     unsigned char* codes = a.held[tensor] + unit * a.rows * (D / 2) + 4 * c;
     unsigned char* groups = a.held[tensor] + a.groups_at + unit * a.rows * (D / AMSKV_KV4_GROUP) + c / 4;
@@ -109,15 +112,17 @@ hipError_t go(const HoldCall& c, hipStream_t st) {
   a.lengths = c.lengths;
   a.offsets = c.offsets;
   a.rows = c.offsets ? c.kv_rows : c.kv_tokens;
-  a.units = c.offsets ? c.kv_heads : (long long)c.batch * c.kv_heads;
-  a.groups_at = a.units * a.rows * (c.head_dim / 2);
+  const long long units = c.offsets ? c.kv_heads : (long long)c.batch * c.kv_heads;
+  a.groups_at = units * a.rows * (c.head_dim / 2);
   a.kv_heads = c.kv_heads;
   a.batch = c.batch;
   a.kv_tokens = c.kv_tokens;
   const int per = 256 / (c.head_dim / 8) * kRows;
-  a.blocks = (a.rows + per - 1) / per;
-  if (a.units * a.blocks == 0) return hipSuccess;
-  const dim3 grid((unsigned)(a.units * a.blocks < kMostGroups ? a.units * a.blocks : kMostGroups), 2);
+  a.blocks = (unsigned)((a.rows + per - 1) / per);
+  if (units * a.blocks > 0x7fffffffll) return hipErrorInvalidValue;  // (the loop's counter)
+  a.all_blocks = (unsigned)(units * a.blocks);
+  if (a.all_blocks == 0) return hipSuccess;
+  const dim3 grid(a.all_blocks < kMostGroups ? a.all_blocks : kMostGroups, 2);
   auto kernel = c.head_dim == 64 ? hold_kernel<64, kBack> : hold_kernel<128, kBack>;
   hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
   return hipGetLastError();

@@ -90,6 +90,7 @@ int hold(const amskv_cross* x, const void* k, const void* v, const void* k_held,
   if ((k && !map_of(&x->k, n, x->head_dim, 2, back, &c.k_map)) || (v && !map_of(&x->v, n, x->head_dim, 2, back, &c.v_map)))
     return AMSKV_ERR_INVALID_ARG;
   if (misaligned(k) || misaligned(v) || misaligned(k_held) || misaligned(v_held)) return AMSKV_ERR_INVALID_ARG;
+  if (n[0] * n[1] * n[2] > ((int64_t)1 << 36)) return AMSKV_ERR_INVALID_ARG;  // the launch counts blocks of 64 rows in 31 bits
   if (held_bytes(x, offsets_dev != nullptr) == 0 || (offsets_dev && x->batch == 0)) return AMSKV_OK;
   if ((!k && !v) || (k && !k_held) || (v && !v_held)) return AMSKV_ERR_INVALID_ARG;
   // what is written is no other tensor of the call

@@ -1,9 +1,9 @@
 // The calls that a model makes for every layer and scale -- amskv_append_scale, amskv_attend, amskv_append_scale_rotary,
-// amskv_rotate and amskv_cross_attend -- as a CPython extension: argument marshalling only, for binding.py (all other calls
+// amskv_rotate, amskv_cross_attend, amskv_cross_hold and amskv_cross_export -- as a CPython extension: argument marshalling only, for binding.py (all other calls
 // go through ctypes).  One image through a 16-layer stack is 320 of these calls and 160 short launches, and with ctypes and
 // torch's public stream lookup (about 3.6 us a call by itself) the host side took longer than the kernels: 1908 us a pass, 719
-// with this (launches included).  The library stays behind its C ABI: bind() and bind_operators() are given the addresses of the
-// functions.
+// with this (launches included).  The library stays behind its C ABI: bind(), bind_operators() and bind_held() are given the addresses
+// of the functions.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <cstdint>
@@ -16,11 +16,13 @@ typedef int32_t (*AppendRotary)(void*, int32_t, int32_t, const void*, const void
 typedef int32_t (*Rotate)(const void*, int32_t, int32_t, int32_t, int32_t, int32_t, const void*, int64_t, int32_t, const void*, const void*, void*,
                           const void*, void*);
 typedef int32_t (*Cross)(const void*, const void*, const void*, const void*, void*, const void*, const void*, void*, uint64_t, void*);
+typedef int32_t (*Held)(const void*, const void*, const void*, void*, void*, const void*, const void*, void*);
 Append append_fn = nullptr;
 Attend attend_fn = nullptr;
 AppendRotary append_rotary_fn = nullptr;
 Rotate rotate_fn = nullptr;
 Cross cross_fn = nullptr;
+Held hold_fn = nullptr, export_fn = nullptr;
 PyObject *rope_class = nullptr, *strides_class = nullptr, *cross_class = nullptr;
 PyObject* lookup = nullptr;  // asked once, when a call first leaves the stream to torch: (current device, current stream) functions
 PyObject *get_device = nullptr, *get_stream = nullptr;  // its answer; None: there is no device
@@ -184,6 +186,35 @@ PyObject* cross_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
+// (cross, K, V, K_held, V_held, lengths, offsets, stream), or the held tensors first -> status
+PyObject* held(Held fn, PyObject* const* a, Py_ssize_t n) {
+  int32_t status;
+  void *cross, *t[6], *st;
+  if (!arguments(n, 8, fn) || !structure(a[0], cross_class, &cross)) return nullptr;
+  for (int i = 0; i < 6; ++i)
+    if (!tensor(a[1 + i], &t[i])) return nullptr;
+  if (!stream(a[7], &st)) return nullptr;
+  Py_BEGIN_ALLOW_THREADS
+  status = fn(cross, t[0], t[1], t[2], t[3], t[4], t[5], st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+PyObject* cross_hold(PyObject*, PyObject* const* a, Py_ssize_t n) { return held(hold_fn, a, n); }
+PyObject* cross_export(PyObject*, PyObject* const* a, Py_ssize_t n) { return held(export_fn, a, n); }
+
+// bind_held(addresses of amskv_cross_hold, amskv_cross_export), after bind_operators()
+PyObject* bind_held(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void *f, *g;
+  if (n != 2) {
+    PyErr_SetString(PyExc_TypeError, "two arguments expected");
+    return nullptr;
+  }
+  if (!address(a[0], &f) || !address(a[1], &g)) return nullptr;
+  hold_fn = reinterpret_cast<Held>(f);
+  export_fn = reinterpret_cast<Held>(g);
+  Py_RETURN_NONE;
+}
+
 // bind_operators(addresses of amskv_append_scale_rotary, amskv_rotate, amskv_cross_attend, the classes Rope, Strides, Cross)
 PyObject* bind_operators(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 6) {
@@ -222,6 +253,9 @@ PyMethodDef methods[] = {
     {"append_scale_rotary", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(append_scale_rotary)), METH_FASTCALL, "amskv_append_scale_rotary"},
     {"rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rotate)), METH_FASTCALL, "amskv_rotate"},
     {"cross_attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cross_attend)), METH_FASTCALL, "amskv_cross_attend"},
+    {"cross_hold", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cross_hold)), METH_FASTCALL, "amskv_cross_hold"},
+    {"cross_export", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(cross_export)), METH_FASTCALL, "amskv_cross_export"},
+    {"bind_held", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind_held)), METH_FASTCALL, "function addresses"},
     {"bind_operators", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind_operators)), METH_FASTCALL, "function addresses and structures"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycalls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

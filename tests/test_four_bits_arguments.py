@@ -147,6 +147,9 @@ def test_held_directions():
     for rows in (-1, 1 << 31):
         for call in (_hold, _export):
             _refused(INVALID, call, cross=_cross(kv_rows=rows), offsets=A)
+    far = amskv.Strides(1 << 37, 1 << 33, 64)
+    for call in (_hold, _export):   # 2^36 rows and 2^26 more
+        _refused(INVALID, call, cross=_cross(batch=1025, heads=1, kv_heads=1, q_tokens=1, kv_tokens=1 << 26, k=far, v=far))
 
 
 @pytest.mark.parametrize("strides", [(2112, 64, 100), (-2112, 64, 192), (2112, 64, 1 << 41)], ids=str)
