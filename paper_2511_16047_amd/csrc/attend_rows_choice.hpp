@@ -120,7 +120,7 @@ inline Division divide(int head_dim, long long units, long long n, int keys) {
 // arguments, Q and its parts, first tiles, O.  Beside it K, V, Q and O come from memory (5 TB/s) and K and V from the L2s again for every row
 // tile (lone waves 10 TB/s, teams 6.5); the three are added in squares.  Splits cost a launch and the way of their sums.
 // The constants are those that fit 322 shapes best, 310 of them drawn, 1 to 25 forms and splits each (MI355X; rms 0.14 of the time); the choice
-// then takes 1.019 of the best on average, the rule of 16-bit keys 1.078 (up to 2.97).  us, that rule / this: head dim 128, 64 units, 4 rows x 14400
+// then takes 1.018 of the best on average, the rule of 16-bit keys 1.078 (up to 2.97).  us, that rule / this: head dim 128, 64 units, 4 rows x 14400
 // 48 / 25; head dim 64, 1024 x 1 x 4000 115 / 45, 288 x 1 x 9266 101 / 42, 143 x 8 x 214 x 35 38 / 30.
 inline double estimate4(int head_dim, double units, double n, double keys, Form f, int splits) {
   struct Times {
@@ -129,7 +129,7 @@ inline double estimate4(int head_dim, double units, double n, double keys, Form 
   const bool wide = head_dim == 128;
   const int w = f.team_waves, which = w == 1 ? (f.teams == 1 ? 0 : f.teams == 4 ? 1 : 2) : w == 4 ? 3 : 4;
   static const Times times[2][5] = {{{0.52, 0.27, 1.5}, {0.48, 0.26, 2.2}, {0.42, 0.28, 1.5}, {0.40, 0.23, 2.6}, {0.32, 0.21, 2.9}},
-                                    {{0.68, 0.27, 1.6}, {0.65, 0.18, 3.3}, {0.50, 0.47, 3.4}, {0.48, 0.30, 3.4}, {0.38, 0.35, 3.7}}};
+                                    {{0.68, 0.27, 1.6}, {0.65, 0.18, 3.3}, {0.50, 0.47, 3.4}, {0.48, 0.35, 2.6}, {0.38, 0.345, 3.7}}};
   const Times& t = times[wide][which];
   const int waves = w * f.teams, fit = (w == 1 ? (wide ? 8 : 12) : w == 4 ? (wide ? 12 : 16) : (wide ? 8 : 16)) / waves;
   const double tiles = std::ceil(n / (32 * w)), groups = units * tiles, blocks = std::ceil(keys / 32), tile = w == 8 ? 2 : 1;

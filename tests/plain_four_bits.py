@@ -32,7 +32,7 @@ def held(x):
     scale = _two_to(exponents(x))
     numbers = torch.tensor(NUMBERS, dtype=torch.float64, device=x.device)
     z = (y.abs() / scale).clamp(max=6.0)
-    hi = torch.searchsorted(numbers, z).clamp(max=7)
+    hi = torch.searchsorted(numbers, z.contiguous()).clamp(max=7)
     lo = (hi - 1).clamp(min=0)
     up, down = numbers[hi] - z, z - numbers[lo]
     out = torch.where((up < down) | ((up == down) & (hi % 2 == 0)), numbers[hi], numbers[lo])

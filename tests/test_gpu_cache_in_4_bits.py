@@ -205,6 +205,13 @@ def test_many_units_over_many_tokens(D, before):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("queries,before", [(576, 500), (512, 705), (505, 551), (576, 0), (551, 449)])
+def test_many_rows_over_many_tokens(D, queries, before):
+    for borrow in (False, True):
+        _drive(([(1, before)] if before else []) + [(1, queries)], 4, 16, D, [(0, 0, True)], seed=before, borrow_unretained=borrow)
+
+
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("layout", [COMPACT, PLANNED], ids=["compact", "planned"])
 @pytest.mark.parametrize("packed", [False, True])
 def test_many_units_of_short_segments(D, layout, packed):
@@ -283,6 +290,38 @@ def test_turned_on_the_way(pairing, D, rot):
             _check(o, turned, kk, vv, "scale %d" % s)
         ko, vo = c.read(0)
         assert torch.equal(ko.double(), kk) and torch.equal(vo.double(), vv)
+
+
+@pytest.mark.parametrize("D,rot,pairing", [(64, 48, amskv.AMSKV_ROPE_HALF), (128, 128, amskv.AMSKV_ROPE_INTERLEAVED)])
+def test_turned_out_of_one_projection(D, rot, pairing):
+    """Q, K and V side by side for each token; the last scale's keys are turned where they are and read in place."""
+    import plain_operators
+    sides, B, H = [(2, 2), (5, 9), (16, 17)], 2, 3
+    rope = amskv.Rope(rot_dim=rot, pairing=pairing, axes=2)
+    how = "half" if pairing == amskv.AMSKV_ROPE_HALF else "interleaved"
+    with Cache(sides, B, H, D, [(0, 0, True)], borrow_unretained=True) as c:
+        amskv.amskv_cache_set_io_layout(c.h, amskv.AMSKV_IO_TOKEN_MAJOR, H * D, 3 * H * D, H * D)
+        kept = []
+        for s, (a, b) in enumerate(sides):
+            T, last = a * b, s + 1 == len(sides)
+            x = _normal(B, T, 3, H, D, seed=s).bfloat16()
+            was = x.clone()
+            tab = torch.empty(T, rot // 2, 2, device="cuda")
+            t = torch.arange(T, device="cuda")
+            amskv.amskv_rope_table(rope, torch.stack((t // b, t % b), dim=1).double(), tab)
+            turned = torch.empty(B, T, H, D, dtype=torch.bfloat16, device="cuda")
+            o = torch.empty_like(turned)
+            amskv.amskv_append_scale_rotary(c.h, 0, s, rope, tab, x[:, :, 0], 3 * H * D, turned, x[:, :, 1], x[:, :, 2])
+            amskv.amskv_attend(c.h, 0, s, turned, o)
+            q, k, v = was.permute(2, 0, 3, 1, 4)
+            want_q, want_k = plain_operators.turn(q.float(), tab, how), plain_operators.turn(k.float(), tab, how)
+            assert torch.equal(turned.transpose(1, 2), want_q.bfloat16())
+            if last:
+                was[:, :, 1] = want_k.bfloat16().transpose(1, 2)
+            assert torch.equal(x, was)
+            kept.append((want_k.bfloat16().double(), v.double()) if last else (plain.held(want_k), plain.held(v)))
+            kk, vv = (torch.cat([y[j] for y in kept], dim=2) for j in range(2))
+            _check(o.transpose(1, 2), turned.transpose(1, 2), kk, vv, "scale %d" % s)
 
 
 def test_same_bits_again():

@@ -249,6 +249,35 @@ def test_far_rows():
         assert bool(((out[b].double() - want).abs() <= bound).all())
 
 
+def test_far_rows_of_one_head():
+    """One unit whose codes pass 2^31 bytes: a batch element of nearly all rows, whose last 150 weigh some e^180 times the others, and one of 150."""
+    D, T, n = 128, 34000000, 300
+    q = torch.round(_normal(2, 1, 3, D, seed=3)).clamp(-1, 1).bfloat16()
+    q[..., :64] = 1
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    k, v = (torch.empty(T, D, dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(2))
+    k[:T - n, :64] = -32.0
+    k[:T - n, 64:] = 0
+    k[T - n:] *= 0.125
+    out = torch.empty_like(q)
+    qs, st = amskv.Strides(3 * D, 3 * D, D), amskv.Strides(0, D, D)
+    x = amskv.Cross(batch=2, heads=1, kv_heads=1, head_dim=D, dtype=KV4, q_tokens=3, kv_tokens=T, kv_rows=T, q=qs, k=st, v=st, o=qs)
+    held = [torch.empty(amskv.amskv_cross_held_bytes(x, packed=True), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    assert T * D // 2 > 2 ** 31
+    offsets = torch.tensor([0, T - n // 2, T], dtype=torch.int32, device="cuda")
+    ws = torch.empty(amskv.amskv_cross_workspace_bytes(x), dtype=torch.uint8, device="cuda")
+    amskv.amskv_cross_hold(x, k, v, *held, offsets=offsets)
+    amskv.amskv_cross_attend(x, q, *held, out, offsets=offsets, workspace=ws)
+    for b, rows in ((0, slice(T - n, T - n // 2)), (1, slice(T - n // 2, T))):
+        want, bound = plain.attention(q[b], *(plain.held(y[rows])[None] for y in (k, v)), 1 / math.sqrt(D))
+        assert bool(((out[b].double() - want).abs() <= bound).all())
+    v.fill_(9.0)
+    amskv.amskv_cross_export(x, held[0], None, v, None, offsets=offsets)
+    for i in range(0, T, 1 << 20):
+        assert torch.equal(v[i:i + (1 << 20)].double(), plain.held(k[i:i + (1 << 20)]))
+
+
 def test_captured_and_replayed():
     """Lengths are read when the graph runs, not when it is captured; new states are held, attended and read back in it; eager calls in
     between use buffers of their own."""
