@@ -210,8 +210,8 @@ typedef struct {
  * is at most 2/7 of m; elements of at most 2^-102 become 0.  4.25 bits an element.
  * A token's values depend on nothing but the token: slots may start at any token and capacities are any number of them.
  * The attention's products take K as held and Q either as it is or, in launches of many rows, scaled by softmax_scale * log2(e) and
- * off by at most 1/480 of the largest magnitude of a row's AMSKV_KV4_GROUP channels (bf16 itself: 1/256 of each value).  The sum of
- * |q| |k| over the channels, times softmax_scale, has to be below 2^124.
+ * off by at most 1/480 of the largest magnitude of a row's AMSKV_KV4_GROUP channels (from 2^-108 on; bf16 itself: 1/256 of each value).  The sum of
+ * |q| |k| over the channels, times softmax_scale, has to be below 2^124, and so has |q| * softmax_scale.
  * amskv_cache_bytes_held counts half a byte per element and one per group.  The modes, layouts and limits of the 8-bit
  * cache, the similarity and density calls among them. */
 
@@ -536,8 +536,8 @@ int32_t amskv_cross_hold(const amskv_cross* cross, const void* K_dev, const void
 int32_t amskv_cross_export(const amskv_cross* cross, const void* K_held_dev, const void* V_held_dev, void* K_out_dev, void* V_out_dev,
                            const int32_t* lengths_dev, const int32_t* offsets_dev, void* stream);
 
-/* amskv_cross_attend over held states: K_dev and V_dev are the held tensors, cross->k and cross->v are not read, lengths_dev and
- * offsets_dev as they were held with; Q's rounding and the scores' range are the 4-bit cache's; all else is as above. */
+/* amskv_cross_attend over held states: K_dev and V_dev are the held tensors, cross->k and cross->v are not read, lengths_dev,
+ * offsets_dev, batch, kv_heads, head_dim and kv_tokens (packed: kv_rows) as they were held with; Q's rounding and the scores' range are the 4-bit cache's; all else is as above. */
 
 /* Static text for a status code. */
 const char* amskv_status_string(int32_t status);

@@ -283,7 +283,7 @@ hipError_t launch_theta_flag(const float* totals_dev, int heads, double n_tok, f
 hipError_t launch_density_total(const float* partial_ws, int batch, int heads, int n_qblk, int n_groups, float* out_dev,
                                 hipStream_t st);
 
-// ---- rotary positions and the 8-bit cache.  A build of the host layer by itself, without the device compiler (a test of it on the
+// ---- rotary positions, the caches of 8 and 4 bits, cross attention.  A build of the host layer by itself, without the device compiler (a test of it on the
 // CPU), need not have them: a cache without either never calls them.  In the library they are as all others.
 #if defined(__HIPCC__)
 #define AMSKV_OPTIONAL

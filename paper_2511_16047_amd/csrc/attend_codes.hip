@@ -16,9 +16,9 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void att
     float scale_log2e, int n_bh, int n_qtiles, int n_whole) {
   fetch_arguments<6 * 8 + 16 + sizeof(SegTable) + sizeof(ExtKV) + sizeof(CallerIo)>();
   using U = rows::Unit<D, kTeamWaves, kTeams, kBits>;
-  constexpr bool kParts = kBits == 4 && kTeamWaves > 1 && !(kMixed && D == 64);  // K goes to the matrix cores in 4 bits
+  constexpr bool kFour = kBits == 4 && kTeamWaves > 1 && !(kMixed && D == 64);  // K goes to the matrix cores in 4 bits
   using Team = rows::FourBitTeam<D, kTeamWaves == 1 ? 4 : kTeamWaves, kMixed>;
-  __shared__ __align__(1024) char lds[kParts ? Team::kLds : U::kLds];
+  __shared__ __align__(1024) char lds[kFour ? Team::kLds : U::kLds];
   Place at{(int)blockIdx.x, 0};
   if (n_qtiles > 1) at = place<true>(blockIdx.x, n_bh, n_qtiles, n_whole);
   const long long bh = at.bh;
@@ -42,7 +42,7 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void att
   }
   typename U::Result x;
   U::clear(x);
-  if constexpr (kParts) {
+  if constexpr (kFour) {
     typename Team::Query parts;
     rows::split_query(parts, q_row(lane), h, scale_log2e);
     Team::walk(x, parts, [&]() { return q_row(U::fresh(threadIdx.x)); }, lds, keys, seg, 0, Team::tiles(keys), scale_log2e, active);
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void att
   U::meet(x, lds);
   const int row = base + (U::fresh(threadIdx.x) & 31);  // (not kept over the walk)
   int heads = io.heads;
-  if constexpr (kParts) asm volatile("" : "+s"(heads));  // (nor what divides by them)
+  if constexpr (kFour) asm volatile("" : "+s"(heads));  // (nor what divides by them)
   U::put(x, reinterpret_cast<__bf16*>(o + unit_offset(io.o, bh, heads) + min(row, t_q - 1) * io.o.tok), active && row < t_q);
 }
 

@@ -3,13 +3,19 @@
 //
 // The matrix cores take e2m1 numbers with a power of two to every 32 along the sum: S^T = K Q^T is formed by
 // v_mfma_scale_f32_32x32x64_f8f6f4 from K's codes and powers straight out of LDS, a quarter of bf16's bytes there and no
-// conversion.  Its other operand may have 6 bits without loss of speed (4 times bf16's rate; 8 bits: twice), so Q is held as the
-// sum of two e2m3 numbers (4 significant bits each), made once for a workgroup: 32 channels with largest element m, 2^a the least power
-// with m <= 7.5 * 2^a, are hi * 2^a + lo * 2^(a - 4), hi the number nearest to q * 2^-a, lo nearest to what is left.  What is left of a
-// bf16 number of at least 2^a is a multiple of half of hi's step times 2^-3, which lo holds exactly; smaller elements are off by at most
-// 2^(a - 8), 2^-9.9 of m.  Two products at 4 times the rate: half of the time of bf16's.  (e4m3 parts would be exact over a wider range
-// and take bf16's time.)  V becomes bf16 on its way to LDS, once for all waves: weights in 6 bits would have to be split in two for
+// conversion.  Its other operand may have 6 bits without loss of speed (4 times bf16's rate; 8 bits: twice), so y = q times the factor of
+// the scores is held as the sum of two e2m3 numbers (4 significant bits each), made once for a workgroup: 32 channels with largest
+// element m, 2^a the least power with m <= 7.5 * 2^a, are hi * 2^a + lo * 2^(a - 4), hi the number nearest to y * 2^-a, lo nearest to
+// what is left.  hi's step is 1/2 from 4 on, 1/4 from 2 on and 1/8 below, so lo's number is at most 4 and its own step 1/4 at most, 1/8
+// where hi's is 1/4 or less: y is off by at most 2^(a - 7) from 4 * 2^a on and 2^(a - 8) below (a bf16 number itself stands for
+// what lies within 2^(a - 6) there).  Over normal Q and K a weight moves by 0.0011 of itself (rms), its rounding to bf16 by 0.0016.  Two products at 4 times the rate: half of the time of bf16's (15.4 ns of a SIMD for 64 channels, bf16 36.8; with
+// e4m3 parts 28.6).  V becomes bf16 on its way to LDS, once for all waves: weights in 6 bits would have to be split in two for
 // every block, which takes the vector ALUs more (a conversion of 32 numbers 38 ns, back 33) than the matrix cores save.
+//
+// Bound, and what it measured.  Head dim 128, 64 units: the matrix pipes and the power they take, 4096 x 6421 by teams of eight 576 to 601 us
+// (1.43 to 1.50 PFLOP/s; codes of 8 bits through bf16 784), 2304 x 3925 by teams of four 234 to 255, 576 x 1076 29.  Head dim 64, 3840 units: the vector ALUs
+// (0.66 of a SIMD's cycles, the matrix pipe 0.20), 256 x 530 174 to 181 us (with 256 of the keys read in place as bf16, by attend_rows.hpp, 195 to
+// 201), x 2066 481 to 503 (1.03 to 1.08 PFLOP/s).
 //
 // kExt: rows of bf16 may follow the codes (a scale that is read in place); they are walked as in attend_rows.hpp, with Q as it is.
 #pragma once
@@ -23,9 +29,10 @@ typedef unsigned u32x6 __attribute__((ext_vector_type(6)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// Q of a lane times the factor of its scores: channels 64 c + 32 h .. + 31 of its row in kParts parts, largest first, and the bytes of
+// Q of a lane times the factor of its scores: channels 64 c + 32 h .. + 31 of its row in two parts, the larger first, and the bytes of
 // their powers.
-template <int D, int kParts>
+constexpr int kParts = 2;
+template <int D>
 struct QueryParts {
   u32x6 part[D / 64][kParts];
   unsigned powers[D / 64];
@@ -43,8 +50,8 @@ __device__ __forceinline__ f32x32 values_of(const u32x6& x, float by) {
   asm("v_cvt_scalef32_pk32_f32_fp6 %0, %1, %2\n\ts_nop 7" : "=&v"(r) : "v"(x), "v"(by));
   return r;
 }
-template <int D, int kParts>
-__device__ __forceinline__ void split_query(QueryParts<D, kParts>& q, const char* row, int h, float factor) {
+template <int D>
+__device__ __forceinline__ void split_query(QueryParts<D>& q, const char* row, int h, float factor) {
   u32x4 raw[D / 64][4];
 #pragma unroll
   for (int c = 0; c < D / 64; ++c)
@@ -93,11 +100,10 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
   static constexpr int kOfK = kExt ? Base::kTensor : kPowers + 32 * kTile;
   static constexpr int kStage = kOfK + Base::kTensor;
   static constexpr int kLds = 4 * kStage;
-  static constexpr int kParts = 2;
   // The products start from the references: S^T - ref comes out of the matrix cores, 16 multiply-adds of a block's 90 vector
   // instructions fewer, for 16 registers that hold -ref.
   static constexpr bool kFolds = D == 64 || kTeamWaves == 8;
-  typedef QueryParts<D, kParts> Query;
+  typedef QueryParts<D> Query;
   static_assert(kPowers + 32 * kTile <= kOfK && kThreads == 8 * kTile, "eight threads bring a row of K and of V");
 
   __device__ static __forceinline__ int tiles(const Keys& k) { return kExt ? Base::tiles(k) : Base::tiles_of_codes(k); }
@@ -199,11 +205,9 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
   __device__ static __forceinline__ f32x16 product(const KeyCodes& kc, const Query& q, const f32x16& less_ref) {
     f32x16 s = multiply<0, 0>(kc, q, less_ref);
     s = multiply<1, 0>(kc, q, s);
-    if constexpr (kParts == 3) s = multiply<2, 0>(kc, q, s);
     if constexpr (D == 128) {
       s = multiply<0, 1>(kc, q, s);
       s = multiply<1, 1>(kc, q, s);
-      if constexpr (kParts == 3) s = multiply<2, 1>(kc, q, s);
     }
     return s;
   }

@@ -1,5 +1,5 @@
 // Attention of up to 32 * kTeamWaves query rows over the keys of one (b,h) or (b, kv head), for kernels whose keys are not
-// plain rows of a bf16 cache: codes in 8 bits (attend_codes.hip), rows whose number only the device knows (cross.hip).
+// plain rows of a bf16 cache: codes in 8 or 4 bits (attend_codes.hip), rows whose number only the device knows (cross.hip).
 //
 // Formulation as in attend_bf16.hip: a wave owns 32 query rows and forms S^T = K Q^T and O^T += V^T P^T with
 // v_mfma_f32_32x32x16_bf16, 32 keys at a time; a lane holds 16 keys of one query, so softmax sums are in-lane, and the

@@ -44,9 +44,9 @@ template <int D, int kTeamWaves, int kTeams, int kMinWavesPerSimd, int kBits>
 __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cross_kernel(CrossArgs a) {
   fetch_arguments<sizeof(CrossArgs)>();
   using U = rows::Unit<D, kTeamWaves, kTeams, kBits>;
-  constexpr bool kParts = kBits == 4 && kTeamWaves > 1;  // K goes to the matrix cores in 4 bits
+  constexpr bool kFour = kBits == 4 && kTeamWaves > 1;  // K goes to the matrix cores in 4 bits
   using Team = rows::FourBitTeam<D, kTeamWaves == 1 ? 4 : kTeamWaves, false>;
-  __shared__ __align__(1024) char lds[kParts ? Team::kLds : U::kLds];
+  __shared__ __align__(1024) char lds[kFour ? Team::kLds : U::kLds];
   const int tiles = a.row_tiles * a.splits;
   Place at{(int)blockIdx.x, 0};
   if (tiles > 1) at = place<true>(blockIdx.x, a.n_units, tiles, a.n_whole);
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   U::clear(x);
   SegTable none;
   none.n = 0;
-  if constexpr (kParts) {
+  if constexpr (kFour) {
     typename Team::Query parts;
     rows::split_query(parts, q_row, h, a.scale_log2e);
     Team::walk(x, parts, [&]() { return q_row; }, lds, keys, none, from, to, a.scale_log2e, active);
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   const int late = U::fresh(threadIdx.x) & 63;
   if (a.splits == 1) {
     int q_tokens = a.q_tokens;
-    if constexpr (kParts) asm volatile("" : "+s"(q_tokens));
+    if constexpr (kFour) asm volatile("" : "+s"(q_tokens));
     U::put(x, reinterpret_cast<__bf16*>(a.o + row_at(a.o_map, late, q_tokens)), active && base + (late & 31) < n_rows);
     return;
   }

@@ -1,4 +1,4 @@
-// How the launches of take_kernels.hip that move an 8-bit cache's codes are divided: plain host code.  A launch has fewer than 2^32
+// How the launches of take_kernels.hip that move the codes of a cache of 8 or 4 bits are divided: plain host code.  A launch has fewer than 2^32
 // threads along an axis.
 #pragma once
 

@@ -368,3 +368,17 @@ def test_steps_of_a_model():
             assert torch.equal(got.double(), torch.cat([kept[l][i][j] for i in sorted(kept[l])], dim=2))
     torch.cuda.synchronize()
     amskv.amskv_cache_destroy(h)
+
+
+def test_without_the_extension_module(monkeypatch):
+    """Both directions through ctypes: the same values."""
+    from paper_2511_16047_amd import binding
+    c = Case(6, 3, 64, 5, 40, [40, 0, 33])
+    want = c.export()
+    for name in ("_hold", "_export", "_cross"):
+        monkeypatch.setattr(binding, name, binding._not_built)
+    for x in c.held:
+        x.fill_(0xFF)
+    c.hold()
+    assert all(torch.equal(a, b) for a, b in zip(want, c.export()))
+    c.check(c.run())
