@@ -5,10 +5,12 @@
 // v_mfma_scale_f32_32x32x64_f8f6f4 from K's codes and powers straight out of LDS, a quarter of bf16's bytes there and no
 // conversion.  Its other operand may have 6 bits without loss of speed (4 times bf16's rate; 8 bits: twice), so y = q times the factor of
 // the scores is held as the sum of two e2m3 numbers (4 significant bits each), made once for a workgroup: 32 channels with largest
-// element m, 2^a the least power with m <= 7.5 * 2^a, are hi * 2^a + lo * 2^(a - 4), hi the number nearest to y * 2^-a, lo nearest to
-// what is left.  hi's step is 1/2 from 4 on, 1/4 from 2 on and 1/8 below, so lo's number is at most 4 and its own step 1/4 at most, 1/8
-// where hi's is 1/4 or less: y is off by at most 2^(a - 7) from 4 * 2^a on and 2^(a - 8) below (a bf16 number itself stands for
-// what lies within 2^(a - 6) there).  Over normal Q and K a weight moves by 0.0011 of itself (rms), its rounding to bf16 by 0.0016.  Two products at 4 times the rate: half of the time of bf16's (15.4 ns of a SIMD for 64 channels, bf16 36.8; with
+// element m, 2^a the least power with m <= 7.5 * 2^a, are hi * 2^a + lo * 2^(a - 5), hi the number nearest to y * 2^-a, lo nearest to
+// what is left.  hi's step is 1/2 from 4 on, 1/4 from 2 on and 1/8 below, which leaves up to 8, 4 and 2 for lo: y is off by at most 2^(a - 8)
+// from 2 * 2^a on and 2^(a - 9) below; from 4 * 2^a on by 2^(a - 7), and up to 2^(a - 6) where lo would be 7.75 to 8 and is 7.5 (one of 32;
+// a bf16 number itself stands for what lies within 2^(a - 6) there).  lo at 2^(a - 4) has no such end, but steps twice as wide for all others: over
+// normal values y is off by 0.0008 of its size (rms) as it is here, 0.0011 as it would be there, with gains from channel to channel of e^(0.5 normal)
+// 0.0009 and 0.0015.  Two products at 4 times the rate: half of the time of bf16's (15.4 ns of a SIMD for 64 channels, bf16 36.8; with
 // e4m3 parts 28.6).  V becomes bf16 on its way to LDS, once for all waves: weights in 6 bits would have to be split in two for
 // every block, which takes the vector ALUs more (a conversion of 32 numbers 38 ns, back 33) than the matrix cores save.
 //
@@ -72,7 +74,7 @@ __device__ __forceinline__ void split_query(QueryParts<D>& q, const char* row, i
     q.powers[c] = 0;
 #pragma unroll
     for (int p = 0; p < kParts; ++p) {
-      const int byte = a - 4 * p + 127;
+      const int byte = a - 5 * p + 127;
       const float by = power_of_byte(byte);
       q.powers[c] |= (unsigned)byte << (8 * p);
       q.part[c][p] = parts_of(even, odd, by);

@@ -42,8 +42,10 @@ def held(x):
 def attention(q, k, v, scale):
     """As plain.attention, over held k and v, with the products' rounding of Q: y = q * scale * log2(e), whose group's largest is m, 2^a the
     least power with m <= 7.5 * 2^a, is held as the number of 4 significant bits next to y * 2^-a, times 2^a, and the number of 4 significant
-    bits (steps of 1/8 at least) next to 2^4 times what is left: off by at most 2^(a - 7) where |y| is about 4 * 2^a and more, else 2^(a - 8).
-    (A y on the grid that the two have there is off by its roundings in fp32 alone, 2^-20 of it at most.)  That moves a score, as a power of
+    bits (steps of 1/8 at least, up to 7.5) next to 2^5 times what is left, r.  r is at most 1/4, 1/8 or 1/16 where |y| * 2^-a is 4, 2 or less than
+    2, the second number then at most 8, 4 or 2 with steps of 1/2, 1/4 or 1/8: half of them are 2^(a - 7), 2^(a - 8), 2^(a - 9), but beyond
+    7.75, for which 7.5 stands, up to 2^(a - 6).  (A y on the grid that the two have there is off by its roundings in fp32 alone, 2^-20 of it at
+    most.)  That moves a score, as a power of
     two, by at most the sum of these times |k|, and a weight, relative to the others', by a factor of 2 to twice that.
 
     Weights of 2^-120 of the largest and less may vanish: a reference that is up to 2^6 below the largest weight of its time is left for
@@ -53,9 +55,11 @@ def attention(q, k, v, scale):
     y = (q * (scale * math.log2(math.e))).unflatten(-1, (-1, GROUP))
     one = _two_to(_least_exponent(y.abs().amax(dim=-1, keepdim=True), 7.5, -110, 130))
     size = y.abs() / one
-    grid = one * torch.where(size >= 3.99, 2.0 ** -5, torch.where(size >= 1.99, 2.0 ** -6, 2.0 ** -7))
-    on_it = (y - torch.round(y / grid) * grid).abs() <= 2.0 ** -20 * y.abs()
-    off = torch.where(on_it, 2.0 ** -20 * y.abs(), one * torch.where(size >= 3.9, 2.0 ** -7, 2.0 ** -8)).flatten(-2)
+    grid = one * torch.where(size >= 3.99, 2.0 ** -6, torch.where(size >= 1.99, 2.0 ** -7, 2.0 ** -8))
+    ends = (size >= 3.9) & ((size - torch.round(size * 2) / 2).abs() > 7.7 / 32)
+    on_it = ((y - torch.round(y / grid) * grid).abs() <= 2.0 ** -20 * y.abs()) & ~ends
+    step = torch.where(ends, 2.0 ** -6, torch.where(size >= 3.9, 2.0 ** -7, torch.where(size >= 1.9, 2.0 ** -8, 2.0 ** -9)))
+    off = torch.where(on_it, 2.0 ** -20 * y.abs(), one * step).flatten(-2)
     far = (off @ k.abs().transpose(-1, -2)).amax(dim=-1, keepdim=True) * math.log(2)
     s = q @ k.transpose(-1, -2) * scale
     p, rel = torch.softmax(s, dim=-1), torch.exp(s - s.amax(dim=-1, keepdim=True))
