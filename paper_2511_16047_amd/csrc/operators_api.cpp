@@ -76,7 +76,7 @@ int check_held(const amskv_cross* x, const int32_t* lengths_dev, const int32_t* 
   if (x->dtype != AMSKV_DTYPE_BF16_KV4) return AMSKV_ERR_INVALID_ARG;
   if ((lengths_dev && offsets_dev) || ((uintptr_t)lengths_dev & 3) != 0 || ((uintptr_t)offsets_dev & 3) != 0) return AMSKV_ERR_INVALID_ARG;
   if (offsets_dev && (x->kv_rows < 0 || x->kv_rows > INT32_MAX)) return AMSKV_ERR_INVALID_ARG;
-  if ((int64_t)x->batch * x->kv_heads > (1 << 24)) return AMSKV_ERR_INVALID_ARG;  // (heads may be 0)
+  if (x->kv_heads > (1 << 24) || (int64_t)x->batch * x->kv_heads > (1 << 24)) return AMSKV_ERR_INVALID_ARG;  // (heads or batch may be 0)
   return AMSKV_OK;
 }
 
