@@ -13,6 +13,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kRows = 4;               // rows of a lane under way
+constexpr int kSideBySide = 512;       // bytes of a row that a workgroup has of several heads
 constexpr unsigned kMostGroups = 1 << 20;  // workgroups; beyond that they take several blocks of rows
 
 struct HoldArgs {
@@ -21,8 +22,9 @@ struct HoldArgs {
   RowMap map[2];
   const int *lengths, *offsets;
   long long rows, groups_at;  // rows of a unit, bytes of codes
-  unsigned blocks, all_blocks;  // blocks of rows to a unit, of all units
+  unsigned blocks, all_blocks;  // blocks of rows to a unit, of all groups of heads
   int kv_heads, batch, kv_tokens;
+  int side;  // 2^side heads side by side in a workgroup, a divisor of kv_heads
 };
 
 // rows [first, end) of a unit that hold states
@@ -46,22 +48,24 @@ __device__ __forceinline__ float quad_max(float m) {
 template <int D, bool kBack>
 __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a) {
   fetch_arguments<sizeof(HoldArgs)>();
-  constexpr int kLanes = D / 8, kAtOnce = 256 / kLanes;  // lanes of a row, rows of a workgroup at a time
+  constexpr int kLanes = D / 8;               // of a row
+  const int at_once = 256 / kLanes >> a.side;  // rows of a workgroup at a time
   const int tensor = blockIdx.y;
   if (a.x[tensor] == nullptr) return;
-  const int c = threadIdx.x % kLanes, r = threadIdx.x / kLanes;
+  const int c = threadIdx.x % kLanes, of_all = threadIdx.x / kLanes, r = of_all >> a.side;
+  const unsigned head = of_all & ((1 << a.side) - 1), groups_of_heads = (unsigned)a.kv_heads >> a.side;
   const RowMap& m = a.map[tensor];
   for (unsigned block = blockIdx.x; block < a.all_blocks; block += gridDim.x) {
     // the heads of a block of rows, which lie side by side in a token-major tensor, go to workgroups of one time
-    const unsigned rest = block / (unsigned)a.kv_heads, g = block - rest * a.kv_heads, b = rest / a.blocks;
-    const long long row0 = (long long)(rest - b * a.blocks) * (kAtOnce * kRows) + r, unit = (long long)b * a.kv_heads + g;
+    const unsigned rest = block / groups_of_heads, g = ((block - rest * groups_of_heads) << a.side) + head, b = rest / a.blocks;
+    const long long row0 = (long long)(rest - b * a.blocks) * (at_once * kRows) + r, unit = (long long)b * a.kv_heads + g;
     long long first, end;
     live_rows(a, b, first, end);
     char* x = a.x[tensor] + b * m.batch + g * m.head + 16 * c;
     unsigned char* codes = a.held[tensor] + unit * a.rows * (D / 2) + 4 * c;
     unsigned char* groups = a.held[tensor] + a.groups_at + unit * a.rows * (D / AMSKV_KV4_GROUP) + c / 4;
     auto live = [&](int i) {
-      const long long row = row0 + i * kAtOnce;
+      const long long row = row0 + i * at_once;
       return row >= first && row < end;
     };
     if constexpr (kBack) {
@@ -69,19 +73,19 @@ __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a) {
 #pragma unroll
       for (int i = 0; i < kRows; ++i)
         if (live(i)) {
-          const long long row = row0 + i * kAtOnce;
+          const long long row = row0 + i * at_once;
           in[i] = *reinterpret_cast<const unsigned*>(codes + row * (D / 2));
           byte[i] = groups[row * (D / AMSKV_KV4_GROUP)];
         }
 #pragma unroll
       for (int i = 0; i < kRows; ++i)
-        if (live(i)) *reinterpret_cast<u32x4*>(x + (row0 + i * kAtOnce) * m.tok) = values4(in[i], power_of_byte(byte[i]));
+        if (live(i)) __builtin_nontemporal_store(values4(in[i], power_of_byte(byte[i])), reinterpret_cast<u32x4*>(x + (row0 + i * at_once) * m.tok));
     } else {
       bf16x8 in[kRows];
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
         in[i] = {};
-        if (live(i)) in[i] = *reinterpret_cast<const bf16x8*>(x + (row0 + i * kAtOnce) * m.tok);
+        if (live(i)) in[i] = *reinterpret_cast<const bf16x8*>(x + (row0 + i * at_once) * m.tok);
       }
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
@@ -93,7 +97,7 @@ __global__ __launch_bounds__(256) void hold_kernel(HoldArgs a) {
         }
         const unsigned byte = group_exponent(quad_max(largest)) + 127;
         if (live(i)) {
-          const long long row = row0 + i * kAtOnce;
+          const long long row = row0 + i * at_once;
           *reinterpret_cast<unsigned*>(codes + row * (D / 2)) = codes4(y, power_of_byte(byte));
           if (c % 4 == 0) groups[row * (D / AMSKV_KV4_GROUP)] = (unsigned char)byte;
         }
@@ -119,10 +123,12 @@ hipError_t go(const HoldCall& c, hipStream_t st) {
   a.kv_heads = c.kv_heads;
   a.batch = c.batch;
   a.kv_tokens = c.kv_tokens;
-  const int per = 256 / (c.head_dim / 8) * kRows;
-  a.blocks = (unsigned)((a.rows + per - 1) / per);
-  if (units * a.blocks > 0x7fffffffll) return hipErrorInvalidValue;  // (the loop's counter)
-  a.all_blocks = (unsigned)(units * a.blocks);
+  while ((c.head_dim * 2 << a.side) < kSideBySide && c.kv_heads % (2 << a.side) == 0) ++a.side;
+  const int per = (256 / (c.head_dim / 8) >> a.side) * kRows;
+  const long long blocks = (a.rows + per - 1) / per, all = (units >> a.side) * blocks;
+  if (all > 0x7fffffffll) return hipErrorInvalidValue;  // (the loop's counter)
+  a.blocks = (unsigned)blocks;
+  a.all_blocks = (unsigned)all;
   if (a.all_blocks == 0) return hipSuccess;
   const dim3 grid(a.all_blocks < kMostGroups ? a.all_blocks : kMostGroups, 2);
   auto kernel = c.head_dim == 64 ? hold_kernel<64, kBack> : hold_kernel<128, kBack>;

@@ -461,6 +461,24 @@ __global__ __launch_bounds__(256) void export_codes_kernel(CodesOf<kBits> c, __b
   const unsigned unit = blockIdx.x / (unsigned)parts, part = blockIdx.x - unit * parts;
   const long long bh = (long long)blockIdx.z * units + unit;
   if (bh >= n_bh) return;
+  if constexpr (kBits == 4) {  // 8 channels twice, so that a wave writes 1024 bytes in a row, past the caches
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const long long i = ((long long)part * 2 + n) * 256 + threadIdx.x;
+      const int j = (int)(i / (2 * kPer)), piece = (int)(i % (2 * kPer));
+      if (j >= seg.total) return;
+      bool ext;
+      const long long at = locate_row(seg, j, ext), row = bh * cap_tokens + at;
+      u32x4 w;
+      if (ext)
+        w = *reinterpret_cast<const u32x4*>((const char*)(blockIdx.y ? ext_kv.v : ext_kv.k) + unit_offset(ext_map, bh, heads) + at * ext_map.tok + piece * 16);
+      else
+        w = values4(*reinterpret_cast<const unsigned*>((blockIdx.y ? c.v : c.k) + row * (D / 2) + piece * 4),
+                    power_of_byte((blockIdx.y ? c.v_group : c.k_group)[row * (D / AMSKV_KV4_GROUP) + piece / 4]));
+      __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(out + (bh * seg.total + j) * D + piece * 8));
+    }
+    return;
+  }
   const long long i = (long long)part * 256 + threadIdx.x;
   const int j = (int)(i / kPer), piece = (int)(i % kPer);
   if (j >= seg.total) return;
@@ -471,13 +489,7 @@ __global__ __launch_bounds__(256) void export_codes_kernel(CodesOf<kBits> c, __b
     const char* row = (const char*)(blockIdx.y ? ext_kv.v : ext_kv.k) + unit_offset(ext_map, bh, heads) + at * ext_map.tok + piece * 32;
     w[0] = *reinterpret_cast<const u32x4*>(row);
     w[1] = *reinterpret_cast<const u32x4*>(row + 16);
-  } else if constexpr (kBits == 4) {
-    const long long row = bh * cap_tokens + at;
-    const u32x2 x = *reinterpret_cast<const u32x2*>((blockIdx.y ? c.v : c.k) + row * (D / 2) + piece * 8);
-    const float scale = power_of_byte((blockIdx.y ? c.v_group : c.k_group)[row * (D / AMSKV_KV4_GROUP) + piece / 2]);
-    w[0] = values4(x[0], scale);
-    w[1] = values4(x[1], scale);
-  } else {
+  } else if constexpr (kBits == 8) {
     const unsigned char* codes = (blockIdx.y ? c.v : c.k) + (bh * cap_tokens + at) * D + piece * 16;
     const u32x4 x = *reinterpret_cast<const u32x4*>(codes);
     const float scale = (blockIdx.y ? c.v_scale : c.k_scale)[(bh * cap_tokens + at) / AMSKV_KV8_BLOCK];
