@@ -28,6 +28,16 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void att
   const bool active = base < t_q;
 
   auto q_row = [&](int of_lane) { return q + unit_offset(io.q, bh, io.heads) + min(base + (of_lane & 31), t_q - 1) * io.q.tok; };
+  rows::bf16x8 qf[U::KS];
+  u32x4 raw[D / 64][4];
+  if constexpr (kFour) {
+    rows::load_query<D>(raw, q_row(lane), h);
+  } else {
+    const char* row = q_row(lane);
+#pragma unroll
+    for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(row + U::q_at(t, h));
+  }
+
   const long long x_unit = unit_offset(io.kv, bh, io.heads), blocks = cap_tokens / AMSKV_KV8_BLOCK;
   rows::Keys keys{nullptr, nullptr, nullptr, nullptr, (const char*)ext.k + x_unit, (const char*)ext.v + x_unit, io.kv.tok, io.kv.tok, seg.ext_start,
                   seg.total - seg.ext_start, nullptr, nullptr};
@@ -44,13 +54,9 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void att
   U::clear(x);
   if constexpr (kFour) {
     typename Team::Query parts;
-    rows::split_query(parts, q_row(lane), h, scale_log2e);
+    rows::split_query(parts, raw, scale_log2e);
     Team::walk(x, parts, [&]() { return q_row(U::fresh(threadIdx.x)); }, lds, keys, seg, 0, Team::tiles(keys), scale_log2e, active);
   } else {
-    rows::bf16x8 qf[U::KS];
-    const char* row = q_row(lane);
-#pragma unroll
-    for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(row + U::q_at(t, h));
     U::walk(x, qf, lds, keys, seg, 0, U::tiles(keys), scale_log2e, active);
   }
   U::meet(x, lds);

@@ -52,13 +52,16 @@ __device__ __forceinline__ f32x32 values_of(const u32x6& x, float by) {
   asm("v_cvt_scalef32_pk32_f32_fp6 %0, %1, %2\n\ts_nop 7" : "=&v"(r) : "v"(x), "v"(by));
   return r;
 }
+// (Q is asked for before anything that has to be waited for)
 template <int D>
-__device__ __forceinline__ void split_query(QueryParts<D>& q, const char* row, int h, float factor) {
-  u32x4 raw[D / 64][4];
+__device__ __forceinline__ void load_query(u32x4 (&raw)[D / 64][4], const char* row, int h) {
 #pragma unroll
   for (int c = 0; c < D / 64; ++c)
 #pragma unroll
     for (int i = 0; i < 4; ++i) raw[c][i] = *reinterpret_cast<const u32x4*>(row + 128 * c + 64 * h + 16 * i);
+}
+template <int D>
+__device__ __forceinline__ void split_query(QueryParts<D>& q, const u32x4 (&raw)[D / 64][4], float factor) {
 #pragma unroll
   for (int c = 0; c < D / 64; ++c) {
     f32x16 even, odd;

@@ -372,11 +372,6 @@ struct Unit {
     if constexpr (!kAhead) load_k(kf, lds_all, block + ka);
     f32x16 s = scores(kf, qf);
     between();
-    behind_scores<kFull>(x, w, s, lds_all, va, block, n_valid, c, lane);
-  }
-  template <bool kFull>
-  __device__ static __forceinline__ void behind_scores(Result& x, Behind& w, f32x16& s, const char* lds_all, int va, int block, int n_valid, float c,
-                                                       int lane) {
     if constexpr (!kFull) mask(s, n_valid, lane);
     if constexpr (kAlone) __builtin_amdgcn_s_setprio(1);
     float sum = 0.f;

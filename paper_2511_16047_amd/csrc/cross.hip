@@ -66,6 +66,16 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   };
 
   const char* q_row = a.q + row_at(a.q_map, lane, a.q_tokens);
+  // (asked for before the number of states is waited for)
+  rows::bf16x8 qf[U::KS];
+  u32x4 raw[D / 64][4];
+  if constexpr (kFour) {
+    rows::load_query<D>(raw, q_row, h);
+  } else {
+#pragma unroll
+    for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + U::q_at(t, h));
+  }
+
   rows::Keys keys{};
   if constexpr (kBits == 16) {
     const long long kb = a.offsets ? first * a.k_map.tok : b * a.k_map.batch, vb = a.offsets ? first * a.v_map.tok : b * a.v_map.batch;
@@ -90,12 +100,9 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   none.n = 0;
   if constexpr (kFour) {
     typename Team::Query parts;
-    rows::split_query(parts, q_row, h, a.scale_log2e);
+    rows::split_query(parts, raw, a.scale_log2e);
     Team::walk(x, parts, [&]() { return q_row; }, lds, keys, none, from, to, a.scale_log2e, active);
   } else {
-    rows::bf16x8 qf[U::KS];
-#pragma unroll
-    for (int t = 0; t < U::KS; ++t) qf[t] = *reinterpret_cast<const rows::bf16x8*>(q_row + U::q_at(t, h));
     U::walk(x, qf, lds, keys, none, from, to, a.scale_log2e, active);
   }
   U::meet(x, lds);

@@ -2,9 +2,11 @@
 //
 // A lane has 8 channels of a row: 16 bytes of bf16, 4 bytes of codes, and a group's 4 lanes are a quad, so its largest element takes two
 // steps on the vector ALU.  A wave's lanes follow the rows of one unit, whose codes lie back to back; a lane has kRows of them under way.
-// Bound: HBM and, at the smallest, a launch.  K and V of 96 packed prompts of up to 512 states, 16 heads, head dim 128: written 63 to 71 us (3.6 to 4.0 TB/s
-// read + write), read back 43 (5.8); 8 documents of up to 16000, 8 heads 135 to 140 (4.3) and 92 (6.5); 77 states of a short prompt 2.7 to 3.5 and
-// 2.5.  The heads of a block of rows go to neighbouring workgroups, not a unit's rows: 124 -> 117 us for both calls of the first.
+// Bound: HBM and, at the smallest, a launch.  K and V of 96 packed prompts of up to 512 states, 16 heads, head dim 128: written 45 to 56 us (4.5 to
+// 5.7 TB/s read + write), read back 41 (6.2); 8 documents of up to 16000, 8 heads, 101 to 113 (5.3 to 5.9) and 92 (6.5); 77 states of a short prompt
+// 2.9 and 2.6.  A workgroup has 512 bytes of a row, of heads side by side in a token-major tensor, and the heads of a block of rows go to
+// neighbouring workgroups: with one head to a workgroup 63 to 71, 135 to 140 us.  What is read back goes past the caches: 8 x 16000 states of 8
+// heads 126 -> 93 us, 96 x 250 of 16, head dim 64, 19.2 -> 17.6.  (Loads past them: 42.7 us for 35.8 where a projection has just made the states.)
 #include "codes.hpp"
 
 namespace amskv {
