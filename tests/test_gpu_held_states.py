@@ -108,6 +108,15 @@ def test_written_and_read_back(layout, D, Hkv, lengths):
     Case(Hkv, Hkv, D, 1, max(lengths + [1]), lengths, layout).check_held()
 
 
+@pytest.mark.parametrize("layout", ["tokens", "heads", "packed"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hkv", [2, 4, 6, 8])
+@pytest.mark.parametrize("lengths", [[1], [5, 0, 31, 32, 33, 64, 65, 0], [128, 127, 129, 200]], ids=str)
+def test_heads_side_by_side(layout, D, Hkv, lengths):
+    """Rows of two and four heads to a workgroup."""
+    Case(Hkv, Hkv, D, 1, max(lengths), lengths, layout, seed=Hkv).check_held()
+
+
 def test_held_with_no_lengths():
     """All rows of a padded tensor; K alone, V alone."""
     c = Case(2, 2, 64, 1, 70, [70, 70], hold=False)
