@@ -11,7 +11,7 @@
 // a bf16 number itself stands for what lies within 2^(a - 6) there).  lo at 2^(a - 4) has no such end, but steps twice as wide for all others: over
 // normal values y is off by 0.0008 of its size (rms) as it is here, 0.0011 as it would be there, with gains from channel to channel of e^(0.5 normal)
 // 0.0009 and 0.0015.  Two products at 4 times the rate: half of the time of bf16's (15.4 ns of a SIMD each for 64 channels, bf16
-// 73.6; e4m3 parts 28.6 each).  V becomes bf16 on its way to LDS, once for all waves: weights in 6 bits would have to be split in two for
+// 73.6; e4m3 parts 28.6 each; a third part at head dim 128, 64 units 4096 x 6421, 584 -> 651 us).  V becomes bf16 on its way to LDS, once for all waves: weights in 6 bits would have to be split in two for
 // every block, which takes the vector ALUs more (a conversion of 32 numbers 38 ns, back 33) than the matrix cores save.
 //
 // Bound, and what it measured.  Head dim 128, 64 units: the matrix pipes and the power they take, 4096 x 6421 by teams of eight 576 to 601 us
