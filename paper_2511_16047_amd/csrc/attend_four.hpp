@@ -2,22 +2,23 @@
 // they are.
 //
 // The matrix cores take e2m1 numbers with a power of two to every 32 along the sum: S^T = K Q^T is formed by
-// v_mfma_scale_f32_32x32x64_f8f6f4 from K's codes and powers straight out of LDS, a quarter of bf16's bytes there and no
-// conversion.  Its other operand may have 6 bits without loss of speed (4 times bf16's rate; 8 bits: twice), so y = q times the factor of
-// the scores is held as the sum of two e2m3 numbers (4 significant bits each), made once for a workgroup: 32 channels with largest
-// element m, 2^a the least power with m <= 7.5 * 2^a, are hi * 2^a + lo * 2^(a - 5), hi the number nearest to y * 2^-a, lo nearest to
-// what is left.  hi's step is 1/2 from 4 on, 1/4 from 2 on and 1/8 below, which leaves up to 8, 4 and 2 for lo: y is off by at most 2^(a - 8)
-// from 2 * 2^a on and 2^(a - 9) below; from 4 * 2^a on by 2^(a - 7), and up to 2^(a - 6) where lo would be 7.75 to 8 and is 7.5 (one of 32;
-// a bf16 number itself stands for what lies within 2^(a - 6) there).  lo at 2^(a - 4) has no such end, but steps twice as wide for all others: over
-// normal values y is off by 0.0008 of its size (rms) as it is here, 0.0011 as it would be there, with gains from channel to channel of e^(0.5 normal)
-// 0.0009 and 0.0015.  Two products at 4 times the rate: half of the time of bf16's (15.4 ns of a SIMD each for 64 channels, bf16
-// 73.6; e4m3 parts 28.6 each; a third part at head dim 128, 64 units 4096 x 6421, 584 -> 651 us).  V becomes bf16 on its way to LDS, once for all waves: weights in 6 bits would have to be split in two for
-// every block, which takes the vector ALUs more (a conversion of 32 numbers 38 ns, back 33) than the matrix cores save.
+// v_mfma_scale_f32_32x32x64_f8f6f4 from K's codes and powers straight out of LDS, a quarter of bf16's bytes there and no conversion.  Its
+// other operand may have 6 bits without loss of speed (4 times bf16's rate; 8 bits: twice), so y = q times the factor of the scores is held
+// as the sum of two e2m3 numbers (4 significant bits each), made once for a workgroup: 32 channels with largest element m, 2^a the least
+// power with m <= 7.5 * 2^a, are hi * 2^a + lo * 2^(a - 5), hi the number nearest to y * 2^-a, lo nearest to what is left.  hi's step is
+// 1/2 from 4 on, 1/4 from 2 on and 1/8 below, which leaves up to 8, 4 and 2 for lo: y is off by at most 2^(a - 8) from 2 * 2^a on and 2^(a
+// - 9) below; from 4 * 2^a on by 2^(a - 7), and up to 2^(a - 6) where lo would be 7.75 to 8 and is 7.5 (one of 32; a bf16 number itself
+// stands for what lies within 2^(a - 6) there).  lo at 2^(a - 4) has no such end, but steps twice as wide for all others: over normal
+// values y is off by 0.0008 of its size (rms) as it is here, 0.0011 as it would be there, with gains from channel to channel of e^(0.5
+// normal) 0.0009 and 0.0015.  Two products at 4 times the rate: half of the time of bf16's (15.4 ns of a SIMD each for 64 channels, bf16
+// 73.6; e4m3 parts 28.6 each; a third part at head dim 128, 64 units 4096 x 6421, 584 -> 651 us).  V becomes bf16 on its way to LDS, once
+// for all waves: weights in 6 bits would have to be split in two for every block, which takes the vector ALUs more (a conversion of 32
+// numbers 38 ns, back 33) than the matrix cores save.
 //
-// Bound, and what it measured.  Head dim 128, 64 units: the matrix pipes and the power they take, 4096 x 6421 by teams of eight 576 to 601 us
-// (1.43 to 1.50 PFLOP/s; codes of 8 bits through bf16 784), 2304 x 3925 by teams of four 234 to 255, 576 x 1076 29.  Head dim 64, 3840 units: the vector ALUs
-// (0.66 of a SIMD's cycles, the matrix pipe 0.20), 256 x 530 174 to 181 us (with 256 of the keys read in place as bf16, by attend_rows.hpp, 195 to
-// 201), x 2066 481 to 503 (1.03 to 1.08 PFLOP/s).
+// Bound, and what it measured.  Head dim 128, 64 units: the matrix pipes and the power they take, 4096 x 6421 by teams of eight 576 to 601
+// us (1.43 to 1.50 PFLOP/s; codes of 8 bits through bf16 784), 2304 x 3925 by teams of four 234 to 255, 576 x 1076 29.  Head dim 64, 3840
+// units: the vector ALUs (0.66 of a SIMD's cycles, the matrix pipe 0.20), 256 x 530 174 to 181 us (with 256 of the keys read in place as
+// bf16, by attend_rows.hpp, 195 to 201), x 2066 481 to 503 (1.03 to 1.08 PFLOP/s).
 //
 // kExt: rows of bf16 may follow the codes (a scale that is read in place); they are walked as in attend_rows.hpp, with Q as it is.
 #pragma once
