@@ -100,15 +100,13 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
   typedef typename Base::Result Result;
   typedef typename Base::Staged Staged;
   typedef typename Base::Aim Aim;
+  typedef typename Base::Behind Behind;
   static constexpr int RB = Base::RB, KS = Base::KS, kTile = Base::kTile, kThreads = Base::kThreads;
   static constexpr int kRowK = D / 2;                   // bytes of a row of codes
   static constexpr int kPowers = kTile * kRowK;         // where the powers of a tile's K begin: 32 bytes to a row
   static constexpr int kOfK = kExt ? Base::kTensor : kPowers + 32 * kTile;
   static constexpr int kStage = kOfK + Base::kTensor;
   static constexpr int kLds = 4 * kStage;
-  // The products start from the references: S^T - ref comes out of the matrix cores, 16 multiply-adds of a block's 90 vector
-  // instructions fewer, for 16 registers that hold -ref.
-  static constexpr bool kFolds = D == 64 || kTeamWaves == 8;
   typedef QueryParts<D> Query;
   static_assert(kPowers + 32 * kTile <= kOfK && kThreads == 8 * kTile, "eight threads bring a row of K and of V");
 
@@ -198,7 +196,7 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
     for (int c = 0; c < D / 64; ++c) kc.code[c] = *reinterpret_cast<const u32x4*>(at + (ka ^ (32 * c)));
     kc.powers = *reinterpret_cast<const unsigned*>(lds_all + slot + 32 * 32 * block + kp) >> (8 * (lane >> 5));
   }
-  // scores times the factor, less the references of the exponentials
+  // scores times the factor
   template <int kPart, int kChunk>
   __device__ static __forceinline__ f32x16 multiply(const KeyCodes& kc, const Query& q, const f32x16& add) {
     const u32x4& k = kc.code[kChunk];
@@ -208,8 +206,11 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
                                                            i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0}, add, 4, 2,
                                                            2 * kChunk, kc.powers, kPart, q.powers[kChunk]);
   }
-  __device__ static __forceinline__ f32x16 product(const KeyCodes& kc, const Query& q, const f32x16& less_ref) {
-    f32x16 s = multiply<0, 0>(kc, q, less_ref);
+  __device__ static __forceinline__ f32x16 product(const KeyCodes& kc, const Query& q) {
+    f32x16 s;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = 0.f;
+    s = multiply<0, 0>(kc, q, s);
     s = multiply<1, 0>(kc, q, s);
     if constexpr (D == 128) {
       s = multiply<0, 1>(kc, q, s);
@@ -217,67 +218,29 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
     }
     return s;
   }
-  // weights of keys 16u .. 16u + 15 against a reference (kFolds: that s already is without); the lane's sum
-  __device__ static __forceinline__ float weights(const f32x16& s, u32x4& pf, float ref, int u) {
-    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-    float sum = 0.f;
-#pragma unroll
-    for (int v = 0; v < 8; v += 2) {
-      const float a = s[8 * u + v], b = s[8 * u + v + 1];
-      const bf16x2 pk = {(__bf16)__builtin_amdgcn_exp2f(kFolds ? a : a - ref), (__bf16)__builtin_amdgcn_exp2f(kFolds ? b : b - ref)};
-      sum = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, sum, false);
-      pf[v / 2] = __builtin_bit_cast(unsigned, pk);
-    }
-    return sum;
-  }
-  // Unit::Behind.  kFolds: less_ref is what the references are taken off by, -0 for a reference of 0 and +0 in a lane that has none yet
-  // (and Result::ref is kept there); else it is 0 and Result::ref the reference.
-  struct Behind {
-    u32x4 pf[2];
-    f32x16 less_ref;
-    int block;
-    float most;  // a larger sum moves the references: kTripSum; kFolds: -1 while a lane has none (uniform)
-  };
-  __device__ static __forceinline__ float reference(const Result& x, const Behind& w) {
-    if constexpr (!kFolds) return x.ref;
-    return __builtin_bit_cast(unsigned, w.less_ref[0]) == 0 ? kNoKeys : -w.less_ref[0];
-  }
-  // Unit::step in one basic block: the first block, which has none before it, takes weights of 0 for what lies in its slot.
+  // Unit::step in one basic block (as its kOneBlock): the first block, which has none before it, takes weights of 0 for what lies in its slot.
+  // The products start from 0: started from the references, a block would save 16 multiply-adds of some 106 vector instructions, but
+  // scores come out rounded at the size of a reference that may lie far from them.
   template <bool kFull, class Between>
-  __device__ static __forceinline__ void step_codes(Result& x, Behind& w, KeyCodes& kc, const Query& q, const char* lds_all, int va, int block,
+  __device__ static __forceinline__ void step_codes(Result& x, Behind& w, const KeyCodes& kc, const Query& q, const char* lds_all, int va, int block,
                                                     int n_valid, int lane, Between between) {
-    f32x16 s = product(kc, q, w.less_ref);
+    f32x16 s = product(kc, q);
     between();
     if constexpr (!kFull) Base::mask(s, n_valid, lane);
     if constexpr (Base::kAlone) __builtin_amdgcn_s_setprio(1);
     float sum = 0.f;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      Base::add_values(x, __builtin_bit_cast(bf16x8, w.pf[u]), lds_all, w.block + va, u);
-      sum += weights(s, w.pf[u], x.ref, u);
+      Base::add_values(x, w.pf[u], lds_all, w.block + va, u);
+      sum += Base::weights(s, w.pf[u], 1.f, x.ref, u);
     }
-    const bool trip = __builtin_amdgcn_ballot_w64(!(sum <= w.most)) != 0;
-    if (__builtin_expect(trip, 0)) {
-      const float top = Base::largest(s, 1.f), old = reference(x, w);
-      const bool without = old == kNoKeys;
-      const float above = kFolds && without ? top : kFolds ? top + old : top;  // the block's largest score
-      const float ref = above - old > kMaxLag ? above : old, alpha = __builtin_amdgcn_exp2f(old - ref);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kTripSum)) != 0, 0)) {
+      const float full = Base::largest(s, 1.f), ref = full - x.ref > kMaxLag ? full : x.ref, alpha = __builtin_amdgcn_exp2f(x.ref - ref);
+      x.ref = ref;
       x.sum *= alpha;
       Base::scale_by(x, alpha);
-      if constexpr (kFolds) {
-        const float by = ref == kNoKeys ? 0.f : without ? ref : ref - old, less = ref == kNoKeys ? 0.f : ref == 0.f ? -0.f : -ref;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          s[v] -= by;
-          w.less_ref[v] = less;
-        }
-        asm volatile("" : "+v"(w.less_ref));  // (16 registers: one would be copied to them in every step)
-        w.most = __builtin_amdgcn_ballot_w64(ref == kNoKeys) != 0 ? -1.f : kTripSum;
-      } else {
-        x.ref = ref;
-      }
-      sum = weights(s, w.pf[0], ref, 0);
-      sum += weights(s, w.pf[1], ref, 1);
+      sum = Base::weights(s, w.pf[0], 1.f, ref, 0);
+      sum += Base::weights(s, w.pf[1], 1.f, ref, 1);
     }
     if constexpr (Base::kAlone) __builtin_amdgcn_s_setprio(0);
     x.sum += sum;
@@ -335,13 +298,14 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
       return;
     }
     if (it >= to) return;
-    Behind w;
-    w.block = 0;  // (weights of 0 for what lies there)
+    Behind w;  // (rescale and first: never so here)
+    w.alpha = 1.f;
+    w.rescale = w.first = false;
+    w.block = 0;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) w.pf[u] = u32x4{0, 0, 0, 0};
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) w.less_ref[v] = 0.f;
-    w.most = kFolds ? -1.f : kTripSum;
+      for (int e = 0; e < 8; ++e) w.pf[u][e] = (__bf16)0.f;
     KeyCodes kc;
     if (it < t8) load_codes(kc, lds_all, slot, 0, ka, kp, lane);
     // tiles of which everything is known have no branch between their instructions
@@ -373,13 +337,6 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
     }
     if constexpr (kExt) {
       if (it < to) {
-        typename Base::Behind w2;
-        w2.pf[0] = __builtin_bit_cast(bf16x8, w.pf[0]);
-        w2.pf[1] = __builtin_bit_cast(bf16x8, w.pf[1]);
-        x.ref = reference(x, w);
-        w2.alpha = 1.f;
-        w2.block = w.block;
-        w2.rescale = w2.first = false;
         bf16x8 qf[KS], kf[KS];
         const char* row = q_row();
 #pragma unroll
@@ -392,10 +349,10 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
           while (it + 3 < to && (it - 1 >= t8 || it == from)) {  // (Unit::walk: behind a tile of two blocks)
             Base::template aim<Base::kRowsOnly>(to_come, k, seg, it + 3, member);
             if constexpr (kTile == 64)
-              Base::template step<true>(x, w2, kf, qf, lds_all, kr, va, slot, 32, c, lane, [&]() {
+              Base::template step<true>(x, w, kf, qf, lds_all, kr, va, slot, 32, c, lane, [&]() {
                 if constexpr (kAhead) Base::load_k(kf, lds_all, slot + kr + 32 * RB);
               });
-            Base::template step<true>(x, w2, kf, qf, lds_all, kr, va, slot + (kTile - 32) * RB, 32, c, lane, [&]() {
+            Base::template step<true>(x, w, kf, qf, lds_all, kr, va, slot + (kTile - 32) * RB, 32, c, lane, [&]() {
               if constexpr (kTile == 32) __syncthreads();
               Base::template store<Base::kRowsOnly>(s, lds_all, after, k, it + 2, member);
               Base::template fetch<Base::kRowsOnly>(s, to_come, k, it + 3, member);
@@ -407,12 +364,12 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
           if (it + 3 < to) Base::template aim<Base::kRowsOnly>(to_come, k, seg, it + 3, member);
           int left = valid(k, it), done = 0;
           if (kTile == 64 && left > 32) {
-            Base::template step<false>(x, w2, kf, qf, lds_all, kr, va, slot, 32, c, lane, [&]() {
+            Base::template step<false>(x, w, kf, qf, lds_all, kr, va, slot, 32, c, lane, [&]() {
               if constexpr (kAhead) Base::load_k(kf, lds_all, slot + kr + 32 * RB);
             });
             done = 32;
           }
-          Base::template step<false>(x, w2, kf, qf, lds_all, kr, va, slot + done * RB, left - done, c, lane, [&]() {
+          Base::template step<false>(x, w, kf, qf, lds_all, kr, va, slot + done * RB, left - done, c, lane, [&]() {
             __syncthreads();
             if (it + 2 < to) {
               Base::template store<Base::kRowsOnly>(s, lds_all, after, k, it + 2, member);
@@ -422,13 +379,11 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
           });
           next_tile();
         }
-        Base::finish(x, w2, lds_all, va);
+        Base::finish(x, w, lds_all, va);
         return;
       }
     }
-    x.ref = reference(x, w);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) Base::add_values(x, __builtin_bit_cast(bf16x8, w.pf[u]), lds_all, w.block + va, u);
+    Base::finish(x, w, lds_all, va);
   }
 };
 

@@ -1,0 +1,85 @@
+"""Scores of the attentions over K and V in 4 bits where they are hard to keep, in every form that a launch takes: the shapes
+below reach all of them, which test_four_bits_scores_choice.py asks of the code that chooses."""
+import math
+
+import pytest
+import torch
+
+import paper_2511_16047_amd as amskv
+import plain_four_bits as plain
+import plain_operators
+from test_gpu_cache_in_4_bits import EVEN, Cache, _normal
+from test_gpu_held_states import Case
+
+pytestmark = pytest.mark.gpu
+
+# head dim -> (B, H, tokens before, queries) of a step over a cache
+STEPS = {64: [(1, 4, 48, 3), (1, 4, 64, 60), (1, 4, 840, 60), (8, 16, 48, 225), (8, 16, 64, 257), (4, 16, 300, 520)],
+         128: [(1, 4, 48, 3), (1, 4, 64, 60), (1, 4, 840, 60), (4, 16, 48, 257), (4, 16, 300, 400), (4, 16, 64, 520)]}
+# head dim -> (B, kv heads, queries, states) of a call over held states
+CALLS = {64: [(1, 1, 1, 20), (1, 4, 3, 150), (1, 4, 3, 1100), (2, 2, 1, 5000), (10, 15, 260, 600), (8, 16, 257, 557)],
+         128: [(1, 1, 1, 20), (1, 4, 3, 150), (1, 4, 60, 600), (1, 4, 3, 1100), (4, 16, 260, 150), (8, 16, 257, 557)]}
+steps = pytest.mark.parametrize("D,shape", [(d, x) for d in STEPS for x in STEPS[d]], ids=str)
+calls = pytest.mark.parametrize("D,shape", [(d, x) for d in CALLS for x in CALLS[d]], ids=str)
+
+
+def _coarse(*shape, seed):
+    """Numbers of few bits."""
+    return torch.round(_normal(*shape, seed=seed)).clamp(-2, 2)
+
+
+def _check(out, q, k, v, scale, what=""):
+    """Against the formula with Q as it is; weights of 2^-120 of the largest and less may vanish (plain_four_bits.attention)."""
+    q, k, v = (x.double() for x in (q, k, v))
+    o, bound = plain_operators.attention(q, k, v, scale)
+    s = q @ k.transpose(-1, -2) * scale
+    p, rel = torch.softmax(s, dim=-1), torch.exp(s - s.amax(dim=-1, keepdim=True))
+    bound = bound + torch.where(rel <= 1.01 * 2.0 ** -120, p, torch.zeros_like(p)) @ v.abs()
+    off = (out.double() - o).abs()
+    assert bool((off <= bound).all()), "%s: %.3e of the bound" % (what, float((off / bound).nan_to_num(math.inf).max()))
+
+
+def _step(D, B, H, before, queries, q, k, v, borrow, scale=0.0):
+    """k, v: of both scales.  The second one's output, and K and V as its attention has them."""
+    with Cache([(1, before), (1, queries)], B, H, D, [(0, 0, True)], borrow_unretained=borrow, softmax_scale=scale) as c:
+        o = torch.full_like(q, 9.0)
+        for s in range(2):
+            amskv.amskv_append_scale(c.h, 0, s, k[s], v[s])
+        amskv.amskv_attend(c.h, 0, 1, q, o)
+        held = [[plain.held(x[0]), x[1].double() if borrow else plain.held(x[1])] for x in (k, v)]
+        return o, held[0], held[1]
+
+
+# ---------------------------------------------------------------- a reference that moves far
+@steps
+@pytest.mark.parametrize("far", [2.0 ** 10, 2.0 ** 30, 2.0 ** 60])
+@pytest.mark.parametrize("borrow", [False, True])
+def test_scores_behind_far_lower_ones(D, shape, far, borrow):
+    """The first scale's scores are some -far^2; the second's come out as if alone.  (With queries of few bits.)"""
+    B, H, before, queries = shape
+    k = [_normal(B, H, n, D, seed=n).bfloat16() for n in (before, queries)]
+    v = [_normal(B, H, n, D, seed=n + 1).bfloat16() for n in (before, queries)]
+    q = _coarse(B, H, queries, D, seed=5).bfloat16()
+    q[..., :32] = 0
+    q[..., 0], k[0][..., 0], k[1][..., :32] = far, -far, 0
+    o, kk, vv = _step(D, B, H, before, queries, q, k, v, borrow, EVEN)
+    _check(o, q, kk[1], vv[1], EVEN, "far below")
+
+
+@calls
+@pytest.mark.parametrize("far", [2.0 ** 10, 2.0 ** 30, 2.0 ** 60])
+def test_held_scores_behind_far_lower_ones(D, shape, far):
+    """The same over held states: the first third of every length is far below."""
+    B, H, queries, keys = shape
+    lengths = [max(2, keys - 17 * b) for b in range(B)]
+    c = Case(H, H, D, queries, keys, lengths, sharp=2.0, hold=False)
+    c.q[..., :32] = 0
+    c.q[..., 0] = far
+    for b, n in enumerate(lengths):
+        c.k[b, :n, :, :32] = 0
+        c.k[b, :n // 3, :, 0] = -far
+    c.hold()
+    out = c.run()
+    for b, n in enumerate(lengths):
+        k, v = (plain.held(x[b, n // 3:n]).transpose(0, 1) for x in (c.k, c.v))
+        _check(out[b], c.q[b], k, v, EVEN, "%d states" % n)
