@@ -211,7 +211,8 @@ typedef struct {
  * A token's values depend on nothing but the token: slots may start at any token and capacities are any number of them.
  * The attention's products take K as held and Q either as it is or, in launches of many rows, scaled by softmax_scale * log2(e) and
  * off by at most 1/272 of the largest magnitude of a row's AMSKV_KV4_GROUP channels (from 2^-108 on; bf16 itself: 1/256 of each value).  The sum of
- * |q| |k| over the channels, times softmax_scale, has to be below 2^124, and so has |q| * softmax_scale.
+ * |q| |k| over the channels, times softmax_scale, has to be below 2^124, and so has |q| * softmax_scale.  A row of Q with a NaN comes out
+ * as NaN, and so does one with an infinite element (but in launches of few rows not where all of its scores are -inf: they weigh nothing).
  * amskv_cache_bytes_held counts half a byte per element and one per group.  The modes, layouts and limits of the 8-bit
  * cache, the similarity and density calls among them. */
 

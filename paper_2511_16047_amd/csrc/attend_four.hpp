@@ -29,6 +29,7 @@ namespace amskv {
 namespace rows {
 
 typedef unsigned u32x6 __attribute__((ext_vector_type(6)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
@@ -66,13 +67,16 @@ __device__ __forceinline__ void split_query(QueryParts<D>& q, const u32x4 (&raw)
 #pragma unroll
   for (int c = 0; c < D / 64; ++c) {
     f32x16 even, odd;
+    u16x2 most = {0, 0};  // the bits of the largest magnitudes
     float m = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       even[i] = __builtin_bit_cast(float, raw[c][i / 4][i % 4] << 16) * factor;
       odd[i] = __builtin_bit_cast(float, raw[c][i / 4][i % 4] & 0xffff0000u) * factor;
       m = max3(m, __builtin_fabsf(even[i]), __builtin_fabsf(odd[i]));
+      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, raw[c][i / 4][i % 4] & 0x7fff7fffu));
     }
+    const bool finite = max(most[0], most[1]) < 0x7f80;
     const int bits = __builtin_bit_cast(int, m);  // 7.5 = 1.875 * 2^2
     const int a = min(max((bits >> 23) - 127 - 2 + ((bits & 0x7fffff) > 0x700000 ? 1 : 0), -110), 126);
     q.powers[c] = 0;
@@ -80,7 +84,7 @@ __device__ __forceinline__ void split_query(QueryParts<D>& q, const u32x4 (&raw)
     for (int p = 0; p < kParts; ++p) {
       const int byte = a - 5 * p + 127;
       const float by = power_of_byte(byte);
-      q.powers[c] |= (unsigned)byte << (8 * p);
+      q.powers[c] |= (unsigned)(finite ? byte : 255) << (8 * p);  // (255: NaN, which is what all scores of the row become)
       q.part[c][p] = parts_of(even, odd, by);
       if (p + 1 < kParts) {
         const f32x32 held = values_of(q.part[c][p], by);

@@ -83,3 +83,42 @@ def test_held_scores_behind_far_lower_ones(D, shape, far):
     for b, n in enumerate(lengths):
         k, v = (plain.held(x[b, n // 3:n]).transpose(0, 1) for x in (c.k, c.v))
         _check(out[b], c.q[b], k, v, EVEN, "%d states" % n)
+
+
+# ---------------------------------------------------------------- queries that are not finite
+def _spoilt(q):
+    """Rows with one channel that is NaN or infinite, and which they are."""
+    q, spoilt = q.clone(), torch.zeros(q.shape[:-1], dtype=torch.bool, device="cuda")
+    D, flat, rows = q.shape[-1], q.view(-1, q.shape[-1]), spoilt.view(-1)
+    for i, x in enumerate((math.nan, math.inf, -math.inf)):
+        for j, row in enumerate((i, len(flat) // 2 + i, len(flat) - 1 - i)):
+            flat[row % len(flat), (7 * j + 33 * i) % D], rows[row % len(flat)] = x, True
+    return q, spoilt
+
+
+# The reference of a row moves when any row of its wave asks for it (a score more than 2^6 above it is taken as it is while the sum stays
+# below 2^10), so the other rows need not be the same bits: they are as near to the formula as ever.
+def _check_rest(out, rows, q, k, v):
+    want, bound = plain.attention(q.masked_fill(rows[..., None], 0.0), k, v, 1 / math.sqrt(q.shape[-1]))
+    assert bool(torch.isnan(out[rows]).all()) and bool(((out.double() - want).abs() <= bound)[~rows].all())
+
+
+@steps
+@pytest.mark.parametrize("borrow", [False, True])
+def test_queries_that_are_not_finite(D, shape, borrow):
+    """A row with a channel that is not finite comes out as NaN in every form, and no other row does."""
+    B, H, before, queries = shape
+    k, v = ([_normal(B, H, n, D, seed=n + i).bfloat16() for n in (before, queries)] for i in range(2))
+    q, rows = _spoilt(_normal(B, H, queries, D, seed=5).bfloat16())
+    out, k, v = _step(D, B, H, before, queries, q, k, v, borrow)
+    _check_rest(out, rows, q, *(torch.cat(x, dim=2) for x in (k, v)))
+
+
+@calls
+def test_held_states_and_queries_that_are_not_finite(D, shape):
+    B, H, queries, keys = shape
+    c = Case(H, H, D, queries, keys, [max(1, keys - 17 * b) for b in range(B)])
+    c.q, rows = _spoilt(c.q)
+    out = c.run()
+    for b, n in enumerate(c.lengths):
+        _check_rest(out[b], rows[b], c.q[b], *(plain.held(x[b, :n]).transpose(0, 1) for x in c.kv))
