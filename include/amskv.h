@@ -209,10 +209,10 @@ typedef struct {
  * number exactly: off by at most 2^(e-2) below 2^(e+1), 2^(e-1) below 2^(e+2) and 2^e above (elements beyond 7 * 2^125 apart), which
  * is at most 2/7 of m; elements of at most 2^-102 become 0.  4.25 bits an element.
  * A token's values depend on nothing but the token: slots may start at any token and capacities are any number of them.
- * The attention's products take K as held and Q either as it is or, in launches of many rows, scaled by softmax_scale * log2(e) and
- * off by at most 1/272 of the largest magnitude of a row's AMSKV_KV4_GROUP channels (from 2^-108 on; bf16 itself: 1/256 of each value).  The sum of
- * |q| |k| over the channels, times softmax_scale, has to be below 2^124, and so has |q| * softmax_scale.  A row of Q with a NaN comes out
- * as NaN, and so does one with an infinite element (but in launches of few rows not where all of its scores are -inf: they weigh nothing).
+ * The attention's products take K as held and Q as it is (in launches of many rows elements below 2^-14 of the largest magnitude of their
+ * AMSKV_KV4_GROUP channels may be off by 2^-21 of that magnitude, and the products of 8 channels, 8 i .. 8 i + 7, are added up in units of
+ * 2^-13 of the largest).  The sum of |q| |k| over the channels has to be below 2^127, and times softmax_scale below 2^124.  A row of Q with a NaN comes out as NaN, and so does one with an infinite element (but in launches of few rows not
+ * where all of its scores are -inf: they weigh nothing).
  * amskv_cache_bytes_held counts half a byte per element and one per group.  The modes, layouts and limits of the 8-bit
  * cache, the similarity and density calls among them. */
 
@@ -538,7 +538,7 @@ int32_t amskv_cross_export(const amskv_cross* cross, const void* K_held_dev, con
                            const int32_t* lengths_dev, const int32_t* offsets_dev, void* stream);
 
 /* amskv_cross_attend over held states: K_dev and V_dev are the held tensors, cross->k and cross->v are not read, lengths_dev,
- * offsets_dev, batch, kv_heads, head_dim and kv_tokens (packed: kv_rows) as they were held with; Q's rounding and the scores' range are the 4-bit cache's; all else is as above. */
+ * offsets_dev, batch, kv_heads, head_dim and kv_tokens (packed: kv_rows) as they were held with; Q and the scores' range as with the 4-bit cache; all else is as above. */
 
 /* Static text for a status code. */
 const char* amskv_status_string(int32_t status);

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void att
   U::clear(x);
   if constexpr (kFour) {
     typename Team::Query parts;
-    rows::split_query(parts, raw, scale_log2e);
+    rows::split_query(parts, raw);
     Team::walk(x, parts, [&]() { return q_row(U::fresh(threadIdx.x)); }, lds, keys, seg, 0, Team::tiles(keys), scale_log2e, active);
   } else {
     U::walk(x, qf, lds, keys, seg, 0, U::tiles(keys), scale_log2e, active);

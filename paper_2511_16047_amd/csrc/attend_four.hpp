@@ -3,17 +3,23 @@
 //
 // The matrix cores take e2m1 numbers with a power of two to every 32 along the sum: S^T = K Q^T is formed by
 // v_mfma_scale_f32_32x32x64_f8f6f4 from K's codes and powers straight out of LDS, a quarter of bf16's bytes there and no conversion.  Its
-// other operand may have 6 bits without loss of speed (4 times bf16's rate; 8 bits: twice), so y = q times the factor of the scores is held
-// as the sum of two e2m3 numbers (4 significant bits each), made once for a workgroup: 32 channels with largest element m, 2^a the least
-// power with m <= 7.5 * 2^a, are hi * 2^a + lo * 2^(a - 5), hi the number nearest to y * 2^-a, lo nearest to what is left.  hi's step is
-// 1/2 from 4 on, 1/4 from 2 on and 1/8 below, which leaves up to 8, 4 and 2 for lo: y is off by at most 2^(a - 8) from 2 * 2^a on and 2^(a
-// - 9) below; from 4 * 2^a on by 2^(a - 7), and up to 2^(a - 6) where lo would be 7.75 to 8 and is 7.5 (one of 32; a bf16 number itself
-// stands for what lies within 2^(a - 6) there).  lo at 2^(a - 4) has no such end, but steps twice as wide for all others: over normal
-// values y is off by 0.0008 of its size (rms) as it is here, 0.0011 as it would be there, with gains from channel to channel of e^(0.5
-// normal) 0.0009 and 0.0015.  Two products at 4 times the rate: half of the time of bf16's (15.4 ns of a SIMD each for 64 channels, bf16
-// 73.6; e4m3 parts 28.6 each; a third part at head dim 128, 64 units 4096 x 6421, 584 -> 651 us).  V becomes bf16 on its way to LDS, once
-// for all waves: weights in 6 bits would have to be split in two for every block, which takes the vector ALUs more (a conversion of 32
-// numbers 38 ns, back 33) than the matrix cores save.
+// other operand has 8 bits, and Q, whose numbers have 8 significant bits, is the sum of two e4m3 numbers (4 each), made once for a
+// workgroup: 32 channels with largest element m, 2^a the least power with m <= 448 * 2^a, are hi * 2^a + lo * 2^(a - 4), hi the number
+// nearest to q * 2^-a, lo what is left.  That is q itself: hi leaves at most half of its step, a sign and 4 bits.  (e4m3's own range ends it:
+// elements below 2^-6 * 2^a, 2^-14 of m, may be off by 2^-14 * 2^a, 2^-21 of m.)  With 8 bits the products of 8 neighbouring channels are cut
+// to units of 2^-13 of the power of two of their largest before they are added up in fp32 (as measured; products of 6 bits lie within that):
+// a product, of 6 bits itself, loses something if it is 2^-8 of the largest and less.  Parts of 6 bits lose nothing there, but have the
+// range of 4 bits and lose Q's small channels beside a large one.  Emulated, scores of standard deviation 9, outputs off by (rms of their size):
+//                                                          Q itself  here    two e2m3  e4m3 + e3m2  three e2m3  bf16(Q * factor)
+//   plain                                                  0.0015    0.0015  0.0026    0.0015       0.0015      0.0045
+//   a channel of Q 30 times the others                     0.0015    0.0015  0.0071    0.0022       0.0015      0.0038
+//   100 times                                              0.0019    0.0024  0.0097    0.0035       0.0019      0.0023
+//   a channel of Q 30 times, K there as much smaller       0.0015    0.0015  0.014     0.0035       0.0016      0.0047
+//   300 times                                              0.0016    0.0016  0.14      0.027        0.0074      0.0052
+// and as measured (us; 64 units 4096 x 6421 and 2304 x 3925 at head dim 128, 3840 units 256 x 530 at 64): here 679, 263, 190; two e2m3 618, 242,
+// 174; three 679, 269, 194; four, which lose nothing anywhere, 728, 316, 198.  A product of both parts takes 57 ns of a SIMD for 64 channels, bf16's
+// 74 (a part of 6 bits 15).  V becomes bf16 on its way to LDS, once for all waves: weights in 6 bits would have to be split in two for
+// every block, which takes the vector ALUs more (a conversion of 32 numbers 38 ns, back 33) than the matrix cores save.
 //
 // Bound, and what it measured.  Head dim 128, 64 units: the matrix pipes and the power they take, 4096 x 6421 by teams of eight 576 to 601
 // us (1.43 to 1.50 PFLOP/s; codes of 8 bits through bf16 784), 2304 x 3925 by teams of four 234 to 255, 576 x 1076 29.  Head dim 64, 3840
@@ -28,31 +34,28 @@
 namespace amskv {
 namespace rows {
 
-typedef unsigned u32x6 __attribute__((ext_vector_type(6)));
+typedef unsigned u32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x32 __attribute__((ext_vector_type(32)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// Q of a lane times the factor of its scores: channels 64 c + 32 h .. + 31 of its row in two parts, the larger first, and the bytes of
-// their powers.
-constexpr int kParts = 2;
+// Q of a lane's row in two parts, the larger first, where an operand of 8 bits has its channels: 64 c + 16 h .. + 15, then 64 c + 32 + 16 h
+// .. + 15; and the bytes of their powers, of channels 64 c + 32 h .. + 31 (c's in bytes 2 c and 2 c + 1).
 template <int D>
 struct QueryParts {
-  u32x6 part[D / 64][kParts];
-  unsigned powers[D / 64];
+  u32x8 high[D / 64], low[D / 64];
+  unsigned powers;
 };
-// 32 numbers as e2m3 times a power of two, even and odd ones by turns, and back.  Written out: the conversions write their first results
-// before they have read all operands, and the compiler's own may let the two overlap, which gave wrong parts of Q in some builds.  (The
-// wait is for what reads the results: the compiler does not see into inline assembly.)
-__device__ __forceinline__ u32x6 parts_of(const f32x16& even, const f32x16& odd, float by) {
-  u32x6 r;
-  asm("v_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, %3\n\ts_nop 7" : "=&v"(r) : "v"(even), "v"(odd), "v"(by));
-  return r;
-}
-__device__ __forceinline__ f32x32 values_of(const u32x6& x, float by) {
-  f32x32 r;
-  asm("v_cvt_scalef32_pk32_f32_fp6 %0, %1, %2\n\ts_nop 7" : "=&v"(r) : "v"(x), "v"(by));
-  return r;
+// words of channels 32 h .. + 31 to where that is
+__device__ __forceinline__ u32x8 across(u32x8 x) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const auto s = __builtin_amdgcn_permlane32_swap(x[w], x[4 + w], false, false);
+    x[w] = s[0];
+    x[4 + w] = s[1];
+  }
+  return x;
 }
 // (Q is asked for before anything that has to be waited for)
 template <int D>
@@ -62,39 +65,38 @@ __device__ __forceinline__ void load_query(u32x4 (&raw)[D / 64][4], const char* 
 #pragma unroll
     for (int i = 0; i < 4; ++i) raw[c][i] = *reinterpret_cast<const u32x4*>(row + 128 * c + 64 * h + 16 * i);
 }
+// two numbers of Q less what is held of them, which a bf16 number is
+__device__ __forceinline__ bf16x2 left_of(unsigned two, const f32x2& held) {
+  const float x = __builtin_bit_cast(float, two << 16) - held[0], y = __builtin_bit_cast(float, two & 0xffff0000u) - held[1];
+  return __builtin_bit_cast(bf16x2, __builtin_bit_cast(unsigned, x) >> 16 | (__builtin_bit_cast(unsigned, y) & 0xffff0000u));
+}
 template <int D>
-__device__ __forceinline__ void split_query(QueryParts<D>& q, const u32x4 (&raw)[D / 64][4], float factor) {
+__device__ __forceinline__ void split_query(QueryParts<D>& q, const u32x4 (&raw)[D / 64][4]) {
+  q.powers = 0;
 #pragma unroll
   for (int c = 0; c < D / 64; ++c) {
-    f32x16 even, odd;
-    u16x2 most = {0, 0};  // the bits of the largest magnitudes
-    float m = 0.f;
+    u16x2 most = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      even[i] = __builtin_bit_cast(float, raw[c][i / 4][i % 4] << 16) * factor;
-      odd[i] = __builtin_bit_cast(float, raw[c][i / 4][i % 4] & 0xffff0000u) * factor;
-      m = max3(m, __builtin_fabsf(even[i]), __builtin_fabsf(odd[i]));
-      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, raw[c][i / 4][i % 4] & 0x7fff7fffu));
+    for (int i = 0; i < 16; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, raw[c][i / 4][i % 4] & 0x7fff7fffu));
+    const int m = max((int)most[0], (int)most[1]);  // the bits of the largest magnitude; 448 = 1.75 * 2^8
+    const int byte = max((m >> 7) - 8 + ((m & 0x7f) > 0x60 ? 1 : 0), 5);
+    const float by = power_of_byte(byte), by_low = power_of_byte(byte - 4);
+    // (0xff: NaN, which is what all scores of the row become)
+    q.powers |= (m < 0x7f80 ? (unsigned)byte | (unsigned)(byte - 4) << 8 : 0xffffu) << (16 * c);
+    u32x8 high, low;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const unsigned x = raw[c][w / 2][2 * (w % 2)], y = raw[c][w / 2][2 * (w % 2) + 1];
+      i16x2 code = {0, 0}, left = {0, 0};
+      code = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(code, __builtin_bit_cast(bf16x2, x), by, false);
+      code = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(code, __builtin_bit_cast(bf16x2, y), by, true);
+      high[w] = __builtin_bit_cast(unsigned, code);
+      left = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(left, left_of(x, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(high[w], by, false)), by_low, false);
+      left = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(left, left_of(y, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(high[w], by, true)), by_low, true);
+      low[w] = __builtin_bit_cast(unsigned, left);
     }
-    const bool finite = max(most[0], most[1]) < 0x7f80;
-    const int bits = __builtin_bit_cast(int, m);  // 7.5 = 1.875 * 2^2
-    const int a = min(max((bits >> 23) - 127 - 2 + ((bits & 0x7fffff) > 0x700000 ? 1 : 0), -110), 126);
-    q.powers[c] = 0;
-#pragma unroll
-    for (int p = 0; p < kParts; ++p) {
-      const int byte = a - 5 * p + 127;
-      const float by = power_of_byte(byte);
-      q.powers[c] |= (unsigned)(finite ? byte : 255) << (8 * p);  // (255: NaN, which is what all scores of the row become)
-      q.part[c][p] = parts_of(even, odd, by);
-      if (p + 1 < kParts) {
-        const f32x32 held = values_of(q.part[c][p], by);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          even[i] -= held[2 * i];
-          odd[i] -= held[2 * i + 1];
-        }
-      }
-    }
+    q.high[c] = across(high);
+    q.low[c] = across(low);
   }
 }
 
@@ -200,34 +202,30 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
     for (int c = 0; c < D / 64; ++c) kc.code[c] = *reinterpret_cast<const u32x4*>(at + (ka ^ (32 * c)));
     kc.powers = *reinterpret_cast<const unsigned*>(lds_all + slot + 32 * 32 * block + kp) >> (8 * (lane >> 5));
   }
-  // scores times the factor
-  template <int kPart, int kChunk>
-  __device__ static __forceinline__ f32x16 multiply(const KeyCodes& kc, const Query& q, const f32x16& add) {
+  template <int kChunk>
+  __device__ static __forceinline__ f32x16 multiply(const KeyCodes& kc, const Query& q, f32x16 s) {
     const u32x4& k = kc.code[kChunk];
-    const u32x6& x = q.part[kChunk][kPart];
-    // (4: e2m1, 2: e2m3; the bytes of the powers are picked by constants)
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(i32x8{(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0},
-                                                           i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0}, add, 4, 2,
-                                                           2 * kChunk, kc.powers, kPart, q.powers[kChunk]);
+    const i32x8 codes = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
+    // (4: e2m1, 0: e4m3; the bytes of the powers are picked by constants)
+    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes, __builtin_bit_cast(i32x8, q.high[kChunk]), s, 4, 0, 2 * kChunk, kc.powers,
+                                                        2 * kChunk, q.powers);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes, __builtin_bit_cast(i32x8, q.low[kChunk]), s, 4, 0, 2 * kChunk, kc.powers,
+                                                           2 * kChunk + 1, q.powers);
   }
+  // S^T of these keys.  The products start from 0: started from the references, a block would save 16 multiply-adds of some 106 vector
+  // instructions, but scores come out rounded at the size of a reference that may lie far from them.
   __device__ static __forceinline__ f32x16 product(const KeyCodes& kc, const Query& q) {
     f32x16 s;
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = 0.f;
-    s = multiply<0, 0>(kc, q, s);
-    s = multiply<1, 0>(kc, q, s);
-    if constexpr (D == 128) {
-      s = multiply<0, 1>(kc, q, s);
-      s = multiply<1, 1>(kc, q, s);
-    }
+    s = multiply<0>(kc, q, s);
+    if constexpr (D == 128) s = multiply<1>(kc, q, s);
     return s;
   }
   // Unit::step in one basic block (as its kOneBlock): the first block, which has none before it, takes weights of 0 for what lies in its slot.
-  // The products start from 0: started from the references, a block would save 16 multiply-adds of some 106 vector instructions, but
-  // scores come out rounded at the size of a reference that may lie far from them.
   template <bool kFull, class Between>
   __device__ static __forceinline__ void step_codes(Result& x, Behind& w, const KeyCodes& kc, const Query& q, const char* lds_all, int va, int block,
-                                                    int n_valid, int lane, Between between) {
+                                                    int n_valid, float c, int lane, Between between) {
     f32x16 s = product(kc, q);
     between();
     if constexpr (!kFull) Base::mask(s, n_valid, lane);
@@ -236,15 +234,15 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       Base::add_values(x, w.pf[u], lds_all, w.block + va, u);
-      sum += Base::weights(s, w.pf[u], 1.f, x.ref, u);
+      sum += Base::weights(s, w.pf[u], c, x.ref, u);
     }
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kTripSum)) != 0, 0)) {
-      const float full = Base::largest(s, 1.f), ref = full - x.ref > kMaxLag ? full : x.ref, alpha = __builtin_amdgcn_exp2f(x.ref - ref);
+      const float full = Base::largest(s, c), ref = full - x.ref > kMaxLag ? full : x.ref, alpha = __builtin_amdgcn_exp2f(x.ref - ref);
       x.ref = ref;
       x.sum *= alpha;
       Base::scale_by(x, alpha);
-      sum = Base::weights(s, w.pf[0], 1.f, ref, 0);
-      sum += Base::weights(s, w.pf[1], 1.f, ref, 1);
+      sum = Base::weights(s, w.pf[0], c, ref, 0);
+      sum += Base::weights(s, w.pf[1], c, ref, 1);
     }
     if constexpr (Base::kAlone) __builtin_amdgcn_s_setprio(0);
     x.sum += sum;
@@ -259,9 +257,9 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
     asm volatile("" : "+v"(lane));  // (not kept for what follows)
     const int t8 = min(Base::tiles_of_codes(k), to);
     int it = from;
-    const int ka = k_lane4(lane), va = Base::v_lane(lane) - Base::kTensor + kOfK;
-    int kp = kPowers + 32 * (lane & 31) + 4 * ((lane & 31) >> 3);
-    asm volatile("" : "+v"(kp));  // (one register)
+    const int ka = k_lane4(lane);
+    int va = Base::v_lane(lane) - Base::kTensor + kOfK, kp = kPowers + 32 * (lane & 31) + 4 * ((lane & 31) >> 3);
+    asm volatile("" : "+v"(va), "+v"(kp));  // (a register each)
     Staged s;
     Aim to_come;
     auto load = [&](Staged& y, int i) {
@@ -316,8 +314,8 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
     while (it + 3 < t8) {
       aim_codes(to_come, k, seg, it + 3, member);
       if constexpr (kTile == 64)
-        step_codes<true>(x, w, kc, q, lds_all, va, slot, 32, lane, [&]() { load_codes(kc, lds_all, slot, 1, ka, kp, lane); });
-      step_codes<true>(x, w, kc, q, lds_all, va, slot + (kTile - 32) * RB, 32, lane, [&]() {
+        step_codes<true>(x, w, kc, q, lds_all, va, slot, 32, c, lane, [&]() { load_codes(kc, lds_all, slot, 1, ka, kp, lane); });
+      step_codes<true>(x, w, kc, q, lds_all, va, slot + (kTile - 32) * RB, 32, c, lane, [&]() {
         if constexpr (kTile == 32) __syncthreads();
         store_codes(s, lds_all, after, member);
         fetch_codes(s, to_come, k, member);
@@ -327,13 +325,14 @@ struct FourBitTeam : Unit<D, kTeamWaves, 1, 4> {
       next_tile();
     }
     while (it < t8) {
+      asm volatile("" : "+v"(lane), "+v"(member));  // (what is derived from them is not kept from tile to tile: 12 registers, a spill at head dim 128)
       if (it + 3 < to) aim_any(to_come, k, seg, it + 3, member);
       int left = valid(k, it), done = 0;
       if (kTile == 64 && left > 32) {
-        step_codes<true>(x, w, kc, q, lds_all, va, slot, 32, lane, [&]() { load_codes(kc, lds_all, slot, 1, ka, kp, lane); });
+        step_codes<true>(x, w, kc, q, lds_all, va, slot, 32, c, lane, [&]() { load_codes(kc, lds_all, slot, 1, ka, kp, lane); });
         done = 32;
       }
-      step_codes<false>(x, w, kc, q, lds_all, va, slot + done * RB, left - done, lane, [&]() {
+      step_codes<false>(x, w, kc, q, lds_all, va, slot + done * RB, left - done, c, lane, [&]() {
         turn_over();
         if (it + 1 < t8) load_codes(kc, lds_all, next, 0, ka, kp, lane);
       });

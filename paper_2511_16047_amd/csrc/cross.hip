@@ -100,7 +100,7 @@ __global__ __launch_bounds__(64 * kTeamWaves* kTeams, kMinWavesPerSimd) void cro
   none.n = 0;
   if constexpr (kFour) {
     typename Team::Query parts;
-    rows::split_query(parts, raw, a.scale_log2e);
+    rows::split_query(parts, raw);
     Team::walk(x, parts, [&]() { return q_row; }, lds, keys, none, from, to, a.scale_log2e, active);
   } else {
     U::walk(x, qf, lds, keys, none, from, to, a.scale_log2e, active);

@@ -28,15 +28,38 @@ def _coarse(*shape, seed):
     return torch.round(_normal(*shape, seed=seed)).clamp(-2, 2)
 
 
+def _lost(q, k):
+    """Most that a score (of one head, q [Tq, D], k [Tk, D], times the scale still to come) may lose in launches of many rows.
+
+    32 channels of Q with largest element m are numbers of 8 bits times 2^a, 224 * 2^a < m <= 448 * 2^a, in two parts of 4 significant
+    bits: exact down to 2^-6 * 2^a, below off by 2^-14 * 2^a at most, which is less than 2^-21.8 m.  The products of 8 channels are cut to
+    units of 2^-13 of the power of two of the largest.  Q's larger part is off by 2^-4 of q at most, so with P the largest |q k| the unit is at most U =
+    2^-13 * 2^floor(log2(17/16 P)), and a product, of 4 + 2 bits, that is 32 U or more is a multiple of it: what is lost is at most min(U, 17/16
+    |q k|) where 15/16 |q k| < 32 U.  The smaller part is at most 2^-4 q, its unit U / 16: 7 of those."""
+    m = q.unflatten(-1, (-1, 32)).abs().amax(dim=-1, keepdim=True).expand(-1, -1, 32).flatten(-2)
+    off = torch.where(q.abs() < m * (2.0 ** -6 / 224), m * 2.0 ** -21.8, torch.zeros_like(m)) @ k.abs().T
+    for i in range(0, q.shape[-1], 8):
+        p = (q[:, None, i:i + 8] * k[None, :, i:i + 8]).abs()
+        unit = torch.exp2(torch.floor(torch.log2(p.amax(dim=-1, keepdim=True) * (17 / 16) + 1e-300)) - 13)
+        off += torch.where(p * (15 / 16) < 32 * unit, torch.minimum(p * (17 / 16), unit), torch.zeros_like(p)).sum(dim=-1) + 7 / 16 * unit[..., 0]
+    return off
+
+
 def _check(out, q, k, v, scale, what=""):
-    """Against the formula with Q as it is; weights of 2^-120 of the largest and less may vanish (plain_four_bits.attention)."""
-    q, k, v = (x.double() for x in (q, k, v))
-    o, bound = plain_operators.attention(q, k, v, scale)
-    s = q @ k.transpose(-1, -2) * scale
-    p, rel = torch.softmax(s, dim=-1), torch.exp(s - s.amax(dim=-1, keepdim=True))
-    bound = bound + torch.where(rel <= 1.01 * 2.0 ** -120, p, torch.zeros_like(p)) @ v.abs()
-    off = (out.double() - o).abs()
-    assert bool((off <= bound).all()), "%s: %.3e of the bound" % (what, float((off / bound).nan_to_num(math.inf).max()))
+    """[..., T, D] against the formula with Q as it is; scores may be off by _lost(), and weights of 2^-120 of the largest and less may
+    vanish (plain_four_bits.attention).  With weights p_j e^d_j, |d_j| <= e_j, in both sums O is off by at most sum p_j |e^d_j - 1| |v_j - o| / sum
+    p_j e^d_j <= e^max(e) sum p_j (e^e_j - 1) (|v_j| + |o|)."""
+    out, q, k, v = (x.double().flatten(0, -3) for x in (out, q, k, v))
+    for i in range(len(q)):
+        o, bound = plain_operators.attention(q[i], k[i], v[i], scale)
+        e = _lost(q[i], k[i]) * scale
+        s = q[i] @ k[i].T * scale
+        p, rel = torch.softmax(s, dim=-1), torch.exp(s - s.amax(dim=-1, keepdim=True))
+        w = p * torch.expm1(e) * torch.exp(e.amax(dim=-1, keepdim=True))
+        bound = bound * torch.exp(e.amax(dim=-1, keepdim=True)) + w @ v[i].abs() + w.sum(dim=-1, keepdim=True) * o.abs()
+        bound = bound + torch.where(rel <= 1.01 * 2.0 ** -120, p, torch.zeros_like(p)) @ v[i].abs()
+        off = (out[i] - o).abs()
+        assert bool((off <= bound).all()), "%s, %d: %.3e of the bound" % (what, i, float((off / bound).nan_to_num(math.inf).max()))
 
 
 def _step(D, B, H, before, queries, q, k, v, borrow, scale=0.0):
@@ -122,3 +145,66 @@ def test_held_states_and_queries_that_are_not_finite(D, shape):
     out = c.run()
     for b, n in enumerate(c.lengths):
         _check_rest(out[b], rows[b], c.q[b], *(plain.held(x[b, :n]).transpose(0, 1) for x in c.kv))
+
+
+# ---------------------------------------------------------------- queries as they come
+def _queries(kind, *shape):
+    """Q, and what K's channels are taken by: scores of a standard deviation of 20; a channel of Q 30 and 300 times the others, whose
+    keys are as much smaller, scores of 8; channels of every size down to 2^-24, each with a random one in full."""
+    x, D = _normal(*shape, seed=11), shape[-1]
+    gain = torch.ones(D, device="cuda")
+    if kind == "sharp":
+        return (20 * x).bfloat16(), gain
+    if kind.startswith("outlier"):
+        gain[5], gain[D - 20] = float(kind[7:]), float(kind[7:])
+        return (8 * x * gain).bfloat16(), 1 / gain
+    size = 2.0 ** (-24 * torch.rand(*shape, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda"))
+    return (x * size).bfloat16(), gain
+
+
+KINDS = ["sharp", "outlier30", "outlier300", "wide"]
+
+
+@steps
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("borrow", [False, True])
+def test_queries_as_they_come(D, shape, kind, borrow):
+    B, H, before, queries = shape
+    q, by = _queries(kind, B, H, queries, D)
+    k = [(_normal(B, H, n, D, seed=n) * by).bfloat16() for n in (before, queries)]
+    v = [_normal(B, H, n, D, seed=n + 1).bfloat16() for n in (before, queries)]
+    o, k, v = _step(D, B, H, before, queries, q, k, v, borrow)
+    _check(o, q, torch.cat(k, dim=2), torch.cat(v, dim=2), 1 / math.sqrt(D), kind)
+
+
+@calls
+@pytest.mark.parametrize("kind", KINDS)
+def test_held_states_and_queries_as_they_come(D, shape, kind):
+    B, H, queries, keys = shape
+    c = Case(H, H, D, queries, keys, [max(1, keys - 17 * b) for b in range(B)], spoil=False, hold=False)
+    c.q, by = _queries(kind, B, H, queries, D)
+    c.k *= by
+    c.hold()
+    out = c.run()
+    for b, n in enumerate(c.lengths):
+        k, v = (plain.held(x[b, :n]).transpose(0, 1) for x in (c.k, c.v))
+        _check(out[b], c.q[b], k, v, 1 / math.sqrt(D), "%s, %d states" % (kind, n))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_row_is_the_same_in_every_form(D):
+    """Rows of one query at a time (waves by themselves) and of all (teams): each within the bound of Q as it is."""
+    B, H, queries, keys = (8, 16, 257, 557)
+    c = Case(H, H, D, queries, keys, [keys] * B, spoil=False, hold=False)
+    c.q, by = _queries("outlier300", B, H, queries, D)
+    c.k *= by
+    c.hold()
+    many = c.run()
+    q, c.x.q_tokens = c.q, 1
+    few = torch.empty_like(q[:, :, :1])
+    c.x.o = amskv.Strides(H * D, D, D)
+    for row in (0, 100, 256):
+        amskv.amskv_cross_attend(c.x, q[:, :, row:].data_ptr(), *c.held, few)
+        k, v = (plain.held(x).transpose(1, 2) for x in (c.k, c.v))
+        for o in (few, many[:, :, row:row + 1]):
+            _check(o, q[:, :, row:row + 1], k, v, 1 / math.sqrt(D), "row %d" % row)
