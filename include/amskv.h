@@ -521,7 +521,9 @@ int32_t amskv_cross_attend(const amskv_cross* cross, const void* Q_dev, const vo
 /* States held in 4 bits (amskv_cross.dtype = AMSKV_DTYPE_BF16_KV4).  A prompt's K and V are made once and read by every step: they can
  * be held in 4 bits, in the format of the 4-bit cache, 4.25 bits an element.  A held tensor is a caller's buffer of
  * amskv_cross_held_bytes bytes (packed 0: batch * kv_heads units of kv_tokens rows; 1: kv_heads units of kv_rows rows, for offsets_dev),
- * 16-byte aligned, of which no other call writes anything.  kv_heads up to 2^24.  Host only. */
+ * 16-byte aligned, of which no other call writes anything.  The calls below take its address without a size: *cross says how long it is and where
+ * its powers of two begin, so batch, kv_heads, head_dim and kv_tokens or kv_rows are the same in all of them (a part of a held batch cannot be
+ * attended; batch elements may have no states).  kv_heads up to 2^24.  Host only. */
 int32_t amskv_cross_held_bytes(const amskv_cross* cross, int32_t packed, uint64_t* bytes_out);
 
 /* K_dev and V_dev (bf16, strides cross->k and cross->v) into held tensors; either pair may be NULL.  Rows that hold states are

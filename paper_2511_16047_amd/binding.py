@@ -191,7 +191,7 @@ def load_library() -> C.CDLL:
         _pycalls.bind_operators(*(C.cast(f, vp).value for f in (lib.amskv_append_scale_rotary, lib.amskv_rotate, lib.amskv_cross_attend)),
                                 Rope, Strides, Cross)
         _hold, _export = _pycalls.cross_hold, _pycalls.cross_export
-        _pycalls.bind_held(*(C.cast(f, vp).value for f in (lib.amskv_cross_hold, lib.amskv_cross_export)))
+        _pycalls.bind_held(*(C.cast(f, vp).value for f in (lib.amskv_cross_hold, lib.amskv_cross_export, lib.amskv_cross_held_bytes)))
     _lib = lib
     return lib
 
@@ -507,7 +507,7 @@ def amskv_cross_workspace_bytes(cross) -> int:
 
 
 def amskv_cross_attend(cross, Q, K, V, O, lengths=None, offsets=None, workspace=None, workspace_bytes=None, stream=None):
-    """K, V: the states, or with dtype AMSKV_DTYPE_BF16_KV4 their held tensors (amskv_cross_hold).
+    """K, V: the states, or with dtype AMSKV_DTYPE_BF16_KV4 their held tensors (amskv_cross_hold), of just the size that `cross` says.
     lengths: device int32 [batch]; offsets: device int32 [batch + 1]; workspace: device tensor (its size is taken from it) or,
     with workspace_bytes, an address."""
     if workspace is None:
@@ -519,8 +519,9 @@ def amskv_cross_attend(cross, Q, K, V, O, lengths=None, offsets=None, workspace=
     try:
         status = _cross(cross, Q, K, V, O, lengths, offsets, workspace, workspace_bytes, stream)
     except _UNUSUAL:
-        status = _lib.amskv_cross_attend(cross, _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(lengths), _ptr(offsets), _ptr(workspace),
-                                         workspace_bytes, _stream(stream))
+        status = _right_size(cross, offsets, K, V) or \
+            _lib.amskv_cross_attend(cross, _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(lengths), _ptr(offsets), _ptr(workspace),
+                                    workspace_bytes, _stream(stream))
     if status:
         _check(status, "amskv_cross_attend")
 
@@ -532,14 +533,29 @@ def amskv_cross_held_bytes(cross, packed=False) -> int:
     return int(out.value)
 
 
+def _right_size(cross, offsets, *held):
+    """Status of a call with these held tensors, as far as their sizes go (csrc/pycalls.cpp does the same)."""
+    need = C.c_uint64(0)
+    if cross is None or _lib.amskv_cross_held_bytes(cross, int(offsets is not None), C.byref(need)) or not need.value:
+        return 0
+    for x in held:
+        have = need.value if x is None or isinstance(x, int) else x.numel() * x.element_size()
+        if have != need.value:
+            return AMSKV_ERR_ARENA_TOO_SMALL if have < need.value else AMSKV_ERR_INVALID_ARG
+    return 0
+
+
 def amskv_cross_hold(cross, K, V, K_held, V_held, lengths=None, offsets=None, stream=None):
-    """K, V: bf16 states at the strides of `cross`; K_held, V_held: device tensors of amskv_cross_held_bytes bytes each."""
+    """K, V: bf16 states at the strides of `cross`; K_held, V_held: device tensors of amskv_cross_held_bytes bytes each: a smaller one is
+    refused with AMSKV_ERR_ARENA_TOO_SMALL, a larger one, which belongs to another shape, with AMSKV_ERR_INVALID_ARG, here and by
+    the calls that read them.  Raw addresses are taken as they are."""
     if _lib is None:
         load_library()
     try:
         status = _hold(cross, K, V, K_held, V_held, lengths, offsets, stream)
     except _UNUSUAL:
-        status = _lib.amskv_cross_hold(cross, _ptr(K), _ptr(V), _ptr(K_held), _ptr(V_held), _ptr(lengths), _ptr(offsets), _stream(stream))
+        status = _right_size(cross, offsets, K_held, V_held) or \
+            _lib.amskv_cross_hold(cross, _ptr(K), _ptr(V), _ptr(K_held), _ptr(V_held), _ptr(lengths), _ptr(offsets), _stream(stream))
     if status:
         _check(status, "amskv_cross_hold")
 
@@ -551,6 +567,7 @@ def amskv_cross_export(cross, K_held, V_held, K_out, V_out, lengths=None, offset
     try:
         status = _export(cross, K_held, V_held, K_out, V_out, lengths, offsets, stream)
     except _UNUSUAL:
-        status = _lib.amskv_cross_export(cross, _ptr(K_held), _ptr(V_held), _ptr(K_out), _ptr(V_out), _ptr(lengths), _ptr(offsets), _stream(stream))
+        status = _right_size(cross, offsets, K_held, V_held) or \
+            _lib.amskv_cross_export(cross, _ptr(K_held), _ptr(V_held), _ptr(K_out), _ptr(V_out), _ptr(lengths), _ptr(offsets), _stream(stream))
     if status:
         _check(status, "amskv_cross_export")

@@ -7,6 +7,9 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <cstdint>
+#include <initializer_list>
+
+#include "../../include/amskv.h"
 
 namespace {
 
@@ -22,11 +25,13 @@ Attend attend_fn = nullptr;
 AppendRotary append_rotary_fn = nullptr;
 Rotate rotate_fn = nullptr;
 Cross cross_fn = nullptr;
+typedef int32_t (*HeldBytes)(const void*, int32_t, uint64_t*);
 Held hold_fn = nullptr, export_fn = nullptr;
+HeldBytes held_bytes_fn = nullptr;
 PyObject *rope_class = nullptr, *strides_class = nullptr, *cross_class = nullptr;
 PyObject* lookup = nullptr;  // asked once, when a call first leaves the stream to torch: (current device, current stream) functions
 PyObject *get_device = nullptr, *get_stream = nullptr;  // its answer; None: there is no device
-PyObject *name_data_ptr = nullptr, *name_cuda_stream = nullptr;
+PyObject *name_data_ptr = nullptr, *name_cuda_stream = nullptr, *name_nbytes = nullptr;
 
 bool integer(PyObject* o, int32_t* out) {
   const long v = PyLong_AsLong(o);
@@ -171,6 +176,26 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
+// Held tensors have the size that the call's shape says: a larger one was held with another shape, which the call would read wrongly
+// (where the groups' bytes begin follows from it), a smaller one does not hold it.  Addresses have no size.
+bool right_size(const void* cross, bool packed, PyObject* x, PyObject* y, int32_t* status) {
+  uint64_t need = 0;
+  *status = AMSKV_OK;
+  // (what the shape is refused for, the call itself says; one of states that are not held is none of these)
+  if (!cross || !held_bytes_fn || held_bytes_fn(cross, packed, &need) != AMSKV_OK || need == 0) return true;
+  for (PyObject* o : {x, y}) {
+    if (o == Py_None || PyLong_Check(o)) continue;
+    PyObject* n = PyObject_GetAttr(o, name_nbytes);
+    if (!n) return false;
+    const unsigned long long have = PyLong_AsUnsignedLongLong(n);
+    Py_DECREF(n);
+    if (have == (unsigned long long)-1 && PyErr_Occurred()) return false;
+    if (have != need) *status = have < need ? AMSKV_ERR_ARENA_TOO_SMALL : AMSKV_ERR_INVALID_ARG;
+    if (*status != AMSKV_OK) return true;
+  }
+  return true;
+}
+
 // (cross, Q, K, V, O, lengths, offsets, workspace, workspace_bytes, stream) -> status
 PyObject* cross_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t status;
@@ -179,39 +204,42 @@ PyObject* cross_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!arguments(n, 10, cross_fn) || !structure(a[0], cross_class, &cross)) return nullptr;
   for (int i = 0; i < 7; ++i)
     if (!tensor(a[1 + i], &t[i])) return nullptr;
-  if (!wide(a[8], &bytes) || !stream(a[9], &st)) return nullptr;
+  if (!wide(a[8], &bytes) || !stream(a[9], &st) || !right_size(cross, a[6] != Py_None, a[2], a[3], &status)) return nullptr;
+  if (status != AMSKV_OK) return PyLong_FromLong(status);
   Py_BEGIN_ALLOW_THREADS
   status = cross_fn(cross, t[0], t[1], t[2], t[3], t[4], t[5], t[6], (uint64_t)bytes, st);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(status);
 }
 
-// (cross, K, V, K_held, V_held, lengths, offsets, stream), or the held tensors first -> status
-PyObject* held(Held fn, PyObject* const* a, Py_ssize_t n) {
+// (cross, K, V, K_held, V_held, lengths, offsets, stream), or the held tensors first -> status; at: where they are
+PyObject* held(Held fn, int at, PyObject* const* a, Py_ssize_t n) {
   int32_t status;
   void *cross, *t[6], *st;
   if (!arguments(n, 8, fn) || !structure(a[0], cross_class, &cross)) return nullptr;
   for (int i = 0; i < 6; ++i)
     if (!tensor(a[1 + i], &t[i])) return nullptr;
-  if (!stream(a[7], &st)) return nullptr;
+  if (!stream(a[7], &st) || !right_size(cross, a[6] != Py_None, a[at], a[at + 1], &status)) return nullptr;
+  if (status != AMSKV_OK) return PyLong_FromLong(status);
   Py_BEGIN_ALLOW_THREADS
   status = fn(cross, t[0], t[1], t[2], t[3], t[4], t[5], st);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(status);
 }
-PyObject* cross_hold(PyObject*, PyObject* const* a, Py_ssize_t n) { return held(hold_fn, a, n); }
-PyObject* cross_export(PyObject*, PyObject* const* a, Py_ssize_t n) { return held(export_fn, a, n); }
+PyObject* cross_hold(PyObject*, PyObject* const* a, Py_ssize_t n) { return held(hold_fn, 3, a, n); }
+PyObject* cross_export(PyObject*, PyObject* const* a, Py_ssize_t n) { return held(export_fn, 1, a, n); }
 
-// bind_held(addresses of amskv_cross_hold, amskv_cross_export), after bind_operators()
+// bind_held(addresses of amskv_cross_hold, amskv_cross_export, amskv_cross_held_bytes), after bind_operators()
 PyObject* bind_held(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void *f, *g;
-  if (n != 2) {
-    PyErr_SetString(PyExc_TypeError, "two arguments expected");
+  void *f, *g, *h;
+  if (n != 3) {
+    PyErr_SetString(PyExc_TypeError, "three arguments expected");
     return nullptr;
   }
-  if (!address(a[0], &f) || !address(a[1], &g)) return nullptr;
+  if (!address(a[0], &f) || !address(a[1], &g) || !address(a[2], &h)) return nullptr;
   hold_fn = reinterpret_cast<Held>(f);
   export_fn = reinterpret_cast<Held>(g);
+  held_bytes_fn = reinterpret_cast<HeldBytes>(h);
   Py_RETURN_NONE;
 }
 
@@ -265,5 +293,6 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycalls", nullptr, -1, methods, n
 PyMODINIT_FUNC PyInit__pycalls() {
   name_data_ptr = PyUnicode_InternFromString("data_ptr");
   name_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-  return name_data_ptr && name_cuda_stream ? PyModule_Create(&module) : nullptr;
+  name_nbytes = PyUnicode_InternFromString("nbytes");
+  return name_data_ptr && name_cuda_stream && name_nbytes ? PyModule_Create(&module) : nullptr;
 }
