@@ -17,14 +17,14 @@
 //   a channel of Q 30 times, K there as much smaller       0.0015    0.0015  0.014     0.0035       0.0016      0.0047
 //   300 times                                              0.0016    0.0016  0.14      0.027        0.0074      0.0052
 // and as measured (us; 64 units 4096 x 6421 and 2304 x 3925 at head dim 128, 3840 units 256 x 530 at 64): here 679, 263, 190; two e2m3 618, 242,
-// 174; three 679, 269, 194; four, which lose nothing anywhere, 728, 316, 198.  A product of both parts takes 57 ns of a SIMD for 64 channels, bf16's
+// 174; three 679, 269, 194; four, which lose nothing in either way, 728, 316, 198.  A product of both parts takes 57 ns of a SIMD for 64 channels, bf16's
 // 74 (a part of 6 bits 15).  V becomes bf16 on its way to LDS, once for all waves: weights in 6 bits would have to be split in two for
 // every block, which takes the vector ALUs more (a conversion of 32 numbers 38 ns, back 33) than the matrix cores save.
 //
-// Bound, and what it measured.  Head dim 128, 64 units: the matrix pipes and the power they take, 4096 x 6421 by teams of eight 576 to 601
-// us (1.43 to 1.50 PFLOP/s; codes of 8 bits through bf16 784), 2304 x 3925 by teams of four 234 to 255, 576 x 1076 29.  Head dim 64, 3840
-// units: the vector ALUs (0.66 of a SIMD's cycles, the matrix pipe 0.20), 256 x 530 174 to 181 us (with 256 of the keys read in place as
-// bf16, by attend_rows.hpp, 195 to 201), x 2066 481 to 503 (1.03 to 1.08 PFLOP/s).
+// Bound, and what it measured.  Head dim 128, 64 units: the matrix pipes (0.57 of a SIMD's cycles) and the power they take, 4096 x 6421 by teams
+// of eight 671 to 712 us (1.21 to 1.29 PFLOP/s; codes of 8 bits through bf16 784), 2304 x 3925 by teams of four 258 to 269, 576 x 1076 33.
+// Head dim 64, 3840 units: the vector ALUs (0.66 of a SIMD's cycles, the matrix pipe 0.24), 256 x 530 187 to 195 us (with 256 of the keys read in
+// place as bf16, by attend_rows.hpp, 193 to 206), x 2066 554 (0.94 PFLOP/s).
 //
 // kExt: rows of bf16 may follow the codes (a scale that is read in place); they are walked as in attend_rows.hpp, with Q as it is.
 #pragma once

@@ -119,9 +119,11 @@ inline Division divide(int head_dim, long long units, long long n, int keys) {
 // keys in rounds, a block taking a wave by itself `alone`, and waves that share a SIMD `shared` each once that is longer, `around` a workgroup:
 // arguments, Q and its parts, first tiles, O.  Beside it K, V, Q and O come from memory (5 TB/s) and K and V from the L2s again for every row
 // tile (lone waves 10 TB/s, teams 6.5); the three are added in squares.  Splits cost a launch and the way of their sums.
-// The constants are those that fit 322 shapes best, 310 of them drawn, 1 to 25 forms and splits each (MI355X; rms 0.14 of the time); the choice
-// then takes 1.018 of the best on average, the rule of 16-bit keys 1.078 (up to 2.97).  us, that rule / this: head dim 128, 64 units, 4 rows x 14400
-// 48 / 25; head dim 64, 1024 x 1 x 4000 115 / 45, 288 x 1 x 9266 101 / 42, 143 x 8 x 214 x 35 38 / 30.
+// The constants are a fit to 322 shapes, 310 of them drawn, 1 to 25 forms and splits each (MI355X), but for those of teams at head dim 128, which
+// were set by hand from later kernels, 64 units 4096 x 6421 and the steps before it.  With the kernels as they are the estimate is off by
+// 0.16 of the time (rms) over 272 other shapes, 260 of them drawn, and the choice takes 1.017 of the best on average, 1.36 at most (head
+// dim 64, 32 units, 315 x 15916); constants fitted to these anew would take 1.014.  The rule of 16-bit keys took 1.078 (up to 2.97).  us, that
+// rule / this: head dim 128, 64 units, 4 rows x 14400 48 / 25; head dim 64, 1024 x 1 x 4000 115 / 45, 288 x 1 x 9266 101 / 42, 143 x 8 x 214 x 35 38 / 30.
 inline double estimate4(int head_dim, double units, double n, double keys, Form f, int splits) {
   struct Times {
     double alone, shared, around;

@@ -6,7 +6,9 @@
 // 5.7 TB/s read + write), read back 41 (6.2); 8 documents of up to 16000, 8 heads, 101 to 113 (5.3 to 5.9) and 92 (6.5); 77 states of a short prompt
 // 2.9 and 2.6.  A workgroup has 512 bytes of a row, of heads side by side in a token-major tensor, and the heads of a block of rows go to
 // neighbouring workgroups: with one head to a workgroup 63 to 71, 135 to 140 us.  What is read back goes past the caches: 8 x 16000 states of 8
-// heads 126 -> 93 us, 96 x 250 of 16, head dim 64, 19.2 -> 17.6.  (Loads past them: 42.7 us for 35.8 where a projection has just made the states.)
+// heads 126 -> 93 us, 96 x 250 of 16, head dim 64, 19.2 -> 17.6.  With a kernel behind that reads it the two differ by a tenth either way: K and V of
+// 8 MB both kernels 11.1 us past the caches and 11.9 through them, 34 MB 26.9 and 24.6, 201 MB 121.8 and 118.5, 524 MB 303 both.  (Loads past
+// them: 42.7 us for 35.8 where a projection has just made the states.)
 #include "codes.hpp"
 
 namespace amskv {
