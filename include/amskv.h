@@ -211,8 +211,9 @@ typedef struct {
  * A token's values depend on nothing but the token: slots may start at any token and capacities are any number of them.
  * The attention's products take K as held and Q as it is (in launches of many rows elements below 2^-14 of the largest magnitude of their
  * AMSKV_KV4_GROUP channels may be off by 2^-21 of that magnitude, and the products of 8 channels, 8 i .. 8 i + 7, are added up in units of
- * 2^-13 of the largest).  The sum of |q| |k| over the channels has to be below 2^127, and times softmax_scale below 2^124.  A row of Q with a NaN comes out as NaN, and so does one with an infinite element (but in launches of few rows not
- * where all of its scores are -inf: they weigh nothing).
+ * 2^-13 of the largest).  The sum of |q| |k| over the channels has to be below 2^127, and times softmax_scale below 2^124 (a score that is
+ * beyond fp32 on the negative side weighs nothing).  A row of Q with a NaN comes out as NaN, and so does one with an infinite element (but in
+ * launches of few rows not where all of its scores are -inf).
  * amskv_cache_bytes_held counts half a byte per element and one per group.  The modes, layouts and limits of the 8-bit
  * cache, the similarity and density calls among them. */
 

@@ -75,7 +75,7 @@ def _step(D, B, H, before, queries, q, k, v, borrow, scale=0.0):
 
 # ---------------------------------------------------------------- a reference that moves far
 @steps
-@pytest.mark.parametrize("far", [2.0 ** 10, 2.0 ** 30, 2.0 ** 60])
+@pytest.mark.parametrize("far", [2.0 ** 10, 2.0 ** 30, 2.0 ** 60, 2.0 ** 100])
 @pytest.mark.parametrize("borrow", [False, True])
 def test_scores_behind_far_lower_ones(D, shape, far, borrow):
     """The first scale's scores are some -far^2; the second's come out as if alone.  (With queries of few bits.)"""
@@ -90,7 +90,7 @@ def test_scores_behind_far_lower_ones(D, shape, far, borrow):
 
 
 @calls
-@pytest.mark.parametrize("far", [2.0 ** 10, 2.0 ** 30, 2.0 ** 60])
+@pytest.mark.parametrize("far", [2.0 ** 10, 2.0 ** 30, 2.0 ** 60, 2.0 ** 100])
 def test_held_scores_behind_far_lower_ones(D, shape, far):
     """The same over held states: the first third of every length is far below."""
     B, H, queries, keys = shape
